@@ -22,7 +22,8 @@
  *     margin that no rounding crosses).
  *
  * Conventions
- *   - All pointers in the signatures are HOST pointers unless stated otherwise.
+ *   - All pointers in the signatures are HOST pointers unless stated otherwise (the operators on
+ *     rows, and lda_doc_topics, take device pointers).
  *     The library copies what it needs; the caller keeps ownership of its buffers
  *     and may free them as soon as a call returns.
  *   - Token order at the boundary is the caller's CSR (document-major) order:
@@ -252,10 +253,151 @@ int lda_get_sparse_table(lda_ctx* ctx, int32_t w, int32_t cap_entries, int32_t* 
 int lda_get_beta_table(lda_ctx* ctx, uint32_t* split, uint32_t* alias, uint32_t* cap,
                        uint64_t* mass);
 
+/* ---- operators on rows (beside the sampler; no context) ------------------------------------
+ * Teacher rows out of topic counts, the distillation loss that trains a student on them, and the
+ * verification of tokens that a draft proposed.  All pointers inside the structs and all outputs
+ * are DEVICE pointers; the structs themselves are read on the host during the call.  The calls
+ * enqueue on hip_stream (NULL: the null stream) and return; they allocate nothing, wait for
+ * nothing and can be captured into a graph.  The current device must be the one that holds the
+ * memory and the stream.  Strides count elements; inside a row elements are adjacent.  Inputs may
+ * be read by several calls at once; two calls that may overlap in time need workspaces of their
+ * own.  Outputs must not overlap inputs.  Errors are those of the other entry points, the message
+ * is that of lda_last_error(NULL) on the calling thread. */
+#define LDA_F32 0
+#define LDA_F16 1
+#define LDA_BF16 2
+#define LDA_I32 0
+#define LDA_I64 1
+
+/*
+ * Distillation from a teacher's top logits.  Row i of the student has one logit S_v for each of
+ * `classes` classes (topics, words); row i of the teacher has `slots` slots, an id and a logit t_j each.
+ * A slot whose id lies outside [0, classes) is empty; ids may come in any order and more than once
+ * (their masses add up).  With T = temperature:
+ *   q = softmax(S / T), where q_v = 0 for S_v = -infinity;
+ *   log_norm == NULL: p_j = softmax over the row's slots of t_j / T, r = 0;
+ *   otherwise:        p_j = exp(t_j / T - log_norm), and the mass that is left, if any, is spread
+ *                     evenly over the classes that no slot names: r = max(0, 1 - sum p_j) / their number
+ *                     (a teacher known by its largest masses and a floor, as theta_dk is of n_kd);
+ *   loss = T^2 ( sum_j p_j (log p_j - log q_id_j) + sum over classes without a slot of r (log r - log q_v) )
+ *   d loss / d S_v = T (M q_v - P_v),  P_v = the p_j of v's slots, or r;  M = sum P_v.
+ * A term of mass 0 is 0.  A row without any mass has loss 0 and gradient 0, whatever S holds.  Mass on a
+ * class of q_v = 0 makes the loss +infinity; the gradient is the formula's.  NaN in S, or
+ * +infinity, makes the row's loss and gradient NaN; what an empty slot's logit holds does not count.
+ * Sums are 32-bit inside a thread over S, 64-bit beyond and for the teacher.
+ */
+typedef struct lda_distill_rows {
+    int64_t rows;            /* >= 0 */
+    int32_t classes;         /* >= 1 */
+    int32_t slots;           /* 0 .. 1024 (more: LDA_ERR_UNSUPPORTED) */
+    const void* logits;      /* [rows][classes], rows logits_stride apart */
+    int64_t logits_stride;
+    const void* ids;         /* [rows][slots] */
+    int64_t ids_stride;
+    const void* teacher;     /* [rows][slots] */
+    int64_t teacher_stride;
+    const float* log_norm;   /* [rows] or NULL */
+    const float* weight;     /* weight of row i at weight[i * weight_stride]; NULL: 1.  The gradient's factor.
+                                Rows of weight 0 are left out: gradient 0 (lda_distill_step: and
+                                loss 0), and their logits are not looked at.  Not used by lda_distill_loss */
+    int64_t weight_stride;   /* 0: one weight for every row */
+    int32_t logits_type;     /* LDA_F32, LDA_F16, LDA_BF16 */
+    int32_t ids_type;        /* LDA_I32, LDA_I64 */
+    int32_t teacher_type;    /* as logits_type */
+    float temperature;       /* 1/1024 .. 1024 */
+    void* workspace;         /* at least lda_distill_workspace() bytes, aligned to 16; what it holds is of
+                                no use after the call's work */
+    int64_t workspace_bytes;
+    void* hip_stream;
+    int32_t reserved[4];     /* must be zero */
+} lda_distill_rows;
+
+/* Bytes of workspace that a call on these rows needs (may be 0), or a negative LDA_ERR_*. */
+int64_t lda_distill_workspace(const lda_distill_rows* rows);
+/* loss [rows]; stats [rows][2] for lda_distill_grad (the row's largest logit and the sum of
+ * exp((S - largest) / T)), or NULL.  Both 32-bit floats. */
+int lda_distill_loss(const lda_distill_rows* rows, float* loss, float* stats);
+/* The gradient of sum_i weight_i loss_i, [rows][classes] in the logits' type, rows grad_stride
+ * apart; what lies between rows is left as it was.  stats: of lda_distill_loss on the same rows. */
+int lda_distill_grad(const lda_distill_rows* rows, const float* stats, void* grad, int64_t grad_stride);
+/* Both in one call, for a program that knows the weights beforehand: the logits are read once from
+ * memory where they fit the registers. */
+int lda_distill_step(const lda_distill_rows* rows, float* loss, void* grad, int64_t grad_stride);
+
+/*
+ * Verification of drafted tokens.  Sequence b has n_b = lengths[b] drafted tokens x_i (all `steps` of
+ * them if lengths is NULL; lengths are clamped to [0, steps]), drawn from the rows q_i of `draft`, and n_b + 1 rows
+ * p_i of `target`.  Draft i is accepted if accept_u[b][i] * q_i(x_i) < p_i(x_i) and all before it are; a
+ * token outside [0, classes) is not.  accepted[b] = a, the number of accepted drafts, and out[b] is
+ * x_0 .. x_{a-1}, then one drawn token, then -1 up to steps + 1 entries.  The token is drawn from masses
+ * m_v:  a = n_b: p_a(v);  else max(0, p_a(v) - q_a(v)), or p_a(v) if none of these is positive.
+ * It is the first v with m_v > 0 and m_0 + .. + m_v > draw_u[b] * (sum of all), the last v with m_v > 0
+ * if there is none such, -1 if no m_v is positive.  Products and sums are 64-bit.  Masses need not
+ * sum to 1; a NaN has no mass.  The result is that of these random numbers, and distributed
+ * as draws from the target are.  steps = 0: plain draws (draft, tokens, accept_u are not looked at).
+ */
+typedef struct lda_draft_rows {
+    int64_t sequences;       /* >= 0 */
+    int32_t steps;           /* 0 .. 4096 */
+    int32_t classes;         /* >= 1 */
+    const void* target;      /* [sequences][steps + 1][classes] */
+    int64_t target_sequence_stride, target_row_stride;
+    const void* draft;       /* [sequences][steps][classes] */
+    int64_t draft_sequence_stride, draft_row_stride;
+    const void* tokens;      /* [sequences][steps] */
+    int64_t tokens_stride;
+    const int32_t* lengths;  /* [sequences] or NULL */
+    const float* accept_u;   /* [sequences][steps] */
+    int64_t accept_u_stride;
+    const float* draw_u;     /* [sequences] */
+    int32_t probs_type;      /* of target and draft: LDA_F32, LDA_F16, LDA_BF16 */
+    int32_t tokens_type;     /* of tokens and out: LDA_I32, LDA_I64 */
+    void* workspace;         /* at least lda_verify_workspace() bytes, aligned to 16 */
+    int64_t workspace_bytes;
+    void* hip_stream;
+    int32_t reserved[4];     /* must be zero */
+} lda_draft_rows;
+
+int64_t lda_verify_workspace(const lda_draft_rows* rows);
+/* accepted [sequences]; out [sequences][steps + 1], rows out_stride apart */
+int lda_verify_drafts(const lda_draft_rows* rows, int32_t* accepted, void* out, int64_t out_stride);
+
+/*
+ * Top topics of documents: for each, the `slots` topics that most of its tokens have, the most
+ * frequent first, ties to the lower topic, with logits log(n + alpha), n the number of
+ * tokens; slots without a topic get id -1 and logit -infinity.  log_norm = log(L + K alpha), L the
+ * tokens counted: with these three lda_distill_loss learns the document's whole
+ * theta_dk = (n_dk + alpha) / (L + K alpha), at temperature 1, when slots holds all of its topics.
+ */
+typedef struct lda_topic_rows {
+    int64_t rows;            /* rows of output, >= 0 */
+    const int32_t* docs;     /* [rows] the document of each row, or NULL: row i is document i.  A document
+                                outside [0, documents) is empty */
+    int64_t documents;       /* >= 0; with docs == NULL at least rows */
+    const void* offsets;     /* [documents + 1] document d is z[offsets[d]] .. z[offsets[d + 1] - 1] */
+    int32_t offsets_type;    /* LDA_I32, LDA_I64 */
+    int32_t K;               /* 1 .. 2^20 - 2; a z outside [0, K) is not counted */
+    const int32_t* z;        /* [tokens] */
+    int64_t tokens;          /* offsets are clamped to [0, tokens]; a document of more than 2^31 - 1 tokens
+                                is cut there */
+    int32_t slots;           /* 1 .. 1024 (more: LDA_ERR_UNSUPPORTED) */
+    int32_t reserved_word;   /* must be zero */
+    double alpha;            /* > 0 */
+    void* hip_stream;
+    int32_t reserved[4];     /* must be zero */
+} lda_topic_rows;
+
+/* ids [rows][slots], logits [rows][slots], log_norm [rows] or NULL */
+int lda_top_topics(const lda_topic_rows* rows, int32_t* ids, float* logits, float* log_norm);
+/* The same from the context's current assignment, its K and alpha, on its stream; docs and the outputs are
+ * device pointers.  Any state.  With stream_block_tokens: LDA_ERR_UNSUPPORTED (z is in host memory). */
+int lda_doc_topics(lda_ctx* ctx, int64_t rows, const int32_t* docs, int32_t slots, int32_t* ids,
+                   float* logits, float* log_norm);
+
 /* Wait for all work enqueued by this context. */
 int lda_sync(lda_ctx* ctx);
-/* Message of the last error of this context (ctx == NULL: of the last failed lda_init on this
- * thread).  The string is owned by the library and valid until the next call. */
+/* Message of the last error of this context (ctx == NULL: of the last failed call on this thread,
+ * lda_init and the operators on rows among them).  The string is owned by the library and valid until the next call. */
 const char* lda_last_error(const lda_ctx* ctx);
 /* Free the context and all its device memory.  NULL is allowed. */
 void lda_destroy(lda_ctx* ctx);

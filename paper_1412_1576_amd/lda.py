@@ -26,7 +26,9 @@ EXPORTS = [
     "lda_update_counts", "lda_loglik", "lda_loglik_noalloc",
     "lda_num_tokens", "lda_sweep_index", "lda_get_z", "lda_set_z", "lda_get_nk",
     "lda_get_nkw_row", "lda_get_ndk_row", "lda_get_alias_row", "lda_get_sparse_table",
-    "lda_get_beta_table", "lda_sync", "lda_last_error", "lda_destroy",
+    "lda_get_beta_table",
+    "lda_distill_workspace", "lda_distill_loss", "lda_distill_grad", "lda_distill_step",
+    "lda_verify_workspace", "lda_verify_drafts", "lda_top_topics", "lda_doc_topics", "lda_sync", "lda_last_error", "lda_destroy",
 ]
 
 
@@ -51,6 +53,43 @@ class lda_options(C.Structure):
         ("doc_refresh", C.c_int32),
         ("stream_block_tokens", C.c_int32),
         ("reserved", C.c_int32 * 5),
+    ]
+
+
+class lda_distill_rows(C.Structure):
+    _fields_ = [
+        ("rows", C.c_int64), ("classes", C.c_int32), ("slots", C.c_int32),
+        ("logits", C.c_void_p), ("logits_stride", C.c_int64),
+        ("ids", C.c_void_p), ("ids_stride", C.c_int64),
+        ("teacher", C.c_void_p), ("teacher_stride", C.c_int64),
+        ("log_norm", C.c_void_p), ("weight", C.c_void_p), ("weight_stride", C.c_int64),
+        ("logits_type", C.c_int32), ("ids_type", C.c_int32), ("teacher_type", C.c_int32),
+        ("temperature", C.c_float),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64), ("hip_stream", C.c_void_p),
+        ("reserved", C.c_int32 * 4),
+    ]
+
+
+class lda_draft_rows(C.Structure):
+    _fields_ = [
+        ("sequences", C.c_int64), ("steps", C.c_int32), ("classes", C.c_int32),
+        ("target", C.c_void_p), ("target_sequence_stride", C.c_int64),
+        ("target_row_stride", C.c_int64),
+        ("draft", C.c_void_p), ("draft_sequence_stride", C.c_int64), ("draft_row_stride", C.c_int64),
+        ("tokens", C.c_void_p), ("tokens_stride", C.c_int64), ("lengths", C.c_void_p),
+        ("accept_u", C.c_void_p), ("accept_u_stride", C.c_int64), ("draw_u", C.c_void_p),
+        ("probs_type", C.c_int32), ("tokens_type", C.c_int32),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64), ("hip_stream", C.c_void_p),
+        ("reserved", C.c_int32 * 4),
+    ]
+
+
+class lda_topic_rows(C.Structure):
+    _fields_ = [
+        ("rows", C.c_int64), ("docs", C.c_void_p), ("documents", C.c_int64),
+        ("offsets", C.c_void_p), ("offsets_type", C.c_int32), ("K", C.c_int32),
+        ("z", C.c_void_p), ("tokens", C.c_int64), ("slots", C.c_int32), ("reserved_word", C.c_int32),
+        ("alpha", C.c_double), ("hip_stream", C.c_void_p), ("reserved", C.c_int32 * 4),
     ]
 
 
@@ -105,6 +144,14 @@ def load_library():
                                            C.POINTER(C.c_uint64)]),
         "lda_get_beta_table": (C.c_int, [vp, _u32p, _u32p, C.POINTER(C.c_uint32),
                                          C.POINTER(C.c_uint64)]),
+        "lda_distill_workspace": (C.c_int64, [C.POINTER(lda_distill_rows)]),
+        "lda_distill_loss": (C.c_int, [C.POINTER(lda_distill_rows), vp, vp]),
+        "lda_distill_grad": (C.c_int, [C.POINTER(lda_distill_rows), vp, vp, C.c_int64]),
+        "lda_distill_step": (C.c_int, [C.POINTER(lda_distill_rows), vp, vp, C.c_int64]),
+        "lda_verify_workspace": (C.c_int64, [C.POINTER(lda_draft_rows)]),
+        "lda_verify_drafts": (C.c_int, [C.POINTER(lda_draft_rows), vp, vp, C.c_int64]),
+        "lda_top_topics": (C.c_int, [C.POINTER(lda_topic_rows), vp, vp, vp]),
+        "lda_doc_topics": (C.c_int, [vp, C.c_int64, vp, C.c_int32, vp, vp, vp]),
         "lda_sync": (C.c_int, [vp]),
         "lda_last_error": (C.c_char_p, [vp]),
         "lda_destroy": (None, [vp]),
@@ -153,6 +200,7 @@ class Lda:
             opt.dev_free = self._free_cb
         self.D = len(doc_offsets) - 1
         self.V, self.K = int(V), int(K)
+        self.stream = int(stream) if stream else 0
         rc = L.lda_init(C.byref(self._h), self.D, self.V, self.K, doc_offsets, word_ids,
                         float(alpha), float(beta), int(seed), C.byref(opt))
         if rc != LDA_OK:
@@ -233,6 +281,14 @@ class Lda:
         row = np.empty(self.K, np.int32)
         self._ck(_lib.lda_get_ndk_row(self._h, int(d), row))
         return row
+
+    def doc_topics(self, slots, docs=None):
+        """(ids int32, logits float32, log_norm float32) of documents as torch tensors on the GPU:
+        their `slots` most frequent topics with log(n_dk + alpha), and log(L + K alpha) -- teacher
+        rows for operators.distill_loss.  docs: int32 GPU tensor (None: every document).  The work is
+        on the context's stream; torch's current stream waits for it."""
+        from . import operators
+        return operators.doc_topics(self, slots, docs)
 
     def get_alias_row(self, w):
         split = np.empty(self.K, np.uint32)

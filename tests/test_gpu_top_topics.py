@@ -1,0 +1,233 @@
+"""Top topics of documents on the GPU against counting on the host; from tensors and from a sampler.
+Ids are equal; a logit is the logarithm in 64 bits rounded once (half a step, 2^-24), of a value that the
+host's differs from by 2^-50 at most."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ops():
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_1412_1576_amd import operators
+    return operators
+
+
+def reference(z, offsets, K, slots, alpha, docs):
+    n = len(docs)
+    ids, logits, norm = np.full((n, slots), -1), np.full((n, slots), -np.inf), np.zeros(n)
+    for i, d in enumerate(docs):
+        part = z[offsets[d]:offsets[d + 1]] if 0 <= d < len(offsets) - 1 else z[:0]
+        part = part[(part >= 0) & (part < K)]
+        topic, count = np.unique(part, return_counts=True)
+        order = np.lexsort((topic, -count))[:slots]
+        ids[i, :len(order)] = topic[order]
+        logits[i, :len(order)] = np.log(count[order] + alpha)
+        norm[i] = np.log(len(part) + K * alpha)
+    return ids, logits, norm
+
+
+def same(got, want):
+    ids, logits, norm = [x.cpu().numpy() for x in got]
+    assert np.array_equal(ids, want[0])
+    for g, w in ((logits, want[1]), (norm, want[2])):
+        some = np.isfinite(w)
+        assert np.array_equal(g[~some], w[~some].astype(np.float32))
+        assert (np.abs(g[some] - w[some]) <= np.abs(w[some]) * 2.0 ** -24 * 1.001 + 1e-15).all()
+
+
+def check(ops, z, lengths, K, slots, alpha=0.1, docs=None, dtype=np.int64):
+    offsets = np.concatenate([[0], np.cumsum(lengths)]).astype(dtype)
+    z = np.ascontiguousarray(z[:offsets[-1]], np.int32)
+    on = None if docs is None else torch.tensor(np.asarray(docs, np.int32)).cuda()
+    got = ops.top_topics(torch.from_numpy(z).cuda(), torch.from_numpy(offsets).cuda(), K, slots, alpha, docs=on)
+    same(got, reference(z, offsets, K, slots, alpha, range(len(lengths)) if docs is None else docs))
+    return got
+
+
+def some_z(rng, n, K, flat=0.5):
+    few = rng.integers(0, K, 9)
+    return np.where(rng.random(n) < flat, rng.integers(0, K, n), few[rng.integers(0, 9, n)])
+
+
+@pytest.mark.parametrize("slots", [1, 8, 100, 1024])
+@pytest.mark.parametrize("K", [1, 10, 1000, 12_289, 1_000_000])
+def test_sizes(ops, K, slots):
+    rng = np.random.default_rng(K + slots)
+    lengths = np.concatenate([[0, 1, 2, 63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1023, 1024, 1025],
+                              rng.integers(0, 300, 40), [2047, 2048, 2049, 4095, 4096, 4097, 5000, 0]])
+    check(ops, some_z(rng, lengths.sum(), K), lengths, K, slots)
+
+
+@pytest.mark.parametrize("K", [3, 5000, 100_000, 2 ** 20 - 2])
+def test_long_documents(ops, K):
+    rng = np.random.default_rng(K)
+    lengths = [30_000, 8191, 8192, 8193, 0, 16_384, 200_000, 12_288, 12_289, 65_537]
+    z = some_z(rng, sum(lengths), K)
+    check(ops, z, lengths, K, 64, dtype=np.int32)
+    check(ops, z, lengths, K, 1000)
+
+
+@pytest.mark.parametrize("length", [50, 64, 100, 500, 3000, 40_000])
+def test_ties_and_extremes(ops, length):
+    """Every topic once, every topic twice, one topic alone: ties go to the lower topic."""
+    K = 100_000
+    each = np.arange(length)[::-1] * (K // length)
+    twice = np.repeat(np.arange(length // 2), 2)[::-1]
+    z = np.concatenate([each, twice, np.full(length, K - 1), np.full(length, 0)])
+    lengths = [length, len(twice), length, length]
+    check(ops, z, lengths, K, 7)
+    check(ops, z, lengths, K, 300)
+
+
+def test_topics_outside_and_documents_outside(ops):
+    rng = np.random.default_rng(1)
+    lengths = rng.integers(0, 200, 50)
+    lengths[7] = 9000
+    z = some_z(rng, lengths.sum(), 40)
+    z[::3] = rng.choice([-1, 40, 41, 2 ** 31 - 1, -2 ** 31, 2 ** 20 - 1], len(z[::3]))
+    check(ops, z, lengths, 40, 16)
+    check(ops, z, lengths, 40, 16, docs=[3, 7, 7, -1, 50, 49, 0, 2 ** 31 - 1, 3])
+    check(ops, z, lengths, 40, 16, docs=[])
+
+
+def test_bad_offsets_are_clamped(ops):
+    z = torch.arange(10, dtype=torch.int32, device="cuda")
+    offsets = torch.tensor([-5, 3, 2, 8, 1 << 40, 4], device="cuda")
+    ids, logits, norm = ops.top_topics(z, offsets, 10, 4, 1.0)
+    assert ids.tolist() == [[0, 1, 2, -1], [-1] * 4, [2, 3, 4, 5], [8, 9, -1, -1], [-1] * 4]
+    assert norm.exp().round().int().tolist() == [13, 10, 16, 12, 10]
+
+
+def test_an_empty_assignment(ops):
+    z = torch.zeros(0, dtype=torch.int32, device="cuda")
+    ids, logits, norm = ops.top_topics(z, torch.zeros(4, dtype=torch.int64, device="cuda"), 5, 2, 0.5)
+    assert (ids == -1).all() and torch.isneginf(logits).all() and ids.shape == (3, 2)
+    assert torch.allclose(norm, torch.full((3,), 2.5, device="cuda").log(), rtol=2.0 ** -23)
+    assert ops.top_topics(z, torch.zeros(1, dtype=torch.int64, device="cuda"), 5, 2, 0.5)[0].shape == (0, 2)
+
+
+def test_the_binding_refuses(ops):
+    from paper_1412_1576_amd.lda import LdaError
+    z = torch.zeros(6, dtype=torch.int32, device="cuda")
+    off = torch.tensor([0, 3, 6], device="cuda")
+    for args in ((z.long(), off, 4, 2, 0.1), (z, off.float(), 4, 2, 0.1), (z, off[:0], 4, 2, 0.1),
+                 (z[::2], off, 4, 2, 0.1), (z, off, 1 << 40, 2, 0.1), (z.view(2, 3), off, 4, 2, 0.1)):
+        with pytest.raises(ValueError):
+            ops.top_topics(*args)
+    for args in ((z, off, 0, 2, 0.1), (z, off, 4, 0, 0.1), (z, off, 4, 2000, 0.1), (z, off, 4, 2, 0.0),
+                 (z, off, 2 ** 20, 2, 0.1), (z, off, 4, -3, 0.1)):
+        with pytest.raises(LdaError):
+            ops.top_topics(*args)
+    with pytest.raises(ValueError):
+        ops.top_topics(z, off, 4, 2, 0.1, docs=off)
+
+
+def test_captured_and_replayed(ops):
+    K, D = 500, 300
+    rng = np.random.default_rng(2)
+    lengths = rng.integers(0, 150, D)
+    lengths[5] = 10_000
+    offsets = torch.from_numpy(np.concatenate([[0], np.cumsum(lengths)])).cuda()
+    z = torch.randint(0, K, (int(lengths.sum()),), dtype=torch.int32, device="cuda")
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        ops.top_topics(z, offsets, K, 16, 0.1)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        got = ops.top_topics(z, offsets, K, 16, 0.1)
+    for _ in range(3):
+        z.random_(0, K)
+        graph.replay()
+        torch.cuda.synchronize()
+        for g, w in zip(got, ops.top_topics(z, offsets, K, 16, 0.1)):
+            assert torch.equal(g, w)
+
+
+@pytest.mark.parametrize("own_stream", [False, True])
+def test_of_a_sampler(ops, own_stream):
+    """lda_doc_topics against the sampler's own assignment, in every state, on its stream."""
+    from paper_1412_1576_amd import corpus, lda
+    cfg = corpus.scaled(corpus.CONFIGS["c1"], D=200)
+    doff, words = corpus.make_corpus(cfg)
+    stream = torch.cuda.Stream() if own_stream else None
+    m = lda.Lda(doff, words, cfg.V, cfg.K, cfg.alpha, cfg.beta, seed=3,
+                stream=stream.cuda_stream if own_stream else None)
+    for it in range(3):
+        same(m.doc_topics(20), reference(m.get_z(), doff, cfg.K, 20, cfg.alpha, range(200)))
+        m.build_alias()
+        m.sweep(2)
+        got = m.doc_topics(20, torch.tensor([5, 199, 0, 5, -1, 200], dtype=torch.int32, device="cuda"))
+        same(got, reference(m.get_z(), doff, cfg.K, 20, cfg.alpha, [5, 199, 0, 5, -1, 200]))
+        m.rebuild_counts()
+    row = m.get_ndk_row(7)
+    ids, logits, _ = m.doc_topics(cfg.K)
+    assert ids[7, :int((row > 0).sum())].sort()[0].tolist() == np.flatnonzero(row).tolist()
+    with pytest.raises(lda.LdaError, match="1024"):
+        m.doc_topics(1025)
+    with pytest.raises(lda.LdaError):
+        m.doc_topics(0)
+    with pytest.raises(ValueError):
+        m.doc_topics(4, torch.zeros(2, device="cuda"))
+    m.close()
+
+
+def test_of_a_streamed_sampler(ops):
+    from paper_1412_1576_amd import corpus, lda
+    cfg = corpus.scaled(corpus.CONFIGS["c1"], D=200)
+    doff, words = corpus.make_corpus(cfg)
+    m = lda.Lda(doff, words, cfg.V, cfg.K, cfg.alpha, cfg.beta, stream_block_tokens=5000)
+    with pytest.raises(lda.LdaError, match="streamed"):
+        m.doc_topics(4)
+    m.close()
+
+
+def test_together(ops):
+    """The operators as they are used: a sampler's documents are the teacher, a student of one linear
+    layer over the documents' words learns their topics, proposes topics for new tokens, and its proposals
+    are verified against the sampler's own theta."""
+    from paper_1412_1576_amd import corpus, lda
+    cfg = corpus.scaled(corpus.CONFIGS["c1"], D=400)
+    doff, words = corpus.make_corpus(cfg)
+    m = lda.Lda(doff, words, cfg.V, cfg.K, cfg.alpha, cfg.beta, seed=1)
+    for _ in range(5):
+        m.build_alias()
+        m.sweep(2)
+        m.rebuild_counts()
+    ids, logits, log_norm = m.doc_topics(cfg.K)
+    # theta is what the rows stand for: all of the document's topics have a slot
+    theta = torch.zeros(cfg.D, cfg.K, dtype=torch.float64)
+    for d in range(0, cfg.D, 57):
+        row = m.get_ndk_row(d)
+        theta[d] = torch.from_numpy((row + cfg.alpha) / (row.sum() + cfg.K * cfg.alpha))
+    bag = torch.zeros(cfg.D, cfg.V, device="cuda")
+    doc = torch.from_numpy(np.repeat(np.arange(cfg.D), np.diff(doff))).cuda()
+    bag.index_put_((doc, torch.from_numpy(words).long().cuda()), torch.ones(len(words), device="cuda"),
+                   accumulate=True)
+    student = torch.nn.Linear(cfg.V, cfg.K, device="cuda")
+    out = student(bag)
+    loss = ops.distill_loss(out, ids, logits, log_norm=log_norm)
+    loss.mean().backward()
+    q = torch.softmax(out.detach().double(), 1).cpu()
+    for d in range(0, cfg.D, 57):
+        # logits and norm carry 2^-24 of up to 5 each, theta then 1e-6; the loss that of log theta too
+        want = (theta[d] * (theta[d].log() - q[d].log())).sum()
+        assert abs(float(loss.detach()[d]) - float(want)) <= 1e-5 * max(1.0, float(want))
+    step = ops.distill_loss_and_grad(out.detach(), ids, logits, log_norm=log_norm,
+                                     weight=torch.full((cfg.D,), 1.0 / cfg.D, device="cuda"))
+    assert torch.equal(step[0], loss.detach())
+    want = step[1].t() @ bag
+    assert torch.allclose(student.weight.grad, want, rtol=1e-4, atol=1e-6)
+    # four topics proposed for each document from the student, against theta
+    docs = torch.arange(0, cfg.D, 57)
+    p = theta[docs][:, None].expand(-1, 5, -1).float().cuda()
+    draft = q[docs][:, None].expand(-1, 4, -1).float().cuda()
+    tokens = torch.multinomial(q[docs], 4, replacement=True).cuda()
+    accepted, got = ops.verify_drafts(p, draft, tokens, torch.rand(len(docs), 4, device="cuda"),
+                                      torch.rand(len(docs), device="cuda"))
+    for i, a in enumerate(accepted.tolist()):
+        assert torch.equal(got[i, :a], tokens[i, :a]) and 0 <= got[i, a] < cfg.K and (got[i, a + 1:] == -1).all()
+    m.close()
