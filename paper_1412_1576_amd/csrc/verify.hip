@@ -2,19 +2,23 @@
 // drafts are accepted, and a draw from what the target has left at the first that is not.
 //
 // The accept tests touch two numbers a draft; the draw reads one row of the target, and the draft's
-// row beside it after a rejection.  A row is summed in slices by as many workgroups as it has
-// slices; a second kernel walks the slices' sums to the one that holds the draw's place and looks
-// only through that.  Masses and sums are 64-bit: p - q of two floats is then all but exact, and a
-// draw's place differs from another order of summation by some 2^-50 of the row's mass.
+// row beside it after a rejection.  Rows of up to kDirectClasses classes are one workgroup's, which
+// holds the masses in registers.  Longer ones are summed in segments of kSegment classes by as many waves as
+// there are, and in a second kernel a wave walks a sequence's sums to the segment that holds the
+// draw's place and looks only through that.  Masses and sums are 64-bit: p - q of two floats is
+// then all but exact, and a draw's place differs from another order of summation by some 2^-50 of the
+// row's mass.
 #include "rows.hpp"
 
 namespace lda {
 
 constexpr int32_t kMostSteps = 4096;
 constexpr int kVerifyBlock = 256;
-constexpr int32_t kSliceElements = 4096;
+constexpr int32_t kSegment = 1024;
+constexpr int kEach = kSegment / kWave;                       // neighbours a lane holds in a draw
+constexpr int32_t kDirectClasses = kVerifyBlock * kEach;
 
-struct SliceMass {
+struct Mass {
     double left, target;  // of max(0, p - q), of p
 };
 
@@ -32,8 +36,9 @@ struct VerifyArgs {
     int64_t accept_u_stride;
     const float* draw_u;
     int32_t tokens_type;
-    int32_t slices;
-    SliceMass* sums;  // [sequences][slices]
+    int32_t segments, each;  // of a row; of them, a wave's
+    Mass* sums;              // [sequences][segments]
+    int2* found;             // [sequences] accepted drafts, drafts there are
     int32_t* accepted;
     void* out;
     int64_t out_stride;
@@ -64,140 +69,263 @@ __device__ __forceinline__ int32_t count_accepted(const VerifyArgs& a, int64_t b
     return n;
 }
 
-// p, and max(0, p - q) with q where a draft was rejected; a NaN has no mass
-__device__ __forceinline__ double mass_of(double x) { return x > 0.0 ? x : 0.0; }
+__device__ __forceinline__ double mass_of(double x) { return x > 0.0 ? x : 0.0; }  // a NaN has none
 
-// sums[b][slice] of the masses of elements [slice * kSliceElements, ..)
+// The target's row of the draw, and the draft's row where one was rejected (else NULL)
 template <class T>
-__global__ __launch_bounds__(kVerifyBlock) void verify_sums_kernel(VerifyArgs a)
+struct DrawRows {
+    const T *p, *q;
+    __device__ __forceinline__ DrawRows(const VerifyArgs& a, int64_t b, int32_t k, int32_t n)
+    {
+        p = static_cast<const T*>(a.target) + b * a.target_sequence_stride + k * a.target_row_stride;
+        q = k < n ? static_cast<const T*>(a.draft) + b * a.draft_sequence_stride + k * a.draft_row_stride : nullptr;
+    }
+};
+
+// 16 bytes from anywhere (the hardware takes unaligned addresses), as floats
+template <class T>
+__device__ __forceinline__ void load_anywhere(const T* p, float (&x)[Row<T>::kChunk])
 {
-    __shared__ double part[kVerifyBlock / kWave];
-    for (int64_t b = blockIdx.x; b < a.sequences; b += gridDim.x) {
-        int32_t n;
-        const int32_t k = count_accepted<T>(a, b, n);
-        const T* p = static_cast<const T*>(a.target) + b * a.target_sequence_stride + k * a.target_row_stride;
-        const T* q = k < n ? static_cast<const T*>(a.draft) + b * a.draft_sequence_stride + k * a.draft_row_stride : nullptr;
-        for (int32_t slice = (int32_t)blockIdx.y; slice < a.slices; slice += (int32_t)gridDim.y) {
-            const int64_t v0 = (int64_t)slice * kSliceElements;
-            const int64_t v1 = min(v0 + kSliceElements, (int64_t)a.V);
-            double left = 0.0, target = 0.0;
-            for (int64_t v = v0 + threadIdx.x; v < v1; v += kVerifyBlock) {
-                const double pv = (double)Row<T>::one(p + v);
-                target += mass_of(pv);
-                if (q) left += mass_of(pv - (double)Row<T>::one(q + v));
-            }
-            target = block_sum<kVerifyBlock>(target, part);
-            left = q ? block_sum<kVerifyBlock>(left, part) : target;
-            if (threadIdx.x == 0) a.sums[b * a.slices + slice] = SliceMass{left, target};
+    uint4 r;
+    __builtin_memcpy(&r, p, 16);
+    Row<T>::unpack(r, x);
+}
+
+// elements v .. v + N - 1, 0 from V on
+template <class T, int N>
+__device__ __forceinline__ void load_run(const T* p, int64_t v, int32_t V, float (&x)[N])
+{
+    constexpr int E = Row<T>::kChunk;
+    if (v + N <= V) {
+#pragma unroll
+        for (int i = 0; i < N; i += E) {
+            float y[E];
+            load_anywhere(p + v + i, y);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[i + e] = y[e];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = v + i < V ? Row<T>::one(p + v + i) : 0.0f;
+    }
+}
+
+__device__ __forceinline__ double wave_prefix(double v)  // inclusive
+{
+    const int lane = threadIdx.x % kWave;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+        const double o = __shfl_up(v, d, kWave);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+
+// The draw among a thread's neighbours: the first of mass past the place, and the last of mass
+__device__ __forceinline__ void look_through(const double (&mass)[kEach], double run, double place, int32_t& hit, int32_t& last)
+{
+    hit = last = -1;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        run += mass[e];
+        if (mass[e] > 0.0) {
+            last = e;
+            if (hit < 0 && run > place) hit = e;
         }
     }
 }
 
-// One workgroup a sequence: the slice of the draw's place, the element in it, the outputs.
-template <class T>
-__global__ __launch_bounds__(kVerifyBlock) void verify_draw_kernel(VerifyArgs a)
+__device__ __forceinline__ void write_result(const VerifyArgs& a, int64_t b, int32_t k, int64_t token, int32_t tid, int32_t step)
 {
-    __shared__ double scan[kVerifyBlock / kWave];
-    __shared__ int64_t found[2];
+    if (tid == 0) a.accepted[b] = k;
+    for (int32_t i = tid; i <= a.steps; i += step) {
+        int64_t x = i == k ? token : -1;
+        if (i < k) x = index_at(a.tokens, a.tokens_type, b * a.tokens_stride + i);
+        if (a.tokens_type == LDA_I32) static_cast<int32_t*>(a.out)[b * a.out_stride + i] = (int32_t)x;
+        else static_cast<int64_t*>(a.out)[b * a.out_stride + i] = x;
+    }
+}
+
+// A workgroup a sequence, kEach neighbours of the row a thread
+template <class T>
+__global__ __launch_bounds__(kVerifyBlock) void verify_direct_kernel(VerifyArgs a)
+{
+    constexpr int kWaves = kVerifyBlock / kWave;
+    __shared__ Mass part[kWaves];
+    __shared__ int32_t place_of[2][kWaves];
     const int32_t tid = (int32_t)threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     for (int64_t b = blockIdx.x; b < a.sequences; b += gridDim.x) {
+        const double u = (double)a.draw_u[b];
         int32_t n;
         const int32_t k = count_accepted<T>(a, b, n);
-        const T* p = static_cast<const T*>(a.target) + b * a.target_sequence_stride + k * a.target_row_stride;
-        const T* q = k < n ? static_cast<const T*>(a.draft) + b * a.draft_sequence_stride + k * a.draft_row_stride : nullptr;
-        const SliceMass* sums = a.sums + b * a.slices;
-        // every wave walks the sums in the same order, 64 slices at a time
+        const DrawRows<T> rows(a, b, k, n);
+        const int64_t v = (int64_t)tid * kEach;
+        float p[kEach], q[kEach] = {};
+        load_run<T, kEach>(rows.p, v, a.V, p);
+        if (rows.q) load_run<T, kEach>(rows.q, v, a.V, q);
+        double mass[kEach], target = 0.0, left = 0.0;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            target += mass_of((double)p[e]);
+            mass[e] = mass_of((double)p[e] - (double)q[e]);
+            left += mass[e];
+        }
+        double upto = wave_prefix(left);
+        const double all_target = wave_sum(target);
+        __syncthreads();
+        if (lane == kWave - 1) part[wave] = Mass{upto, all_target};
+        __syncthreads();
+        double before = 0.0, total = 0.0;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) before += part[w].left;
+            total += part[w].left;
+        }
+        if (!(total > 0.0)) {  // nothing left: from the target
+#pragma unroll
+            for (int e = 0; e < kEach; ++e) mass[e] = mass_of((double)p[e]);
+            left = target;
+            upto = wave_prefix(target);
+            before = total = 0.0;
+            for (int w = 0; w < kWaves; ++w) {
+                if (w < wave) before += part[w].target;
+                total += part[w].target;
+            }
+        }
+        int32_t hit, last;
+        look_through(mass, before + (upto - left), u * total, hit, last);
+        const uint64_t hits = __ballot(hit >= 0), lasts = __ballot(last >= 0);
+        const int32_t at_hit = hits ? (int32_t)__builtin_ctzll(hits) : 0;
+        const int32_t at_last = lasts ? 63 - (int32_t)__builtin_clzll(lasts) : 0;
+        hit = __shfl(hit, at_hit, kWave);
+        last = __shfl(last, at_last, kWave);
+        if (lane == 0) {
+            place_of[0][wave] = hits ? (wave * kWave + at_hit) * kEach + hit : -1;
+            place_of[1][wave] = lasts ? (wave * kWave + at_last) * kEach + last : -1;
+        }
+        __syncthreads();
+        int64_t token = -1;
+        for (int w = kWaves - 1; w >= 0; --w)
+            if (place_of[0][w] >= 0) token = place_of[0][w];
+        for (int w = kWaves - 1; w >= 0 && token < 0; --w) token = place_of[1][w];
+        write_result(a, b, k, token, tid, kVerifyBlock);
+    }
+}
+
+// sums[b][segment] of the masses; blockIdx.y walks the segments, each wave of it `each` of them
+template <class T>
+__global__ __launch_bounds__(kVerifyBlock) void verify_sums_kernel(VerifyArgs a)
+{
+    constexpr int E = Row<T>::kChunk, kLoads = kSegment / kWave / E;
+    const int32_t lane = (int32_t)threadIdx.x % kWave;
+    const int32_t s0 = (int32_t)(blockIdx.y * (kVerifyBlock / kWave) + threadIdx.x / kWave) * a.each;
+    const int32_t s1 = min(a.segments, s0 + a.each);
+    for (int64_t b = blockIdx.x; b < a.sequences; b += gridDim.x) {
+        if (s0 >= s1) break;
+        int32_t n;
+        const int32_t k = count_accepted<T>(a, b, n);
+        if (s0 == 0 && lane == 0) a.found[b] = make_int2(k, n);
+        const DrawRows<T> rows(a, b, k, n);
+        for (int32_t s = s0; s < s1; ++s) {
+            double left = 0.0, target = 0.0;
+            float p[kLoads][E], q[kLoads][E] = {};
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j)
+                load_run<T, E>(rows.p, (int64_t)s * kSegment + (j * kWave + lane) * E, a.V, p[j]);
+            if (rows.q) {
+#pragma unroll
+                for (int j = 0; j < kLoads; ++j)
+                    load_run<T, E>(rows.q, (int64_t)s * kSegment + (j * kWave + lane) * E, a.V, q[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    target += mass_of((double)p[j][e]);
+                    left += mass_of((double)p[j][e] - (double)q[j][e]);
+                }
+            target = wave_sum(target);
+            left = wave_sum(left);
+            if (lane == 0) a.sums[b * a.segments + s] = Mass{left, target};
+        }
+    }
+}
+
+// A wave a sequence: the segment of the draw's place, the element in it, the outputs.
+template <class T>
+__global__ __launch_bounds__(kWave) void verify_draw_kernel(VerifyArgs a)
+{
+    const int32_t lane = (int32_t)threadIdx.x;
+    for (int64_t b = blockIdx.x; b < a.sequences; b += gridDim.x) {
+        const int2 found = a.found[b];
+        const double u = (double)a.draw_u[b];
+        const Mass* sums = a.sums + b * a.segments;
         double left = 0.0, target = 0.0;
-        for (int32_t s = lane; s < a.slices; s += kWave) {
+        for (int32_t s = lane; s < a.segments; s += kWave) {
             left += sums[s].left;
             target += sums[s].target;
         }
         left = wave_sum(left);
         target = wave_sum(target);
-        if (!(left > 0.0)) q = nullptr;
-        const bool whole = q == nullptr;
-        const double total = whole ? target : left;
-        const double place = (double)a.draw_u[b] * total;
+        DrawRows<T> rows(a, b, found.x, found.y);
+        const bool whole = !(left > 0.0);
+        if (whole) rows.q = nullptr;
+        const double place = u * (whole ? target : left);
+        // 64 sums at a time, in order
         double before = 0.0;
-        int32_t slice = -1, last = -1;
-        for (int32_t s0 = 0; s0 < a.slices && slice < 0; s0 += kWave) {
+        int32_t segment = -1, last = -1;
+        for (int32_t s0 = 0; s0 < a.segments && segment < 0; s0 += kWave) {
             const int32_t s = s0 + lane;
-            const double own = s < a.slices ? (whole ? sums[s].target : sums[s].left) : 0.0;
-            double sum = own;
-#pragma unroll
-            for (int d = 1; d < kWave; d <<= 1) {
-                const double o = __shfl_up(sum, d, kWave);
-                if (lane >= d) sum += o;
-            }
+            const double own = s < a.segments ? (whole ? sums[s].target : sums[s].left) : 0.0;
+            const double sum = wave_prefix(own);
             const uint64_t some = __ballot(own > 0.0);
             const uint64_t past = __ballot(own > 0.0 && before + sum > place);
             if (some) last = s0 + 63 - (int32_t)__builtin_clzll(some);
             if (past) {
                 const int at = __builtin_ctzll(past);
-                slice = s0 + at;
-                before += __shfl(sum, at, kWave) - __shfl(own, at, kWave);
+                segment = s0 + at;
+                before += __shfl(sum - own, at, kWave);
             } else {
                 before += __shfl(sum, kWave - 1, kWave);
             }
         }
-        const bool inside = slice >= 0;
-        if (!inside) slice = last;  // the last element of any mass
+        const bool inside = segment >= 0;
+        if (!inside) segment = last;  // the last element of any mass
         int64_t token = -1;
-        if (slice >= 0) {
-            const int64_t v0 = (int64_t)slice * kSliceElements;
-            const int64_t v1 = min(v0 + kSliceElements, (int64_t)a.V);
-            constexpr int kEach = kSliceElements / kVerifyBlock;
-            // a thread holds kEach neighbours
+        if (segment >= 0) {
+            const int64_t v = (int64_t)segment * kSegment + lane * kEach;
+            float p[kEach], q[kEach] = {};
+            load_run<T, kEach>(rows.p, v, a.V, p);
+            if (rows.q) load_run<T, kEach>(rows.q, v, a.V, q);
             double mass[kEach], sum = 0.0;
-            const int64_t v = v0 + (int64_t)tid * kEach;
 #pragma unroll
             for (int e = 0; e < kEach; ++e) {
-                mass[e] = 0.0;
-                if (v + e < v1) {
-                    const double pv = (double)Row<T>::one(p + v + e);
-                    mass[e] = mass_of(whole ? pv : pv - (double)Row<T>::one(q + v + e));
-                }
+                mass[e] = mass_of((double)p[e] - (double)q[e]);
                 sum += mass[e];
             }
-            double upto = sum;
-#pragma unroll
-            for (int d = 1; d < kWave; d <<= 1) {
-                const double o = __shfl_up(upto, d, kWave);
-                if (lane >= d) upto += o;
+            const double upto = wave_prefix(sum);
+            int32_t hit, most;
+            look_through(mass, before + (upto - sum), place, hit, most);
+            const uint64_t hits = __ballot(inside && hit >= 0), some = __ballot(most >= 0);
+            if (hits) {
+                const int at = __builtin_ctzll(hits);
+                token = (int64_t)segment * kSegment + at * kEach + __shfl(hit, at, kWave);
+            } else if (some) {
+                const int at = 63 - (int)__builtin_clzll(some);
+                token = (int64_t)segment * kSegment + at * kEach + __shfl(most, at, kWave);
             }
-            __syncthreads();
-            if (lane == kWave - 1) scan[wave] = upto;
-            if (tid < 2) found[tid] = tid == 0 ? INT64_MAX : -1;
-            __syncthreads();
-            double run = before + (upto - sum);
-            for (int w = 0; w < wave; ++w) run += scan[w];
-            int64_t hit = INT64_MAX, most = -1;
-#pragma unroll
-            for (int e = 0; e < kEach; ++e) {
-                run += mass[e];
-                if (mass[e] > 0.0) {
-                    most = v + e;
-                    if (inside && run > place && hit == INT64_MAX) hit = v + e;
-                }
-            }
-            if (hit != INT64_MAX) atomicMin((long long*)&found[0], (long long)hit);
-            if (most >= 0) atomicMax((long long*)&found[1], (long long)most);
-            __syncthreads();
-            token = found[0] != INT64_MAX ? found[0] : found[1];
         }
-        if (tid == 0) a.accepted[b] = k;
-        for (int32_t i = tid; i <= a.steps; i += kVerifyBlock) {
-            int64_t x = i == k ? token : -1;
-            if (i < k) x = index_at(a.tokens, a.tokens_type, b * a.tokens_stride + i);
-            if (a.tokens_type == LDA_I32) static_cast<int32_t*>(a.out)[b * a.out_stride + i] = (int32_t)x;
-            else static_cast<int64_t*>(a.out)[b * a.out_stride + i] = x;
-        }
+        write_result(a, b, found.x, token, lane, kWave);
     }
 }
 
-static int64_t verify_slices(const lda_draft_rows* d)
+static int64_t verify_segments(const lda_draft_rows* d)
 {
-    return ((int64_t)d->classes + kSliceElements - 1) / kSliceElements;
+    return d->classes <= kDirectClasses ? 0 : ((int64_t)d->classes + kSegment - 1) / kSegment;
+}
+static int64_t verify_bytes(const lda_draft_rows* d)
+{
+    const int64_t segments = verify_segments(d);
+    return segments == 0 ? 0 : d->sequences * (segments * (int64_t)sizeof(Mass) + (int64_t)sizeof(int2));
 }
 
 static int check_verify(const lda_draft_rows* d, const char* call)
@@ -222,12 +350,23 @@ static int check_verify(const lda_draft_rows* d, const char* call)
 }
 
 template <class T>
-static void launch_verify_typed(const VerifyArgs& a, hipStream_t stream)
+static void launch_verify_typed(VerifyArgs& a, hipStream_t stream)
 {
     const unsigned gx = (unsigned)(a.sequences < (1 << 20) ? a.sequences : (1 << 20));
-    const unsigned gy = (unsigned)(a.slices < 4096 ? a.slices : 4096);
+    if (a.segments == 0) {
+        verify_direct_kernel<T><<<gx, kVerifyBlock, 0, stream>>>(a);
+        return;
+    }
+    // some 8 workgroups a CU, as every wave begins with the accept tests
+    constexpr int64_t kWaves = kVerifyBlock / kWave, kMost = 256 * 8;
+    int64_t each = a.sequences * a.segments / (kMost * kWaves);
+    const int64_t least = (a.segments + 65535 * kWaves - 1) / (65535 * kWaves);
+    if (each < least) each = least;
+    if (each < 1) each = 1;
+    a.each = (int32_t)(each < a.segments ? each : a.segments);
+    const unsigned gy = (unsigned)((a.segments + kWaves * a.each - 1) / (kWaves * a.each));
     verify_sums_kernel<T><<<dim3(gx, gy), kVerifyBlock, 0, stream>>>(a);
-    verify_draw_kernel<T><<<gx, kVerifyBlock, 0, stream>>>(a);
+    verify_draw_kernel<T><<<gx, kWave, 0, stream>>>(a);
 }
 
 }  // namespace lda
@@ -240,7 +379,7 @@ int64_t lda_verify_workspace(const lda_draft_rows* d)
 try {
     const int rc = check_verify(d, "lda_verify_workspace");
     if (rc != LDA_OK) return rc;
-    return d->sequences * verify_slices(d) * (int64_t)sizeof(SliceMass);
+    return verify_bytes(d);
 } catch (...) {
     return LDA_ERR_OOM;
 }
@@ -273,11 +412,12 @@ try {
     a.accept_u_stride = d->accept_u_stride;
     a.draw_u = d->draw_u;
     a.tokens_type = d->tokens_type;
-    a.slices = (int32_t)verify_slices(d);
-    const int64_t need = a.sequences * a.slices * (int64_t)sizeof(SliceMass);
-    if (!d->workspace || d->workspace_bytes < need || !aligned_to(d->workspace, 16))
+    a.segments = (int32_t)verify_segments(d);
+    const int64_t need = verify_bytes(d);
+    if (need > 0 && (!d->workspace || d->workspace_bytes < need || !aligned_to(d->workspace, 16)))
         return fail(nullptr, LDA_ERR_ARG, "%s: needs a workspace of %lld bytes, aligned to 16", call, (long long)need);
-    a.sums = static_cast<SliceMass*>(d->workspace);
+    a.sums = static_cast<Mass*>(d->workspace);
+    a.found = reinterpret_cast<int2*>(a.sums + a.sequences * a.segments);
     a.accepted = accepted;
     a.out = out;
     a.out_stride = out_stride;

@@ -84,7 +84,7 @@ def test_no_rows_are_no_work(lib):
 
 def draft(**kw):
     r = lda.lda_draft_rows()
-    r.sequences, r.steps, r.classes = 2, 3, 1000
+    r.sequences, r.steps, r.classes = 2, 3, 100_000
     for name in ("target", "draft", "tokens", "accept_u", "draw_u", "workspace"):
         setattr(r, name, 1 << 20)
     r.workspace_bytes = 1 << 20
