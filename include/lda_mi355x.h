@@ -314,8 +314,8 @@ typedef struct lda_distill_rows {
 
 /* Bytes of workspace that a call on these rows needs (may be 0), or a negative LDA_ERR_*. */
 int64_t lda_distill_workspace(const lda_distill_rows* rows);
-/* loss [rows]; stats [rows][2] for lda_distill_grad (the row's largest logit and the sum of
- * exp((S - largest) / T)), or NULL.  Both 32-bit floats. */
+/* loss [rows]; stats, aligned to 16 bytes: 8 floats a row for lda_distill_grad (the row's softmax
+ * and teacher in short), or NULL. */
 int lda_distill_loss(const lda_distill_rows* rows, float* loss, float* stats);
 /* The gradient of sum_i weight_i loss_i, [rows][classes] in the logits' type, rows grad_stride
  * apart; what lies between rows is left as it was.  stats: of lda_distill_loss on the same rows. */

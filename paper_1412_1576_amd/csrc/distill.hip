@@ -1,27 +1,50 @@
 // Distillation from a teacher's top logits: the loss of every row and its gradient (the formulas
 // stand at lda_distill_rows in lda_mi355x.h).
 //
-// A row's softmax needs its largest logit m and s = sum exp((S - m) / T), both found in one pass with
-// the running form: a thread keeps (m, s) of what it has seen and scales s when m grows, the pairs
-// of threads, waves and slices join the same way.  The teacher's masses touch only k of the V
-// classes, so they are evaluated apart: the loss gathers k logits, the gradient is
-// written as if the teacher had its floor r everywhere and the k places are overwritten.
+// A row's softmax needs a base m near its largest logit and s = sum exp((S - m) / T), both found in
+// one pass: a thread keeps (m, s) of what it has seen and scales s only when a logit lies far above m; the
+// pairs of threads, waves and slices join.  The teacher touches k of the V classes: the loss
+// gathers k logits, the gradient is written as if the teacher had its floor everywhere and
+// the k places are written again.
+//
+// Rows that fit a workgroup's registers are read from memory once, loss and gradient both
+// (distill_rows_kernel).  Longer rows, and long ones where there are too few to fill the GPU, are cut
+// into slices: distill_part_kernel, then distill_join_kernel, which reads them a second time for the gradient.
 #include "rows.hpp"
 
 namespace lda {
 
 constexpr int32_t kMostSlots = 1024;
+constexpr int kPartBlock = 256;
+constexpr int kSliceLoads = 8;                                // 16-byte loads of a thread in flight
+constexpr int32_t kSliceChunks = kPartBlock * kSliceLoads;    // 32 KB
+constexpr int32_t kStatFloats = 8;
+constexpr float kFar = 16.0f;  // a base is left where it is until a logit exceeds it by this, in powers of 2
 
-// What a slice of a row tells about its softmax.  ssum and ninf (finite logits summed, logits of
-// -infinity counted) are only there where the teacher has a floor.
+// What a slice of a row tells about its softmax.  scaled_sum (of c S over the finite logits) and
+// ninf (the logits of -infinity) are only there where the teacher has a floor.
 struct RowPart {
     float m, s;
-    double ssum;
+    double scaled_sum;
     int32_t ninf, pad;
 };
 
+// What the slots say: masses are exp(t / T - z), their sum, sum p log p; the floor of the other
+// classes and their number.
+struct TeacherPart {
+    double mass, entropy, z, floor;
+    int32_t others, pad[3];
+};
+
+// A row's softmax and teacher, all that its gradient needs
+struct RowStats {
+    float m, s, mass, floor;
+    double z;
+};
+static_assert(sizeof(RowStats) <= kStatFloats * sizeof(float), "stats");
+
 struct DistillArgs {
-    int64_t rows;
+    int64_t rows, row0;     // a launch's rows begin with row0
     int32_t V, k;
     const void* logits;
     int64_t logits_stride;
@@ -34,22 +57,23 @@ struct DistillArgs {
     int64_t weight_stride;
     int32_t ids_type, teacher_type;
     float T, c;             // c = log2(e) / T
-    int32_t slices;         // of a row, slice_chunks chunks of 16 bytes each
-    int32_t slice_chunks;
-    RowPart* parts;         // [rows][slices]; NULL: a row is one slice
-    const float* stats_in;  // [rows][2]: the softmax is known
+    int32_t slices;         // of kSliceChunks chunks each
+    RowPart* parts;         // [rows][slices]
+    TeacherPart* teachers;  // [rows]
+    const float* stats_in;  // [rows][kStatFloats]
     float* loss;
     float* stats;
     void* grad;
     int64_t grad_stride;
 };
 
-// exp((x - m) / T) with exp2 in hardware; m finite or the row's own infinity or NaN
-__device__ __forceinline__ float exp_above(float x, float m, float c)
-{
-    return __builtin_amdgcn_exp2f((x - m) * c);
-}
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
+// exp((x - base) / T), exp2 in hardware.  The difference comes first: masks of the type's lowest value
+// times c would overflow, and a row of nothing else has to come out even.
+__device__ __forceinline__ float exp_above(float x, float base, float c)
+{
+    return __builtin_amdgcn_exp2f((x - base) * c);
+}
 
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2, float c)
 {
@@ -57,295 +81,541 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2, flo
     s = s * exp_above(m, base, c) + s2 * exp_above(m2, base, c);
     m = top;
 }
-
-template <int BLOCK>
-__device__ __forceinline__ void block_join(float& m, float& s, float c, float2* part)
+__device__ __forceinline__ void wave_join(float& m, float& s, float c)
 {
 #pragma unroll
     for (int d = kWave / 2; d > 0; d >>= 1) {
         const float m2 = __shfl_xor(m, d, kWave), s2 = __shfl_xor(s, d, kWave);
         join(m, s, m2, s2, c);
     }
+}
+template <int BLOCK>
+__device__ __forceinline__ void block_join(float& m, float& s, float c, float2* part)
+{
+    wave_join(m, s, c);
     if (BLOCK == kWave) return;
     __syncthreads();
     if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = make_float2(m, s);
     __syncthreads();
     m = part[0].x;
     s = part[0].y;
-#pragma unroll
+#pragma unroll 1
     for (int w = 1; w < BLOCK / kWave; ++w) join(m, s, part[w].x, part[w].y, c);
 }
 
-// The teacher's slots in LDS.  A slot without a mass has id -1.
-struct TeacherSlots {
-    int32_t* id;   // [k]
-    float* p;      // [k] mass of the slot
-    float* all;    // [k] mass of the slot's class (all its slots)
-    float* logit;  // [k] the student's logit there
-    double* head;  // sum of p, sum of p log p
-    __device__ __forceinline__ TeacherSlots(unsigned char* lds, int32_t k)
+// A row as the whole 16-byte chunks of memory inside it, and the elements before and behind
+// those (fewer than two chunks), which a thread each takes.
+template <class T>
+struct SplitRow {
+    static constexpr int E = Row<T>::kChunk;
+    const T* p;
+    int32_t head, whole, extras;  // elements, chunks, elements
+
+    __device__ __forceinline__ SplitRow(const T* row, int32_t V) : p(row)
     {
-        head = reinterpret_cast<double*>(lds);
-        id = reinterpret_cast<int32_t*>(lds + 16);
-        p = reinterpret_cast<float*>(id + k);
-        all = p + k;
-        logit = all + k;
+        const int32_t lead = (int32_t)(((uintptr_t)row & 15u) / sizeof(T));
+        head = min((E - lead) % E, V);
+        whole = (V - head) / E;
+        extras = V - whole * E;
+    }
+    __device__ __forceinline__ int32_t chunk(int32_t i) const { return head + i * E; }
+    __device__ __forceinline__ int32_t extra(int32_t i) const { return i < head ? i : i + whole * E; }
+    __device__ __forceinline__ uint4 load(int32_t i) const { return *reinterpret_cast<const uint4*>(p + chunk(i)); }
+};
+
+// The running form of one thread's share
+template <class T, bool REST>
+struct Running {
+    static constexpr int E = Row<T>::kChunk;
+    float m = -INFINITY, s = 0.0f;
+    double scaled_sum = 0.0;
+    int32_t ninf = 0;
+
+    template <int N>
+    __device__ __forceinline__ void add(const float (&x)[N], float c)
+    {
+        float top = x[0];
+#pragma unroll
+        for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
+        if ((top - m) * c > kFar) {
+            s *= exp_above(m, top, c);
+            m = top;
+        }
+        const float base = base_of(m);
+        float y[N], sum = 0.0f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            y[e] = (x[e] - base) * c;
+            sum += __builtin_amdgcn_exp2f(y[e]);
+        }
+        s += sum;
+        if (REST) {
+            float least = y[0], ysum = y[0];
+#pragma unroll
+            for (int e = 1; e < N; ++e) {
+                least = fminf(least, y[e]);
+                ysum += y[e];
+            }
+            if (least > -INFINITY) {
+                scaled_sum += (double)ysum + (double)N * ((double)base * (double)c);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    if (x[e] == -INFINITY) ++ninf;
+                    else scaled_sum += (double)x[e] * (double)c;
+                }
+            }
+        }
     }
 };
-inline size_t slots_lds(int32_t k) { return 16 + 16 * (size_t)k; }
 
-// One wave's work: ids, masses, their sum and their entropy.
-__device__ void read_teacher(const DistillArgs& a, int64_t row, const TeacherSlots& ts)
+// ids [k] and masses [k] of a row in LDS; head: TeacherPart of the row
+struct Slots {
+    TeacherPart* head;
+    int32_t* id;  // -1: empty
+    float* p;     // the slot's mass, then the mass of its class (all its slots)
+    float* x;     // the student's logit
+    __device__ __forceinline__ Slots(unsigned char* lds, int32_t k)
+    {
+        head = reinterpret_cast<TeacherPart*>(lds);
+        id = reinterpret_cast<int32_t*>(lds + sizeof(TeacherPart));
+        p = reinterpret_cast<float*>(id + (k + 3) / 4 * 4);
+        x = p + (k + 3) / 4 * 4;
+    }
+};
+inline size_t slots_lds(int32_t k) { return sizeof(TeacherPart) + 12 * ((size_t)(k + 3) / 4 * 4); }
+
+__device__ __forceinline__ int32_t slot_id(const DistillArgs& a, int64_t row, int32_t j)
+{
+    const int64_t id = index_at(a.ids, a.ids_type, row * a.ids_stride + j);
+    return id >= 0 && id < a.V ? (int32_t)id : -1;
+}
+
+// One wave's work: ids, masses, their sum and entropy.
+__device__ __forceinline__ void read_teacher(const DistillArgs& a, int64_t row, const Slots& slots)
 {
     const int lane = threadIdx.x % kWave;
-    const int64_t ids0 = row * a.ids_stride, t0 = row * a.teacher_stride;
     const double inv_t = 1.0 / (double)a.T;
     float top = -INFINITY;
-    for (int32_t j = lane; j < a.k; j += kWave) {
-        const int64_t id = index_at(a.ids, a.ids_type, ids0 + j);
-        const bool full = id >= 0 && id < a.V;
-        const float t = full ? element_at(a.teacher, a.teacher_type, t0 + j) : -INFINITY;
-        ts.id[j] = full ? (int32_t)id : -1;
-        ts.p[j] = t;
+    for (int32_t j = lane; j < (a.k + 3) / 4 * 4; j += kWave) {
+        const int32_t id = j < a.k ? slot_id(a, row, j) : -1;
+        const float t = id >= 0 ? element_at(a.teacher, a.teacher_type, row * a.teacher_stride + j) : -INFINITY;
+        slots.id[j] = id;
+        slots.p[j] = t;
         top = fmaxf(top, t);
     }
-    top = wave_reduce(top, [](float x, float y) { return fmaxf(x, y); });
-    double shift, log_sum = 0.0;
+    double z;
     if (a.log_norm) {
-        shift = (double)a.log_norm[row];
+        z = (double)a.log_norm[row];
     } else {
-        shift = (double)base_of(top) * inv_t;
+        top = wave_reduce(top, [](float x, float y) { return fmaxf(x, y); });
+        z = (double)base_of(top) * inv_t;
         double sum = 0.0;
-        for (int32_t j = lane; j < a.k; j += kWave) sum += exp((double)ts.p[j] * inv_t - shift);
+        for (int32_t j = lane; j < a.k; j += kWave) sum += exp((double)slots.p[j] * inv_t - z);
         sum = wave_sum(sum);
-        log_sum = sum == 0.0 ? 0.0 : log(sum);
+        z += sum == 0.0 ? 0.0 : log(sum);
     }
     double mass = 0.0, entropy = 0.0;
     for (int32_t j = lane; j < a.k; j += kWave) {
-        const double log_p = (double)ts.p[j] * inv_t - shift - log_sum;
-        const double p = exp(log_p);
-        ts.p[j] = (float)p;
+        const double log_p = (double)slots.p[j] * inv_t - z, p = exp(log_p);
+        slots.p[j] = (float)p;
         mass += p;
         if (p != 0.0) entropy += p * log_p;
     }
     mass = wave_sum(mass);
     entropy = wave_sum(entropy);
     if (lane == 0) {
-        ts.head[0] = mass;
-        ts.head[1] = entropy;
+        slots.head->mass = mass;
+        slots.head->entropy = entropy;
+        slots.head->z = z;
     }
 }
 
-// (m, s) and the floor's sums of chunks [c0, c1) of a row
-template <class T, bool REST, int BLOCK>
-__device__ __forceinline__ void scan_chunks(const ChunkedRow<T>& r, int32_t c0, int32_t c1, float c, float& m,
-                                            float& s, double& ssum, int32_t& ninf)
+// Is slot j the first of its class, and what is the mass of all of them?  Read from LDS by
+// the whole workgroup in step, four at a time.
+__device__ __forceinline__ bool first_of_class(const Slots& slots, int32_t k, int32_t j, int32_t id, float& all)
 {
-    constexpr int E = Row<T>::kChunk;
-    m = -INFINITY;
-    s = 0.0f;
-    ssum = 0.0;
-    ninf = 0;
-    for (int32_t i = c0 + (int32_t)threadIdx.x; i < c1; i += BLOCK) {
-        float x[E];
-        r.load(i, x, -INFINITY);
-        float top = x[0];
+    all = 0.0f;
+    bool first = true;
+    for (int32_t i = 0; i < k; i += 4) {
+        const int4 other = *reinterpret_cast<const int4*>(slots.id + i);
+        const float4 p = *reinterpret_cast<const float4*>(slots.p + i);
+        const int32_t o[4] = {other.x, other.y, other.z, other.w};
+        const float q[4] = {p.x, p.y, p.z, p.w};
 #pragma unroll
-        for (int e = 1; e < E; ++e) top = fmaxf(top, x[e]);
-        if (top > m) {
-            s *= exp_above(m, top, c);
-            m = top;
-        }
-        const float base = base_of(m);
-        float sum = 0.0f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) sum += exp_above(x[e], base, c);
-        s += sum;
-        if (REST) {
-            const int64_t v = r.first(i);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const bool none = x[e] == -INFINITY;
-                ssum += none ? 0.0 : (double)x[e];
-                ninf += none && v + e >= 0 && v + e < r.V;
-            }
+        for (int e = 0; e < 4; ++e) {
+            const bool same = o[e] == id;
+            all += same ? q[e] : 0.0f;
+            first = first && !(same && i + e < j);
         }
     }
+    return first;
 }
 
-// One workgroup a row or a slice of it.  FORM: kPart writes the slice's RowPart; kWhole has the
-// row's softmax itself, kJoin takes it from the parts or from stats_in; both then do what of
-// loss, stats and gradient is asked for.
-enum DistillForm { kPart, kWhole, kJoin };
+__device__ __forceinline__ double floor_of(double mass, int32_t others)
+{
+    const double left = 1.0 - mass;
+    return others > 0 && left > 0.0 ? left / (double)others : 0.0;
+}
 
-template <class T, bool REST, int BLOCK, int FORM>
-__global__ __launch_bounds__(BLOCK) void distill_kernel(DistillArgs a)
+// The factors of a row's gradient: w T (M q - floor), and in the slots' places w T (M q - P)
+struct Gradient {
+    float base, c, scale, low, wt;
+    __device__ __forceinline__ Gradient(float m, float s, float mass, float floor, float w, float T, float c)
+        : base(base_of(m)), c(c)
+    {
+        wt = w * T;
+        scale = s == 0.0f ? 0.0f : mass * wt / s;
+        low = floor * wt;
+    }
+    __device__ __forceinline__ float dense(float x) const { return exp_above(x, base, c) * scale - low; }
+    __device__ __forceinline__ float slot(float x, float p) const { return exp_above(x, base, c) * scale - p * wt; }
+};
+
+template <class T>
+__device__ __forceinline__ void store_chunk(T* g, const float (&x)[Row<T>::kChunk])
+{
+    const uint4 r = Row<T>::pack(x);
+    __builtin_memcpy(g, &r, 16);  // from any element on: the hardware takes unaligned addresses
+}
+
+// The loss from its sums over the slots, by one thread
+struct LossSums {
+    double cross = 0.0, named_sum = 0.0;  // sum p log q; c S over the finite logits of named classes
+    int32_t named = 0, named_inf = 0, infinite = 0;
+};
+
+__device__ __forceinline__ void add_slot(LossSums& l, double p, float x, double base, double inv_t, double log_s)
+{
+    if (p == 0.0) return;
+    if (x == -INFINITY) l.infinite = 1;
+    else l.cross += p * (((double)x - base) * inv_t - log_s);
+}
+
+template <bool REST>
+__device__ __forceinline__ float loss_of(const DistillArgs& a, const LossSums& l, const TeacherPart& t, float m, float s,
+                                         double scaled_sum, int32_t ninf)
+{
+    const double T = (double)a.T, log_s = log((double)s), base = (double)base_of(m);
+    double rest = 0.0;
+    bool infinite = l.infinite != 0;
+    if (REST && t.floor > 0.0) {
+        const double beside = (scaled_sum - l.named_sum) / ((double)a.c * T) - (double)t.others * base / T;
+        rest = t.floor * ((double)t.others * (log(t.floor) + log_s) - beside);
+        infinite = infinite || ninf > l.named_inf;
+    }
+    double loss = infinite ? (double)INFINITY : T * T * (t.entropy - l.cross + rest);
+    if (!(s == s) || !(t.mass == t.mass)) loss = (double)NAN;
+    if (t.mass + t.floor * (double)t.others == 0.0) loss = 0.0;
+    return (float)loss;
+}
+
+// A row a workgroup, CHUNKS chunks of it in each thread's registers.
+template <class T, bool REST, int BLOCK, int CHUNKS>
+__global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
 {
     constexpr int E = Row<T>::kChunk;
     extern __shared__ __align__(16) unsigned char lds[];
     __shared__ float2 part2[BLOCK / kWave];
     __shared__ double partd[BLOCK / kWave];
     __shared__ int32_t parti[BLOCK / kWave];
-    const TeacherSlots ts(lds, a.k);
-    const int32_t tid = (int32_t)threadIdx.x, slice = (int32_t)blockIdx.y;
-    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        const ChunkedRow<T> r(static_cast<const T*>(a.logits) + row * a.logits_stride, a.V);
-        const float w = a.weight ? a.weight[row * a.weight_stride] : 1.0f;
-        const int32_t c0 = slice * a.slice_chunks;
-        const int32_t c1 = (int32_t)min((int64_t)r.chunks(), (int64_t)c0 + a.slice_chunks);
-        bool out = a.grad && w == 0.0f;  // left out
-        float m = -INFINITY, s = 0.0f;
-        double ssum = 0.0;
-        int32_t ninf = 0;
-        if (FORM != kPart) {
-            if (tid < kWave) read_teacher(a, row, ts);
+    const Slots slots(lds, a.k);
+    const int32_t tid = (int32_t)threadIdx.x;
+    const int64_t row = a.row0 + blockIdx.x;
+    const SplitRow<T> r(static_cast<const T*>(a.logits) + row * a.logits_stride, a.V);
+    T* const g = static_cast<T*>(a.grad) + row * a.grad_stride;
+    const float w = a.weight ? a.weight[row * a.weight_stride] : 1.0f;
+    bool out = a.grad && w == 0.0f;  // left out
+    float m = -INFINITY, s = 0.0f;
+    double scaled_sum = 0.0;
+    int32_t ninf = 0;
+    uint4 raw[CHUNKS];
+    float extra[1] = {-INFINITY};
+    if (!out) {
+        if (tid < kWave) read_teacher(a, row, slots);
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            const int32_t i = j * BLOCK + tid;
+            if (i < r.whole) raw[j] = r.load(i);
         }
-        if (FORM != kJoin && !out) {
-            scan_chunks<T, REST, BLOCK>(r, c0, c1, a.c, m, s, ssum, ninf);
-            block_join<BLOCK>(m, s, a.c, part2);
-            if (REST) {
-                ssum = block_sum<BLOCK>(ssum, partd);
-                ninf = block_sum<BLOCK>(ninf, parti);
-            }
-        }
-        if (FORM == kPart) {
-            if (tid == 0 && !out) a.parts[row * a.slices + slice] = RowPart{m, s, ssum, ninf, 0};
-            continue;
-        }
-        if (FORM == kJoin && !out) {
-            if (a.stats_in) {
-                m = a.stats_in[2 * row];
-                s = a.stats_in[2 * row + 1];
-            } else {
-                m = -INFINITY;
-                s = 0.0f;
-                for (int32_t q = 0; q < a.slices; ++q) {  // every thread the same: few, and in cache
-                    const RowPart part = a.parts[row * a.slices + q];
-                    join(m, s, part.m, part.s, a.c);
-                    ssum += part.ssum;
-                    ninf += part.ninf;
-                }
-            }
-        }
-        __syncthreads();
-        const double mass = ts.head[0], entropy = ts.head[1];
-        // the slots: the class's whole mass, the student's logit, and the loss's sums
-        const bool first_slice = slice == 0;
-        const bool want_loss = a.loss && first_slice;
-        const double inv_t = 1.0 / (double)a.T;
-        const double base = (double)base_of(m), log_s = log((double)s);
-        double cross = 0.0, named_sum = 0.0;
-        int32_t named = 0, named_inf = 0;
-        bool infinite = false;
-        if (!out) {
-            for (int32_t j = tid; j < a.k; j += BLOCK) {
-                const int32_t id = ts.id[j];
-                if (id < 0) continue;
-                const float x = Row<T>::one(r.p + id);
-                ts.logit[j] = x;
-                if (REST || a.grad) {
-                    float all = 0.0f;
-                    bool first = true;
-                    for (int32_t i = 0; i < a.k; ++i) {
-                        if (ts.id[i] != id) continue;
-                        all += ts.p[i];
-                        first = first && i >= j;
-                    }
-                    ts.all[j] = all;
-                    if (REST && first) {
-                        ++named;
-                        if (x == -INFINITY) ++named_inf;
-                        else named_sum += (double)x;
-                    }
-                }
-                const double p = (double)ts.p[j];
-                if (p != 0.0) {
-                    if (x == -INFINITY) infinite = true;
-                    else cross += p * (((double)x - base) * inv_t - log_s);
-                }
-            }
-        }
-        double floor_mass = 0.0;
-        int32_t others = 0;
-        if (REST) {
-            named = block_sum<BLOCK>(named, parti);
-            others = a.V - named;
-            const double left = 1.0 - mass;
-            floor_mass = others > 0 && left > 0.0 ? left / (double)others : 0.0;
-        }
-        const double all_mass = mass + floor_mass * (double)others;
-        if (want_loss) {
-            cross = block_sum<BLOCK>(cross, partd);
-            infinite = block_sum<BLOCK>((int32_t)infinite, parti) != 0;
-            double rest = 0.0;
-            if (REST) {
-                named_sum = block_sum<BLOCK>(named_sum, partd);
-                named_inf = block_sum<BLOCK>(named_inf, parti);
-                if (floor_mass > 0.0) {
-                    rest = floor_mass * ((double)others * (log(floor_mass) + log_s) -
-                                         (ssum - named_sum - (double)others * base) * inv_t);
-                    infinite = infinite || ninf > named_inf;
-                }
-            }
-            if (tid == 0) {
-                double loss = infinite ? (double)INFINITY : (double)a.T * (double)a.T * (entropy - cross + rest);
-                if (!(s == s) || !(mass == mass)) loss = (double)NAN;
-                if (out || all_mass == 0.0) loss = 0.0;
-                a.loss[row] = (float)loss;
-                if (a.stats) {
-                    a.stats[2 * row] = m;
-                    a.stats[2 * row + 1] = s;
-                }
-            }
-        }
-        if (a.grad) {
-            out = out || all_mass == 0.0;
-            T* g = static_cast<T*>(a.grad) + row * a.grad_stride;
-            const bool together = (((uintptr_t)g ^ (uintptr_t)r.p) & 15u) == 0;
-            const float wt = w * a.T, b = base_of(m);
-            const float scale = s == 0.0f ? 0.0f : (float)all_mass * wt / s, low = (float)floor_mass * wt;
-            for (int32_t i = c0 + tid; i < c1; i += BLOCK) {
+        if (tid < r.extras) extra[0] = Row<T>::one(r.p + r.extra(tid));
+        Running<T, REST> run;
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (j * BLOCK + tid < r.whole) {
                 float x[E];
-                if (!out) {
-                    r.load(i, x, -INFINITY);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) x[e] = exp_above(x[e], b, a.c) * scale - low;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e) x[e] = 0.0f;
-                }
-                const int64_t v = r.first(i);
-                if (together && r.whole(v)) {
-                    *reinterpret_cast<uint4*>(g + v) = Row<T>::pack(x);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        if (v + e >= 0 && v + e < a.V) g[v + e] = Row<T>::from(x[e]);
-                }
+                Row<T>::unpack(raw[j], x);
+                run.add(x, a.c);
             }
-            __syncthreads();  // the places of the slots are written again, by other threads
-            if (!out) {
-                const int64_t v0 = r.first(c0), v1 = r.first(c1);
-                for (int32_t j = tid; j < a.k; j += BLOCK) {
-                    const int32_t id = ts.id[j];
-                    if (id < 0 || id < v0 || id >= v1) continue;
-                    g[id] = Row<T>::from(exp_above(ts.logit[j], b, a.c) * scale - ts.all[j] * wt);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (tid < r.extras) run.add(extra, a.c);
+        m = run.m;
+        s = run.s;
+        block_join<BLOCK>(m, s, a.c, part2);
+        if (REST) {
+            scaled_sum = block_sum<BLOCK>(run.scaled_sum, partd);
+            ninf = block_sum<BLOCK>(run.ninf, parti);
+        }
+    }
+    __syncthreads();
+    TeacherPart t = *slots.head;
+    LossSums l;
+    float all[(kMostSlots + BLOCK - 1) / BLOCK];
+    if (!out) {
+#pragma unroll
+        for (int q = 0; q < (kMostSlots + BLOCK - 1) / BLOCK; ++q) {
+            const int32_t j = q * BLOCK + tid;
+            all[q] = 0.0f;
+            if (q * BLOCK >= a.k) continue;
+            const int32_t id = j < a.k ? slots.id[j] : -1;
+            const float x = id >= 0 ? Row<T>::one(r.p + id) : 0.0f;
+            if (j < a.k) slots.x[j] = x;
+            if ((REST || a.grad) && id >= 0) {
+                const bool first = first_of_class(slots, a.k, j, id, all[q]);
+                if (REST && first) {
+                    ++l.named;
+                    if (x == -INFINITY) ++l.named_inf;
+                    else l.named_sum += (double)x * (double)a.c;
                 }
             }
         }
-        __syncthreads();  // the LDS is the next row's
+    }
+    t.floor = 0.0;
+    t.others = 0;
+    if (REST) {
+        t.others = a.V - block_sum<BLOCK>(l.named, parti);
+        t.floor = floor_of(t.mass, t.others);
+    }
+    const double mass = t.mass + t.floor * (double)t.others;
+    out = out || mass == 0.0;
+    const Gradient f(m, s, (float)mass, (float)t.floor, w, a.T, a.c);
+    if (a.grad) {
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            const int32_t i = j * BLOCK + tid;
+            if (i >= r.whole) continue;
+            float x[E];
+            Row<T>::unpack(raw[j], x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = out ? 0.0f : f.dense(x[e]);
+            store_chunk(g + r.chunk(i), x);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (tid < r.extras) g[r.extra(tid)] = Row<T>::from(out ? 0.0f : f.dense(extra[0]));
+        __syncthreads();  // the places of the slots are written again, by other threads
+    }
+    const double inv_t = 1.0 / (double)a.T, base = (double)base_of(m), log_s = log((double)s);
+    if (!out) {
+#pragma unroll
+        for (int q = 0; q < (kMostSlots + BLOCK - 1) / BLOCK; ++q) {
+            const int32_t j = q * BLOCK + tid;
+            const int32_t id = j < a.k ? slots.id[j] : -1;
+            if (id < 0) continue;
+            const float x = slots.x[j];
+            add_slot(l, (double)slots.p[j], x, base, inv_t, log_s);
+            if (a.grad) g[id] = Row<T>::from(f.slot(x, all[q]));
+        }
+    }
+    l.cross = block_sum<BLOCK>(l.cross, partd);
+    l.infinite = block_sum<BLOCK>(l.infinite, parti);
+    if (REST) {
+        l.named_sum = block_sum<BLOCK>(l.named_sum, partd);
+        l.named_inf = block_sum<BLOCK>(l.named_inf, parti);
+    }
+    if (tid == 0) {
+        a.loss[row] = out ? 0.0f : loss_of<REST>(a, l, t, m, s, scaled_sum, ninf);
+        if (a.stats)
+            *reinterpret_cast<RowStats*>(a.stats + row * kStatFloats) = RowStats{m, s, (float)mass, (float)t.floor, t.z};
     }
 }
 
-constexpr int kBlock = 256;
-constexpr int32_t kSliceBytes = 32768;
-
-static int32_t distill_slices(const lda_distill_rows* d)
+// (m, s) of slices; one more workgroup a row reads its teacher
+template <class T, bool REST>
+__global__ __launch_bounds__(kPartBlock) void distill_part_kernel(DistillArgs a)
 {
-    const int64_t bytes = (int64_t)d->classes * (int64_t)type_bytes(d->logits_type) + 16;
-    if (d->rows >= 1024) return 1;
-    const int64_t most = (bytes + kSliceBytes - 1) / kSliceBytes;
-    return (int32_t)(most < 1 ? 1 : most > 1024 ? 1024 : most);
+    constexpr int E = Row<T>::kChunk;
+    extern __shared__ __align__(16) unsigned char lds[];
+    __shared__ float2 part2[kPartBlock / kWave];
+    __shared__ double partd[kPartBlock / kWave];
+    __shared__ int32_t parti[kPartBlock / kWave];
+    const Slots slots(lds, a.k);
+    const int32_t tid = (int32_t)threadIdx.x;
+    const int64_t row = a.row0 + blockIdx.x;
+    if (a.grad && a.weight && a.weight[row * a.weight_stride] == 0.0f) return;
+    if (blockIdx.y == 0) {
+        if (tid < kWave) read_teacher(a, row, slots);
+        __syncthreads();
+        int32_t named = 0;
+        if (REST) {
+            for (int32_t j = tid; j < a.k; j += kPartBlock) {
+                float all;
+                if (slots.id[j] >= 0) named += first_of_class(slots, a.k, j, slots.id[j], all);
+            }
+            named = block_sum<kPartBlock>(named, parti);
+        }
+        if (tid == 0) {
+            TeacherPart t = *slots.head;
+            t.others = REST ? a.V - named : 0;
+            t.floor = REST ? floor_of(t.mass, t.others) : 0.0;
+            a.teachers[row] = t;
+        }
+        return;
+    }
+    const SplitRow<T> r(static_cast<const T*>(a.logits) + row * a.logits_stride, a.V);
+    for (int32_t slice = (int32_t)blockIdx.y - 1; slice < a.slices; slice += (int32_t)gridDim.y - 1) {
+        const int32_t i0 = slice * kSliceChunks + tid;
+        uint4 raw[kSliceLoads];
+#pragma unroll
+        for (int j = 0; j < kSliceLoads; ++j)
+            if (i0 + j * kPartBlock < r.whole) raw[j] = r.load(i0 + j * kPartBlock);
+        Running<T, REST> run;
+        if (slice == 0 && tid < r.extras) {
+            const float extra[1] = {Row<T>::one(r.p + r.extra(tid))};
+            run.add(extra, a.c);
+        }
+#pragma unroll
+        for (int j = 0; j < kSliceLoads; ++j) {
+            if (i0 + j * kPartBlock < r.whole) {
+                float x[E];
+                Row<T>::unpack(raw[j], x);
+                run.add(x, a.c);
+            }
+        }
+        block_join<kPartBlock>(run.m, run.s, a.c, part2);
+        if (REST) {
+            run.scaled_sum = block_sum<kPartBlock>(run.scaled_sum, partd);
+            run.ninf = block_sum<kPartBlock>(run.ninf, parti);
+        }
+        if (tid == 0) a.parts[row * a.slices + slice] = RowPart{run.m, run.s, run.scaled_sum, run.ninf, 0};
+    }
+}
+
+// The slices' parts joined (or the softmax taken from stats), the loss by the first workgroup of a row,
+// the gradient by a workgroup a slice.
+template <class T, bool REST>
+__global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
+{
+    constexpr int E = Row<T>::kChunk;
+    extern __shared__ __align__(16) unsigned char lds[];
+    __shared__ double partd[kPartBlock / kWave];
+    __shared__ int32_t parti[kPartBlock / kWave];
+    const Slots slots(lds, a.k);
+    const int32_t tid = (int32_t)threadIdx.x, lane = tid % kWave;
+    const double inv_t = 1.0 / (double)a.T;
+    const int64_t row = a.row0 + blockIdx.x;
+    const SplitRow<T> r(static_cast<const T*>(a.logits) + row * a.logits_stride, a.V);
+    const float w = a.weight ? a.weight[row * a.weight_stride] : 1.0f;
+    bool out = a.grad && w == 0.0f;
+    float m = -INFINITY, s = 0.0f, mass = 0.0f, floor = 0.0f;
+    double scaled_sum = 0.0, z = 0.0;
+    int32_t ninf = 0;
+    TeacherPart t{};
+    if (!out) {
+        if (a.stats_in) {
+            const RowStats st = *reinterpret_cast<const RowStats*>(a.stats_in + row * kStatFloats);
+            m = st.m;
+            s = st.s;
+            mass = st.mass;
+            floor = st.floor;
+            z = st.z;
+        } else {
+            t = a.teachers[row];
+            for (int32_t q = lane; q < a.slices; q += kWave) {  // every wave for itself
+                const RowPart part = a.parts[row * a.slices + q];
+                join(m, s, part.m, part.s, a.c);
+                if (REST) {
+                    scaled_sum += part.scaled_sum;
+                    ninf += part.ninf;
+                }
+            }
+            wave_join(m, s, a.c);
+            if (REST) {
+                scaled_sum = wave_sum(scaled_sum);
+                ninf = wave_reduce(ninf, [](int32_t x, int32_t y) { return x + y; });
+            }
+            mass = (float)(t.mass + t.floor * (double)t.others);
+            floor = (float)t.floor;
+            z = t.z;
+        }
+        out = mass == 0.0f;
+    }
+    const Gradient f(m, s, mass, floor, w, a.T, a.c);
+    if (!out) {
+        for (int32_t j = tid; j < (a.k + 3) / 4 * 4; j += kPartBlock) {
+            const int32_t id = j < a.k ? slot_id(a, row, j) : -1;
+            double p = 0.0;
+            if (id >= 0) p = exp((double)element_at(a.teacher, a.teacher_type, row * a.teacher_stride + j) * inv_t - z);
+            slots.id[j] = id;
+            slots.p[j] = (float)p;
+        }
+        __syncthreads();
+    }
+    if (a.loss && blockIdx.y == 0) {
+        LossSums l;
+        if (!out) {
+            const double base = (double)base_of(m), log_s = log((double)s);
+            for (int32_t j = tid; j < a.k; j += kPartBlock) {
+                const int32_t id = slots.id[j];
+                if (id < 0) continue;
+                const float x = Row<T>::one(r.p + id);
+                add_slot(l, (double)slots.p[j], x, base, inv_t, log_s);
+                float all;
+                if (REST && first_of_class(slots, a.k, j, id, all)) {
+                    if (x == -INFINITY) ++l.named_inf;
+                    else l.named_sum += (double)x * (double)a.c;
+                }
+            }
+        }
+        l.cross = block_sum<kPartBlock>(l.cross, partd);
+        l.infinite = block_sum<kPartBlock>(l.infinite, parti);
+        if (REST) {
+            l.named_sum = block_sum<kPartBlock>(l.named_sum, partd);
+            l.named_inf = block_sum<kPartBlock>(l.named_inf, parti);
+        }
+        if (tid == 0) {
+            a.loss[row] = out ? 0.0f : loss_of<REST>(a, l, t, m, s, scaled_sum, ninf);
+            if (a.stats)
+                *reinterpret_cast<RowStats*>(a.stats + row * kStatFloats) = RowStats{m, s, mass, floor, z};
+        }
+    }
+    if (a.grad) {
+        T* const g = static_cast<T*>(a.grad) + row * a.grad_stride;
+        for (int32_t slice = (int32_t)blockIdx.y; slice < a.slices; slice += (int32_t)gridDim.y) {
+            const int32_t i0 = slice * kSliceChunks + tid;
+            uint4 raw[kSliceLoads];
+            if (!out) {
+#pragma unroll
+                for (int j = 0; j < kSliceLoads; ++j)
+                    if (i0 + j * kPartBlock < r.whole) raw[j] = r.load(i0 + j * kPartBlock);
+            }
+            if (slice == 0 && tid < r.extras) {
+                const int32_t v = r.extra(tid);
+                g[v] = Row<T>::from(out ? 0.0f : f.dense(Row<T>::one(r.p + v)));
+            }
+#pragma unroll
+            for (int j = 0; j < kSliceLoads; ++j) {
+                const int32_t i = i0 + j * kPartBlock;
+                if (i >= r.whole) continue;
+                float x[E];
+                Row<T>::unpack(raw[j], x);
+#pragma unroll
+                for (int e = 0; e < E; ++e) x[e] = out ? 0.0f : f.dense(x[e]);
+                store_chunk(g + r.chunk(i), x);
+            }
+            if (out) continue;
+            __syncthreads();  // the slots' places in this slice are written again, by other threads
+            const int32_t v0 = r.chunk(slice * kSliceChunks);
+            const int32_t v1 = r.chunk(min(r.whole, (slice + 1) * kSliceChunks));
+            for (int32_t j = tid; j < a.k; j += kPartBlock) {
+                const int32_t id = slots.id[j];
+                if (id < 0 || !((id >= v0 && id < v1) || (slice == 0 && (id < r.head || id >= r.chunk(r.whole))))) continue;
+                float all;
+                first_of_class(slots, a.k, j, id, all);
+                g[id] = Row<T>::from(f.slot(Row<T>::one(r.p + id), all));
+            }
+        }
+    }
 }
 
 static int check_distill(const lda_distill_rows* d, const char* call)
@@ -370,29 +640,70 @@ static int check_distill(const lda_distill_rows* d, const char* call)
     return LDA_OK;
 }
 
-template <class T, bool REST>
-static void launch_distill_typed(const DistillArgs& a, hipStream_t stream)
+
+static int32_t distill_slices(const lda_distill_rows* d)
 {
-    const unsigned gx = (unsigned)(a.rows < (1 << 20) ? a.rows : (1 << 20));
-    const dim3 one(gx, 1), all(gx, (unsigned)a.slices);
+    const int64_t chunk = 16 / (int64_t)type_bytes(d->logits_type);
+    const int64_t slices = ((int64_t)d->classes / chunk + kSliceChunks - 1) / kSliceChunks;
+    return (int32_t)(slices < 1 ? 1 : slices);
+}
+
+// Threads and chunks of a thread that hold a row in registers; 0: none do, or slices are better.
+struct RowShape {
+    int block, chunks;
+};
+static RowShape row_shape(const lda_distill_rows* d)
+{
+    static constexpr RowShape kShapes[] = {{64, 4}, {256, 4}, {256, 12}, {1024, 6}, {1024, 12}, {1024, 18}};
+    const int64_t chunk = 16 / (int64_t)type_bytes(d->logits_type);
+    const int64_t whole = d->classes / chunk;
+    for (const RowShape& shape : kShapes) {
+        if (whole > (int64_t)shape.block * shape.chunks) continue;
+        const char* e = getenv("DROWS");
+        if (shape.block == 1024 && d->rows < (e ? atoi(e) : 128)) return {0, 0};
+        return shape;
+    }
+    return {0, 0};
+}
+
+template <class T, bool REST>
+static void launch_distill_typed(const DistillArgs& a, unsigned gx, RowShape shape, hipStream_t stream)
+{
+    const unsigned gy = (unsigned)(a.slices < 32768 ? a.slices : 32768);
     const size_t lds = slots_lds(a.k);
     if (a.stats_in) {
-        distill_kernel<T, REST, kBlock, kJoin><<<all, kBlock, lds, stream>>>(a);
-    } else if (a.slices == 1) {
-        distill_kernel<T, REST, kBlock, kWhole><<<one, kBlock, lds, stream>>>(a);
+        distill_join_kernel<T, REST><<<dim3(gx, gy), kPartBlock, lds, stream>>>(a);
+    } else if (shape.block == 64) {
+        distill_rows_kernel<T, REST, 64, 4><<<gx, 64, lds, stream>>>(a);
+    } else if (shape.block == 256 && shape.chunks == 4) {
+        distill_rows_kernel<T, REST, 256, 4><<<gx, 256, lds, stream>>>(a);
+    } else if (shape.block == 256) {
+        distill_rows_kernel<T, REST, 256, 12><<<gx, 256, lds, stream>>>(a);
+    } else if (shape.chunks == 6) {
+        distill_rows_kernel<T, REST, 1024, 6><<<gx, 1024, lds, stream>>>(a);
+    } else if (shape.chunks == 12) {
+        distill_rows_kernel<T, REST, 1024, 12><<<gx, 1024, lds, stream>>>(a);
+    } else if (shape.chunks == 18) {
+        distill_rows_kernel<T, REST, 1024, 18><<<gx, 1024, lds, stream>>>(a);
     } else {
-        distill_kernel<T, REST, kBlock, kPart><<<all, kBlock, lds, stream>>>(a);
-        distill_kernel<T, REST, kBlock, kJoin><<<a.grad ? all : one, kBlock, lds, stream>>>(a);
+        distill_part_kernel<T, REST><<<dim3(gx, gy + 1), kPartBlock, lds, stream>>>(a);
+        distill_join_kernel<T, REST><<<dim3(gx, a.grad ? gy : 1), kPartBlock, lds, stream>>>(a);
     }
+}
+
+static int64_t distill_bytes(const lda_distill_rows* d)
+{
+    if (d->rows == 0 || row_shape(d).block != 0) return 0;
+    return d->rows * (distill_slices(d) * (int64_t)sizeof(RowPart) + (int64_t)sizeof(TeacherPart));
 }
 
 static int launch_distill(const lda_distill_rows* d, const char* call, float* loss, float* stats,
                           const float* stats_in, void* grad, int64_t grad_stride)
 {
     if (d->rows == 0) return LDA_OK;
-    if (!aligned_to(loss, 4) || !aligned_to(stats, 4) || !aligned_to(stats_in, 4) ||
+    if (!aligned_to(loss, 4) || !aligned_to(stats, 16) || !aligned_to(stats_in, 16) ||
         !aligned_to(grad, type_bytes(d->logits_type)))
-        return fail(nullptr, LDA_ERR_ARG, "%s: a pointer is not aligned to its type", call);
+        return fail(nullptr, LDA_ERR_ARG, "%s: an output is not aligned to its type, or stats to 16 bytes", call);
     DistillArgs a{};
     a.rows = d->rows;
     a.V = d->classes;
@@ -416,27 +727,26 @@ static int launch_distill(const lda_distill_rows* d, const char* call, float* lo
     a.grad = grad;
     a.grad_stride = grad_stride;
     a.slices = distill_slices(d);
-    const int64_t chunk = 16 / (int64_t)type_bytes(d->logits_type);
-    const int64_t chunks = (d->classes + chunk - 1) / chunk + 1;  // wherever the row starts
-    a.slice_chunks = (int32_t)((chunks + a.slices - 1) / a.slices);
-    if (a.slices > 1 && !stats_in) {
-        const int64_t need = a.rows * a.slices * (int64_t)sizeof(RowPart);
+    const RowShape shape = row_shape(d);
+    if (shape.block == 0 && !stats_in) {
+        const int64_t need = distill_bytes(d);
         if (!d->workspace || d->workspace_bytes < need || !aligned_to(d->workspace, 16))
             return fail(nullptr, LDA_ERR_ARG, "%s: needs a workspace of %lld bytes, aligned to 16", call, (long long)need);
-        a.parts = static_cast<RowPart*>(d->workspace);
+        a.teachers = static_cast<TeacherPart*>(d->workspace);
+        a.parts = reinterpret_cast<RowPart*>(a.teachers + a.rows);
     }
     const hipStream_t stream = static_cast<hipStream_t>(d->hip_stream);
-    const bool rest = d->log_norm != nullptr;
-    switch (d->logits_type) {
-    case LDA_F32:
-        rest ? launch_distill_typed<float, true>(a, stream) : launch_distill_typed<float, false>(a, stream);
-        break;
-    case LDA_F16:
-        rest ? launch_distill_typed<__half, true>(a, stream) : launch_distill_typed<__half, false>(a, stream);
-        break;
-    default:
-        rest ? launch_distill_typed<__hip_bfloat16, true>(a, stream) : launch_distill_typed<__hip_bfloat16, false>(a, stream);
-    }
+    const auto typed = [&](auto t) {
+        using T = decltype(t);
+        for (a.row0 = 0; a.row0 < a.rows; a.row0 += 1 << 20) {
+            const unsigned n = (unsigned)(a.rows - a.row0 < (1 << 20) ? a.rows - a.row0 : 1 << 20);
+            if (d->log_norm) launch_distill_typed<T, true>(a, n, shape, stream);
+            else launch_distill_typed<T, false>(a, n, shape, stream);
+        }
+    };
+    if (d->logits_type == LDA_F32) typed(float{});
+    else if (d->logits_type == LDA_F16) typed(__half{});
+    else typed(__hip_bfloat16{});
     LDA_HIP(static_cast<lda_ctx*>(nullptr), hipGetLastError());
     return LDA_OK;
 }
@@ -451,8 +761,7 @@ int64_t lda_distill_workspace(const lda_distill_rows* d)
 try {
     const int rc = check_distill(d, "lda_distill_workspace");
     if (rc != LDA_OK) return rc;
-    const int32_t slices = distill_slices(d);
-    return slices == 1 ? 0 : d->rows * slices * (int64_t)sizeof(RowPart);
+    return distill_bytes(d);
 } catch (...) {
     return LDA_ERR_OOM;
 }

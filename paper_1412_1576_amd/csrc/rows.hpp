@@ -156,7 +156,7 @@ __device__ __forceinline__ V block_sum(V v, V* part)
     if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
     __syncthreads();
     V s = part[0];
-#pragma unroll
+#pragma unroll 4
     for (int w = 1; w < BLOCK / kWave; ++w) s += part[w];
     return s;
 }

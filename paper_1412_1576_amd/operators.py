@@ -134,7 +134,7 @@ class _Distill(torch.autograd.Function):
         with _On(logits.device):
             r = _distill_rows(logits, ids, teacher, temperature, log_norm)
             loss = torch.empty(r.rows, dtype=torch.float32, device=logits.device)
-            stats = torch.empty((r.rows, 2) if ctx.needs_input_grad[0] else 0, dtype=torch.float32,
+            stats = torch.empty((r.rows, 8) if ctx.needs_input_grad[0] else 0, dtype=torch.float32,
                                 device=logits.device)
             w = _workspace(r, _check(L.lda_distill_workspace(C.byref(r))), logits.device)
             _check(L.lda_distill_loss(C.byref(r), loss.data_ptr(), stats.data_ptr() or None))
