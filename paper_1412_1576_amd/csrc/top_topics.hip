@@ -4,9 +4,9 @@
 // differ, larger keys come first in the output, and "the k largest" is one set.  What is done a document
 // depends on its length alone (the host does not know it):
 //   up to kWaveTokens   a wave; counts in an open-addressing table in LDS, the keys ranked against each other
-//   up to kTableTokens  a workgroup of 256, the same
+//   up to kTableTokens  a workgroup of 1024, the same
 //   longer              a workgroup of 1024; a counter a topic in LDS, a range of topics at a time
-// A kernel for each length looks through all rows and leaves the others' rows alone.
+// One kernel takes the first, one the others; each looks through all rows and leaves the others' alone.
 #include "rows.hpp"
 
 namespace lda {
@@ -16,7 +16,6 @@ constexpr uint32_t kInverted = (1u << kMixTopicBits) - 1u;  // a key's topic is 
 
 constexpr int kWaveBlock = 256;          // four documents at a time
 constexpr int32_t kWaveTokens = 512;     // table: twice as many slots
-constexpr int kTableBlock = 256;
 constexpr int32_t kTableTokens = 4095;   // the count of a 32-bit key has 12 bits
 constexpr int kLongBlock = 1024;
 constexpr int32_t kLongWords = 31;       // counters in LDS, a thread: an odd number, for its banks
@@ -85,7 +84,7 @@ __device__ __forceinline__ int32_t topics_by_table(const TopicArgs& a, int64_t r
     int32_t n = 0, counted = 0;
     if (TEAM > kWave) {
         if (me == 0) *n_used = 0;
-        __syncthreads();
+        __syncthreads();  // and the table is empty
     }
     for (int32_t i0 = 0; i0 < L; i0 += TEAM) {
         const int32_t i = i0 + me;
@@ -139,7 +138,7 @@ __device__ __forceinline__ int32_t topics_by_table(const TopicArgs& a, int64_t r
     }
     int32_t n_best = n;
     uint32_t least = 1;
-    if (n > 2 * TEAM && n > a.k) {
+    if (n > (TEAM == kWave ? 2 * kWave : 8 * kWave) && n > a.k) {
         // too many to rank them all: the smallest of the best k first, bit by bit
         least = 0;
         for (int bit = 31 - __builtin_clz((uint32_t)L) + (int)kMixTopicBits; bit >= 0; --bit) {
@@ -243,23 +242,6 @@ __device__ __forceinline__ void for_rows_of_length(const TopicArgs& a, int32_t l
     }
 }
 
-__global__ __launch_bounds__(kTableBlock, 2) void table_topics_kernel(TopicArgs a)
-{
-    constexpr int kSlots = 2 * (kTableTokens + 1);
-    __shared__ __align__(16) uint32_t table[kSlots];
-    __shared__ __align__(16) uint32_t keys[kTableTokens + 5];
-    __shared__ uint16_t used[kTableTokens + 1];
-    __shared__ int32_t mine[kTableBlock], n_mine, n_used, part[kTableBlock / kWave];
-    for (int32_t i = (int32_t)threadIdx.x; i < kSlots; i += kTableBlock) table[i] = 0;
-    __syncthreads();
-    const double k_alpha = (double)a.K * a.alpha;
-    for_rows_of_length<kTableBlock>(a, kWaveTokens + 1, kTableTokens, mine, &n_mine, [&](int64_t row, int64_t g0, int32_t L) {
-        const int32_t counted = topics_by_table<kTableBlock, kSlots>(
-            a, row, g0, L, table, keys, used, &n_used, part, [&](int32_t n) { return (float)log((double)n + a.alpha); });
-        if (threadIdx.x == 0 && a.log_norm) a.log_norm[row] = (float)log((double)counted + k_alpha);
-    });
-}
-
 __device__ __forceinline__ uint64_t long_key(uint32_t count, int32_t topic)
 {
     return ((uint64_t)count << kMixTopicBits) | (uint64_t)(kInverted - (uint32_t)topic);
@@ -289,8 +271,16 @@ __device__ __forceinline__ int32_t block_prefix(int32_t v, int32_t* part, int32_
     return before + sum - v;
 }
 
+struct TableLds {
+    uint32_t table[2 * (kTableTokens + 1)];
+    uint32_t keys[kTableTokens + 5];
+    uint16_t used[kTableTokens + 1];
+};
 struct LongLds {
-    uint32_t count[kLongWords * kLongBlock];
+    union {
+        TableLds table;
+        uint32_t count[kLongWords * kLongBlock];
+    };
     uint64_t keys[2 * kMostTopSlots];  // the best so far, and the range's behind them
     uint64_t best[kMostTopSlots];
     uint32_t histogram[1 << kDigit];
@@ -430,11 +420,23 @@ __global__ __launch_bounds__(kLongBlock) void long_topics_kernel(TopicArgs a)
 {
     extern __shared__ __align__(16) unsigned char raw[];
     LongLds& lds = *reinterpret_cast<LongLds*>(raw);
-    for_rows_of_length<kLongBlock>(a, kTableTokens + 1, INT32_MAX, lds.mine, &lds.n_mine,
+    for_rows_of_length<kLongBlock>(a, kWaveTokens + 1, INT32_MAX, lds.mine, &lds.n_mine,
                                    [&](int64_t row, int64_t g0, int32_t L) {
-                                       if (L < 65536) topics_by_counters<false>(a, row, g0, L, lds);
-                                       else topics_by_counters<true>(a, row, g0, L, lds);
-                                   });
+        if (L <= kTableTokens) {
+            constexpr int kSlots = 2 * (kTableTokens + 1);
+            TableLds& t = lds.table;
+            __syncthreads();
+            for (int32_t i = (int32_t)threadIdx.x; i < kSlots; i += kLongBlock) t.table[i] = 0;
+            const int32_t counted = topics_by_table<kLongBlock, kSlots>(
+                a, row, g0, L, t.table, t.keys, t.used, &lds.n_keys, lds.part,
+                [&](int32_t n) { return (float)log((double)n + a.alpha); });
+            if (threadIdx.x == 0 && a.log_norm) a.log_norm[row] = (float)log((double)counted + (double)a.K * a.alpha);
+        } else if (L < 65536) {
+            topics_by_counters<false>(a, row, g0, L, lds);
+        } else {
+            topics_by_counters<true>(a, row, g0, L, lds);
+        }
+    });
 }
 
 static int launch_top_topics(lda_ctx* c, const TopicArgs& a, hipStream_t stream)
@@ -446,8 +448,7 @@ static int launch_top_topics(lda_ctx* c, const TopicArgs& a, hipStream_t stream)
     };
     // documents cannot be longer than all of z
     wave_topics_kernel<<<grid(kWaveBlock / kWave, 256 * 5), kWaveBlock, 0, stream>>>(a);
-    if (a.tokens > kWaveTokens) table_topics_kernel<<<grid(1, 256 * 2), kTableBlock, 0, stream>>>(a);
-    if (a.tokens > kTableTokens) {
+    if (a.tokens > kWaveTokens) {
         LDA_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(long_topics_kernel),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(LongLds)));
         long_topics_kernel<<<grid(1, 256), kLongBlock, sizeof(LongLds), stream>>>(a);

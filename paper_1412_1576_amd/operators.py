@@ -11,8 +11,6 @@ refusals of the library LdaError.
 """
 from __future__ import annotations
 
-import ctypes as C
-
 import torch
 
 from . import lda
@@ -21,21 +19,29 @@ from .lda import LDA_OK, LdaError
 _FLOATS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _INDEXES = {torch.int32: 0, torch.int64: 1}
 _INT32 = 2 ** 31 - 1
+_raw_stream = torch._C._cuda_getCurrentRawStream  # of a device's number; what current_stream() wraps
 
 
-def _tensor(x, name, dims, types, device=None, spread=False):
+def _tensor(x, name, dims, types, device=None, shape=None, spread=False):
+    """The checks of one argument; returns its strides.  A few tests on the way that a right
+    call takes: small calls are bound by the host."""
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise ValueError("%s must be a tensor on the GPU" % name)
     if x.dtype not in types:
         raise ValueError("%s must be one of %s, not %s" % (name, ", ".join(map(str, types)), x.dtype))
-    if x.dim() != dims:
-        raise ValueError("%s must have %d dimensions, not %d" % (name, dims, x.dim()))
-    if device is not None and x.device != device:
-        raise ValueError("%s is on %s, not on %s" % (name, x.device, device))
-    if not spread and x.stride(-1) != 1 and x.size(-1) > 1:
+    size, stride = x.shape, x.stride()
+    if len(size) != dims:
+        raise ValueError("%s must have %d dimensions, not %d" % (name, dims, len(size)))
+    if device is not None and x.get_device() != device:
+        raise ValueError("%s is on %s, not on cuda:%d" % (name, x.device, device))
+    if shape is not None and size != shape:
+        raise ValueError("%s has shape %s, not %s" % (name, tuple(size), tuple(shape)))
+    last = size[-1]
+    if not spread and stride[-1] != 1 and last > 1:
         raise ValueError("%s: elements of a row must be adjacent (call .contiguous())" % name)
-    if x.size(-1) > _INT32 and dims > 1:
+    if last > _INT32 and dims > 1:
         raise ValueError("%s: a row has at most 2^31 - 1 elements" % name)
+    return stride
 
 
 def _int32(x, name):
@@ -45,11 +51,6 @@ def _int32(x, name):
     return x
 
 
-def _shape(x, name, shape):
-    if tuple(x.shape) != tuple(shape):
-        raise ValueError("%s has shape %s, not %s" % (name, tuple(x.shape), tuple(shape)))
-
-
 def _check(rc):
     if rc < LDA_OK:
         raise LdaError(rc, (lda.load_library().lda_last_error(None) or b"").decode())
@@ -57,18 +58,18 @@ def _check(rc):
 
 
 class _On:
-    """The tensors' device as the current one, for the length of a call."""
+    """A device as the current one, for the length of a call."""
 
     def __init__(self, device):
         self.device = device
 
     def __enter__(self):
         self.before = torch.cuda.current_device()
-        if self.before != self.device.index:
+        if self.before != self.device:
             torch.cuda.set_device(self.device)
 
     def __exit__(self, *exc):
-        if self.before != self.device.index:
+        if self.before != self.device:
             torch.cuda.set_device(self.before)
 
 
@@ -82,39 +83,31 @@ def _workspace(r, nbytes, device):
 
 
 def _distill_rows(logits, ids, teacher, temperature, log_norm, weight=None, weight_stride=0):
-    device = logits.device
-    r = lda.lda_distill_rows()
-    r.rows, r.classes = logits.shape
-    r.slots = ids.shape[1]
-    r.logits, r.logits_stride = logits.data_ptr(), logits.stride(0)
-    r.ids, r.ids_stride = ids.data_ptr(), ids.stride(0)
-    r.teacher, r.teacher_stride = teacher.data_ptr(), teacher.stride(0)
-    if log_norm is not None:
-        r.log_norm = log_norm.data_ptr()
-    if weight is not None:
-        r.weight, r.weight_stride = weight.data_ptr(), weight_stride
-    r.logits_type, r.teacher_type = _FLOATS[logits.dtype], _FLOATS[teacher.dtype]
-    r.ids_type = _INDEXES[ids.dtype]
-    r.temperature = temperature
-    r.hip_stream = torch.cuda.current_stream(device).cuda_stream
-    return r
+    # in the order of the struct's fields
+    rows, classes = logits.shape
+    return lda.lda_distill_rows(
+        rows, classes, ids.shape[1], logits.data_ptr(), logits.stride(0), ids.data_ptr(), ids.stride(0),
+        teacher.data_ptr(), teacher.stride(0), None if log_norm is None else log_norm.data_ptr(),
+        None if weight is None else weight.data_ptr(), weight_stride, _FLOATS[logits.dtype],
+        _INDEXES[ids.dtype], _FLOATS[teacher.dtype], temperature, None, 0,
+        _raw_stream(logits.get_device()))
 
 
-def _check_distill(logits, ids, teacher, temperature, log_norm):
+def _check_distill(logits, ids, teacher, log_norm):
     _tensor(logits, "logits", 2, _FLOATS)
-    device, n = logits.device, logits.size(0)
-    if logits.size(1) < 1:
+    device = logits.get_device()
+    n, classes = logits.shape
+    if classes < 1:
         raise ValueError("logits: at least one class needed")
     _tensor(ids, "ids", 2, _INDEXES, device)
-    _tensor(teacher, "teacher", 2, _FLOATS, device)
-    _shape(ids, "ids", (n, ids.size(1)))
-    _shape(teacher, "teacher", ids.shape)
+    if ids.size(0) != n:
+        raise ValueError("ids has %d rows, logits %d" % (ids.size(0), n))
+    _tensor(teacher, "teacher", 2, _FLOATS, device, ids.shape)
     if log_norm is not None:
-        _tensor(log_norm, "log_norm", 1, (torch.float32,), device)
-        _shape(log_norm, "log_norm", (n,))
-    for x, name in ((teacher, "teacher"), (log_norm, "log_norm")):
-        if x is not None and x.requires_grad:
-            raise ValueError("%s: the teacher is a constant (call .detach())" % name)
+        _tensor(log_norm, "log_norm", 1, (torch.float32,), device, (n,))
+    if teacher.requires_grad or log_norm is not None and log_norm.requires_grad:
+        raise ValueError("teacher: a constant (call .detach() on it and on log_norm)")
+    return device
 
 
 def _gradient_like(logits):
@@ -131,13 +124,13 @@ class _Distill(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, ids, teacher, log_norm, temperature):
         L = lda.load_library()
-        with _On(logits.device):
+        with _On(logits.get_device()):
             r = _distill_rows(logits, ids, teacher, temperature, log_norm)
             loss = torch.empty(r.rows, dtype=torch.float32, device=logits.device)
             stats = torch.empty((r.rows, 8) if ctx.needs_input_grad[0] else 0, dtype=torch.float32,
                                 device=logits.device)
-            w = _workspace(r, _check(L.lda_distill_workspace(C.byref(r))), logits.device)
-            _check(L.lda_distill_loss(C.byref(r), loss.data_ptr(), stats.data_ptr() or None))
+            w = _workspace(r, _check(L.lda_distill_workspace(r)), logits.device)
+            _check(L.lda_distill_loss(r, loss.data_ptr(), stats.data_ptr() or None))
             del w
         ctx.save_for_backward(logits, ids, teacher, log_norm, stats)
         ctx.temperature = temperature
@@ -148,11 +141,11 @@ class _Distill(torch.autograd.Function):
     def backward(ctx, upstream):
         logits, ids, teacher, log_norm, stats = ctx.saved_tensors
         L = lda.load_library()
-        with _On(logits.device):
+        with _On(logits.get_device()):
             grad = _gradient_like(logits)
             r = _distill_rows(logits, ids, teacher, ctx.temperature, log_norm, upstream,
                               upstream.stride(0))
-            _check(L.lda_distill_grad(C.byref(r), stats.data_ptr(), grad.data_ptr(), grad.stride(0)))
+            _check(L.lda_distill_grad(r, stats.data_ptr(), grad.data_ptr(), grad.stride(0)))
         return grad, None, None, None, None
 
 
@@ -166,7 +159,7 @@ def distill_loss(logits, ids, teacher, *, temperature=1.0, log_norm=None):
     the classes without a slot.  The loss is temperature^2 KL(teacher || softmax(logits / temperature)).
     Rows of a tensor may lie any distance apart; within a row elements are adjacent.
     """
-    _check_distill(logits, ids, teacher, temperature, log_norm)
+    _check_distill(logits, ids, teacher, log_norm)
     return _Distill.apply(logits, ids, teacher, log_norm, float(temperature))
 
 
@@ -176,19 +169,17 @@ def distill_loss_and_grad(logits, ids, teacher, *, temperature=1.0, log_norm=Non
     weight: float32 [rows], None: ones.  Rows of weight 0 are left out: loss and gradient 0, whatever
     their logits hold.  Use logits.backward(gradient) to go on from there.
     """
-    _check_distill(logits, ids, teacher, temperature, log_norm)
-    logits = logits.detach()
+    device = _check_distill(logits, ids, teacher, log_norm)
+    spread = 0
     if weight is not None:
-        _tensor(weight, "weight", 1, (torch.float32,), logits.device, spread=True)
-        _shape(weight, "weight", (logits.size(0),))
+        spread, = _tensor(weight, "weight", 1, (torch.float32,), device, logits.shape[:1], spread=True)
     L = lda.load_library()
-    with _On(logits.device):
-        r = _distill_rows(logits, ids, teacher, float(temperature), log_norm, weight,
-                          0 if weight is None else weight.stride(0))
-        loss = torch.empty(r.rows, dtype=torch.float32, device=logits.device)
+    with _On(device):
+        r = _distill_rows(logits, ids, teacher, temperature, log_norm, weight, spread)
+        loss = torch.empty(r.rows, dtype=torch.float32, device=device)
         grad = _gradient_like(logits)
-        w = _workspace(r, _check(L.lda_distill_workspace(C.byref(r))), logits.device)
-        _check(L.lda_distill_step(C.byref(r), loss.data_ptr(), grad.data_ptr(), grad.stride(0)))
+        w = _workspace(r, _check(L.lda_distill_workspace(r)), device)
+        _check(L.lda_distill_step(r, loss.data_ptr(), grad.data_ptr(), grad.stride(0)))
         del w
     return loss, grad
 
@@ -203,40 +194,30 @@ def verify_drafts(target, draft, tokens, accept_u, draw_u, *, lengths=None):
     from what the target has left (or from its next row), then -1.  With steps = 0 the call draws
     one token from every row of target.
     """
-    _tensor(target, "target", 3, _FLOATS)
-    device = target.device
-    B, T, V = target.size(0), _int32(target.size(1) - 1, "steps"), target.size(2)
+    in_target = _tensor(target, "target", 3, _FLOATS)
+    device = target.get_device()
+    B, T, V = target.shape
+    T = _int32(T - 1, "steps")
     if T < 0 or V < 1:
         raise ValueError("target must have steps + 1 rows of at least one class")
-    _tensor(draft, "draft", 3, (target.dtype,), device)
-    _shape(draft, "draft", (B, T, V))
-    _tensor(tokens, "tokens", 2, _INDEXES, device)
-    _shape(tokens, "tokens", (B, T))
-    _tensor(accept_u, "accept_u", 2, (torch.float32,), device)
-    _shape(accept_u, "accept_u", (B, T))
-    _tensor(draw_u, "draw_u", 1, (torch.float32,), device)
-    _shape(draw_u, "draw_u", (B,))
+    in_draft = _tensor(draft, "draft", 3, (target.dtype,), device, (B, T, V))
+    in_tokens = _tensor(tokens, "tokens", 2, _INDEXES, device, (B, T))
+    in_accept = _tensor(accept_u, "accept_u", 2, (torch.float32,), device, (B, T))
+    _tensor(draw_u, "draw_u", 1, (torch.float32,), device, (B,))
     if lengths is not None:
-        _tensor(lengths, "lengths", 1, (torch.int32,), device)
-        _shape(lengths, "lengths", (B,))
+        _tensor(lengths, "lengths", 1, (torch.int32,), device, (B,))
     L = lda.load_library()
     with _On(device):
-        r = lda.lda_draft_rows()
-        r.sequences, r.steps, r.classes = B, T, V
-        r.target = target.data_ptr()
-        r.target_sequence_stride, r.target_row_stride = target.stride(0), target.stride(1)
-        r.draft = draft.data_ptr()
-        r.draft_sequence_stride, r.draft_row_stride = draft.stride(0), draft.stride(1)
-        r.tokens, r.tokens_stride = tokens.data_ptr(), tokens.stride(0)
-        r.lengths = None if lengths is None else lengths.data_ptr()
-        r.accept_u, r.accept_u_stride = accept_u.data_ptr(), accept_u.stride(0)
-        r.draw_u = draw_u.data_ptr()
-        r.probs_type, r.tokens_type = _FLOATS[target.dtype], _INDEXES[tokens.dtype]
-        r.hip_stream = torch.cuda.current_stream(device).cuda_stream
+        # in the order of the struct's fields
+        r = lda.lda_draft_rows(
+            B, T, V, target.data_ptr(), in_target[0], in_target[1], draft.data_ptr(), in_draft[0], in_draft[1],
+            tokens.data_ptr(), in_tokens[0], None if lengths is None else lengths.data_ptr(),
+            accept_u.data_ptr(), in_accept[0], draw_u.data_ptr(), _FLOATS[target.dtype],
+            _INDEXES[tokens.dtype], None, 0, _raw_stream(device))
         accepted = torch.empty(B, dtype=torch.int32, device=device)
         out = torch.empty(B, T + 1, dtype=tokens.dtype, device=device)
-        w = _workspace(r, _check(L.lda_verify_workspace(C.byref(r))), device)
-        _check(L.lda_verify_drafts(C.byref(r), accepted.data_ptr(), out.data_ptr(), out.stride(0)))
+        w = _workspace(r, _check(L.lda_verify_workspace(r)), device)
+        _check(L.lda_verify_drafts(r, accepted.data_ptr(), out.data_ptr(), T + 1))
         del w
     return accepted, out
 
@@ -256,30 +237,29 @@ def top_topics(z, doc_offsets, K, slots, alpha, *, docs=None):
     int32: the documents wanted, in this order (None: all).
     """
     _tensor(z, "z", 1, (torch.int32,))
-    device = z.device
+    device = z.get_device()
     _tensor(doc_offsets, "doc_offsets", 1, _INDEXES, device)
-    if doc_offsets.numel() < 1:
+    documents = doc_offsets.numel() - 1
+    if documents < 0:
         raise ValueError("doc_offsets must have documents + 1 entries")
     if docs is not None:
         _tensor(docs, "docs", 1, (torch.int32,), device)
+    n = documents if docs is None else docs.numel()
+    slots = _int32(slots, "slots")
     L = lda.load_library()
     with _On(device):
-        r = lda.lda_topic_rows()
-        r.documents = doc_offsets.numel() - 1
-        r.rows = r.documents if docs is None else docs.numel()
-        r.docs = None if docs is None else docs.data_ptr()
-        r.offsets, r.offsets_type = doc_offsets.data_ptr(), _INDEXES[doc_offsets.dtype]
-        r.K, r.z, r.tokens = _int32(K, "K"), z.data_ptr(), z.numel()
-        r.slots, r.alpha = _int32(slots, "slots"), float(alpha)
-        r.hip_stream = torch.cuda.current_stream(device).cuda_stream
-        ids, logits, log_norm = _teacher_rows(r.rows, max(r.slots, 0), device)
-        _check(L.lda_top_topics(C.byref(r), ids.data_ptr(), logits.data_ptr(), log_norm.data_ptr()))
+        # in the order of the struct's fields
+        r = lda.lda_topic_rows(n, None if docs is None else docs.data_ptr(), documents, doc_offsets.data_ptr(),
+                               _INDEXES[doc_offsets.dtype], _int32(K, "K"), z.data_ptr(), z.numel(), slots, 0,
+                               alpha, _raw_stream(device))
+        ids, logits, log_norm = _teacher_rows(n, max(slots, 0), device)
+        _check(L.lda_top_topics(r, ids.data_ptr(), logits.data_ptr(), log_norm.data_ptr()))
     return ids, logits, log_norm
 
 
 def doc_topics(sampler, slots, docs=None):
     """Lda.doc_topics: top_topics of a sampler's current assignment."""
-    device = torch.device("cuda", torch.cuda.current_device())
+    device = torch.cuda.current_device()
     slots = _int32(slots, "slots")
     if docs is not None:
         _tensor(docs, "docs", 1, (torch.int32,), device)
