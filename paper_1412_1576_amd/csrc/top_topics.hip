@@ -2,24 +2,30 @@
 //
 // A topic with its count is one key, the count above the inverted topic: all keys of a document
 // differ, larger keys come first in the output, and "the k largest" is one set.  What is done a document
-// depends on its length alone (the host does not know it):
-//   up to kWaveTokens   a wave; counts in an open-addressing table in LDS, the keys ranked against each other
-//   up to kTableTokens  a workgroup of 1024, the same
-//   longer              a workgroup of 1024; a counter a topic in LDS, a range of topics at a time
-// One kernel takes the first, one the others; each looks through all rows and leaves the others' alone.
+// depends on its length and its number of topics alone, which the host does not know:
+//   a wave, with a table of counts in LDS, takes documents of up to kWaveTokens tokens and kWaveTopics
+//     topics (all that have at most so many tokens, and most of the others);
+//   a workgroup of 1024 takes the rest, with a counter a topic in LDS, a range of topics at a time, and
+//     the best k chosen by histograms of the counts' digits.  In a very large K (more than
+//     kFewRanges ranges) a table comes first, which holds up to kTableTopics topics whatever K is.
+// The first kernel leaves a mark in the rows that the second has to take.
 #include "rows.hpp"
 
 namespace lda {
 
 constexpr int32_t kMostTopSlots = 1024;
 constexpr uint32_t kInverted = (1u << kMixTopicBits) - 1u;  // a key's topic is kInverted - (key & kInverted)
+constexpr int32_t kUnfinished = -2;      // in a row's first id, between the kernels
 
 constexpr int kWaveBlock = 256;          // four documents at a time
-constexpr int32_t kWaveTokens = 512;     // table: twice as many slots
-constexpr int32_t kTableTokens = 4095;   // the count of a 32-bit key has 12 bits
+constexpr int32_t kWaveTopics = 512;     // the table has twice as many slots
+constexpr int32_t kWaveTokens = 4095;    // the count of a 32-bit key has 12 bits
 constexpr int kLongBlock = 1024;
-constexpr int32_t kLongWords = 31;       // counters in LDS, a thread: an odd number, for its banks
-constexpr int32_t kDigit = 10;           // bits of a count that a histogram takes at a time
+constexpr int32_t kTableSlots = 12288, kTableTopics = 8192;
+constexpr int32_t kLongWords = 31;       // words of counters in LDS, a thread at most
+constexpr int32_t kFewRanges = 4;
+constexpr int32_t kListTopics = kLongWords * kLongBlock / 2;  // keys that fit the counters' room
+constexpr int32_t kDigit = 10;           // bits of a key that a histogram takes at a time
 
 struct TopicArgs {
     int64_t rows;
@@ -47,132 +53,130 @@ __device__ __forceinline__ void document_of(const TopicArgs& a, int64_t row, int
     g1 = min(g1, g0 + INT32_MAX);
 }
 
-// Which threads work on a document together
-template <int TEAM>
-struct Team {
-    static __device__ __forceinline__ int32_t rank() { return (int32_t)threadIdx.x % TEAM; }
-    // LDS written by some threads of the team is read by others after this
-    static __device__ __forceinline__ void order()
-    {
-        if (TEAM == kWave) wave_lds_order();
-        else __syncthreads();
-    }
-    // sum of a wave's count (the same in its lanes) over the team
-    static __device__ __forceinline__ int32_t sum(int32_t wave_count, int32_t* part)
-    {
-        if (TEAM == kWave) return wave_count;
-        __syncthreads();
-        if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = wave_count;
-        __syncthreads();
-        int32_t s = 0;
-#pragma unroll
-        for (int w = 0; w < TEAM / kWave; ++w) s += part[w];
-        return s;
-    }
-};
-
-// One document's counts in a table of SLOTS keys (0: empty), and its best k topics.  `keys` holds
-// the document's keys and `best` (SLOTS / 2 each); the table is empty before and after.
-template <int TEAM, int SLOTS, class LogCount>
-__device__ __forceinline__ int32_t topics_by_table(const TopicArgs& a, int64_t row, int64_t g0, int32_t L,
-                                                   uint32_t* table, uint32_t* keys, uint16_t* used, int32_t* n_used,
-                                                   int32_t* part, LogCount log_count)
+// One document's counts in a table of 2 kWaveTopics keys (0: empty), and its best k topics, by one wave.
+// `used` has room for kWaveTopics slots; the table is empty before and after.
+// Returns the number of tokens counted, -1 if there are too many topics.
+template <class LogCount>
+__device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t row, int64_t g0, int32_t L, uint32_t* table,
+                                                  uint16_t* used, LogCount log_count)
 {
-    constexpr int kEach = SLOTS / 2 / TEAM;  // keys a thread may hold
-    const int32_t me = Team<TEAM>::rank(), lane = (int32_t)threadIdx.x % kWave;
-    const uint64_t below = (1ull << lane) - 1;
+    constexpr int32_t kSlots = 2 * kWaveTopics, kEach = kWaveTopics / kWave, kAhead = 4;
+    const int32_t lane = (int32_t)threadIdx.x % kWave;
+    const int32_t* z = a.z + g0;
     int32_t n = 0, counted = 0;
-    if (TEAM > kWave) {
-        if (me == 0) *n_used = 0;
-        __syncthreads();  // and the table is empty
-    }
-    for (int32_t i0 = 0; i0 < L; i0 += TEAM) {
-        const int32_t i = i0 + me;
-        const int32_t t = i < L ? a.z[g0 + i] : -1;
-        bool open = t >= 0 && t < a.K;
-        counted += (int32_t)__popcll(__ballot(open));
-        const uint32_t inv = kInverted - (uint32_t)t;
-        uint32_t h = ((uint32_t)t * 0x9E3779B1u) >> (32 - __builtin_ctz(SLOTS));
-        int32_t mine = -1;
-        while (__ballot(open)) {  // at most half the slots are in use: every search ends
-            if (open) {
-                uint32_t v = table[h];
-                if (v == 0) v = atomicCAS(&table[h], 0u, (1u << kMixTopicBits) | inv);
-                if (v == 0) {
-                    mine = (int32_t)h;
-                    open = false;
-                } else if ((v & kInverted) == inv) {
-                    atomicAdd(&table[h], 1u << kMixTopicBits);
-                    open = false;
-                } else {
-                    h = (h + 1) & (SLOTS - 1);
+    int32_t next[kAhead];
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) next[e] = e * kWave + lane < L ? z[e * kWave + lane] : -1;
+    bool many = false;
+    for (int32_t i0 = 0; i0 < L && !many; i0 += kAhead * kWave) {
+        int32_t topic[kAhead];
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const int32_t i = i0 + (kAhead + e) * kWave + lane;
+            topic[e] = next[e];
+            next[e] = i < L ? z[i] : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            if (i0 + e * kWave >= L) break;
+            const uint32_t t = (uint32_t)topic[e];
+            bool open = t < (uint32_t)a.K;
+            counted += (int32_t)__popcll(__ballot(open));
+            const uint32_t inv = kInverted - t;
+            int32_t mine = -1;
+            if (a.K <= kSlots) {  // a slot a topic: no search
+                if (open) {
+                    const uint32_t before = atomicAdd(&table[t], 1u << kMixTopicBits);
+                    if (before == 0) mine = (int32_t)t;
+                }
+            } else {
+                uint32_t h = (t * 0x9E3779B1u) >> (32 - __builtin_ctz(kSlots));
+                while (__ballot(open)) {  // half the slots stay empty: every search ends
+                    if (open) {
+                        uint32_t v = table[h];
+                        if (v == 0) v = atomicCAS(&table[h], 0u, (1u << kMixTopicBits) | inv);
+                        if (v == 0) {
+                            mine = (int32_t)h;
+                            open = false;
+                        } else if ((v & kInverted) == inv) {
+                            atomicAdd(&table[h], 1u << kMixTopicBits);
+                            open = false;
+                        } else {
+                            h = (h + 1) & (kSlots - 1);
+                        }
+                    }
                 }
             }
+            const uint64_t fresh = __ballot(mine >= 0);
+            if (mine >= 0) used[n + (int32_t)__builtin_amdgcn_mbcnt_hi((uint32_t)(fresh >> 32),
+                                                                     __builtin_amdgcn_mbcnt_lo((uint32_t)fresh, 0u))] = (uint16_t)mine;
+            n += (int32_t)__popcll(fresh);
+            many = n > kWaveTopics - kWave && i0 + (e + 1) * kWave < L;
+            if (many) break;
         }
-        const uint64_t fresh = __ballot(mine >= 0);
-        int32_t at = n;
-        if (TEAM > kWave) {
-            if (lane == 0) at = atomicAdd(n_used, (int32_t)__popcll(fresh));
-            at = __shfl(at, 0, kWave);
-        }
-        if (mine >= 0) used[at + (int32_t)__popcll(fresh & below)] = (uint16_t)mine;
-        n += (int32_t)__popcll(fresh);
     }
-    counted = Team<TEAM>::sum(counted, part);
-    Team<TEAM>::order();
-    if (TEAM > kWave) {
-        n = *n_used;
-        __syncthreads();
-    }
-    // the keys, into registers and side by side in LDS; the table is cleared behind them
+    wave_lds_order();
+    // the keys, into registers; the table is cleared behind them
     uint32_t key[kEach];
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-        const int32_t i = e * TEAM + me;
+        const int32_t i = e * kWave + lane;
         key[e] = 0;
-        if (e * TEAM < n && i < n) {
+        if (e * kWave < n && i < n) {
             const uint32_t h = used[i];
             key[e] = table[h];
+            if (a.K <= kSlots) key[e] |= kInverted - h;
             table[h] = 0;
         }
     }
+    if (many) {
+        wave_lds_order();
+        return -1;
+    }
     int32_t n_best = n;
     uint32_t least = 1;
-    if (n > (TEAM == kWave ? 2 * kWave : 8 * kWave) && n > a.k) {
-        // too many to rank them all: the smallest of the best k first, bit by bit
+    if (n > kWave && n > a.k) {
+        // too many to rank them all: a border below which lie all but k, bit by bit
         least = 0;
-        for (int bit = 31 - __builtin_clz((uint32_t)L) + (int)kMixTopicBits; bit >= 0; --bit) {
-            const uint32_t at = least | (1u << bit);
-            int32_t above = 0;
+        const int top = 31 - __builtin_clz((uint32_t)L) + (int)kMixTopicBits;
+        if (n <= 2 * kWave) {  // most documents
+            for (int bit = top; bit >= 0; --bit) {
+                const uint32_t at = least | (1u << bit);
+                const int32_t above = (int32_t)__popcll(__ballot(key[0] >= at)) + (int32_t)__popcll(__ballot(key[1] >= at));
+                if (above >= a.k) least = at;
+                if (above == a.k) break;
+            }
+        } else {
+            for (int bit = top; bit >= 0; --bit) {
+                const uint32_t at = least | (1u << bit);
+                int32_t above = 0;
 #pragma unroll
-            for (int e = 0; e < kEach; ++e)
-                if (e * TEAM < n) above += (int32_t)__popcll(__ballot(key[e] >= at));
-            if (Team<TEAM>::sum(above, part) >= a.k) least = at;
+                for (int e = 0; e < kEach; ++e) above += (int32_t)__popcll(__ballot(key[e] >= at));
+                if (above >= a.k) least = at;
+                if (above == a.k) break;
+            }
         }
         n_best = a.k;
     }
-    if (TEAM > kWave) {
-        if (me == 0) *n_used = 0;
-        __syncthreads();
-    }
+    // those side by side, in the table's room
+    wave_lds_order();
+    uint32_t* keys = table;
     int32_t at = 0;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-        if (e * TEAM >= n) continue;
+        if (e * kWave >= n) continue;
         const bool in = key[e] >= least;
         const uint64_t some = __ballot(in);
-        if (TEAM > kWave) {
-            if (lane == 0) at = atomicAdd(n_used, (int32_t)__popcll(some));
-            at = __shfl(at, 0, kWave);
-        }
-        if (in) keys[at + (int32_t)__popcll(some & below)] = key[e];
+        if (in) keys[at + (int32_t)__builtin_amdgcn_mbcnt_hi((uint32_t)(some >> 32),
+                                                             __builtin_amdgcn_mbcnt_lo((uint32_t)some, 0u))] = key[e];
         at += (int32_t)__popcll(some);
     }
-    // up to a whole number of vectors
-    if (me < 4) keys[n_best + me] = 0;
-    Team<TEAM>::order();
+    wave_lds_order();
+    // (what lies behind them, up to a whole vector, is 0: no key is smaller)
     const uint4* four = reinterpret_cast<const uint4*>(keys);
-    for (int32_t i = me; i < n_best; i += TEAM) {
+    int32_t* const ids = a.ids + row * a.k;
+    float* const logits = a.logits + row * a.k;
+    for (int32_t i = lane; i < n_best; i += kWave) {
         const uint32_t own = keys[i];
         int32_t place = 0;
         for (int32_t j = 0; j < (n_best + 3) / 4; ++j) {
@@ -180,46 +184,48 @@ __device__ __forceinline__ int32_t topics_by_table(const TopicArgs& a, int64_t r
             place += (v.x > own) + (v.y > own) + (v.z > own) + (v.w > own);
         }
         if (place < a.k) {
-            a.ids[row * a.k + place] = (int32_t)(kInverted - (own & kInverted));
-            a.logits[row * a.k + place] = log_count((int32_t)(own >> kMixTopicBits));
+            ids[place] = (int32_t)(kInverted - (own & kInverted));
+            logits[place] = log_count((int32_t)(own >> kMixTopicBits));
         }
     }
-    for (int32_t i = n_best + me; i < a.k; i += TEAM) {
-        a.ids[row * a.k + i] = -1;
-        a.logits[row * a.k + i] = -INFINITY;
+    for (int32_t i = n_best + lane; i < a.k; i += kWave) {
+        ids[i] = -1;
+        logits[i] = -INFINITY;
     }
-    Team<TEAM>::order();
+    wave_lds_order();
+    for (int32_t i = lane; i < n_best; i += kWave) keys[i] = 0;
+    wave_lds_order();
     return counted;
 }
 
 __global__ __launch_bounds__(kWaveBlock) void wave_topics_kernel(TopicArgs a)
 {
-    constexpr int kWaves = kWaveBlock / kWave, kSlots = 2 * kWaveTokens;
-    __shared__ __align__(16) uint32_t table[kWaves][kSlots];
-    __shared__ __align__(16) uint32_t keys[kWaves][kWaveTokens + 4];
-    __shared__ uint16_t used[kWaves][kWaveTokens];
-    __shared__ float log_of[kWaveTokens + 1];  // of count + alpha
+    constexpr int kWaves = kWaveBlock / kWave;
+    __shared__ __align__(16) uint32_t table[kWaves][2 * kWaveTopics];
+    __shared__ uint16_t used[kWaves][kWaveTopics];
+    __shared__ float log_of[kWaveTopics + 1];  // of count + alpha
     const int32_t tid = (int32_t)threadIdx.x, wave = tid / kWave, lane = tid % kWave;
-    for (int32_t i = tid; i < kWaves * kSlots; i += kWaveBlock) (&table[0][0])[i] = 0;
-    for (int32_t i = tid; i <= kWaveTokens; i += kWaveBlock) log_of[i] = (float)log((double)i + a.alpha);
+    for (int32_t i = tid; i < kWaves * 2 * kWaveTopics; i += kWaveBlock) (&table[0][0])[i] = 0;
+    for (int32_t i = tid; i <= kWaveTopics; i += kWaveBlock) log_of[i] = (float)log((double)i + a.alpha);
     __syncthreads();
     const double k_alpha = (double)a.K * a.alpha;
     for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < a.rows; row += (int64_t)gridDim.x * kWaves) {
         int64_t g0, g1;
         document_of(a, row, g0, g1);
         if (g1 - g0 > kWaveTokens) continue;
-        const int32_t counted = topics_by_table<kWave, kSlots>(a, row, g0, (int32_t)(g1 - g0), table[wave], keys[wave],
-                                                               used[wave], nullptr, nullptr,
-                                                               [&](int32_t n) { return log_of[n]; });
-        if (lane == 0 && a.log_norm) a.log_norm[row] = (float)log((double)counted + k_alpha);
+        const int32_t counted = topics_by_wave(a, row, g0, (int32_t)(g1 - g0), table[wave], used[wave], [&](int32_t n) {
+            return n <= kWaveTopics ? log_of[n] : (float)log((double)n + a.alpha);
+        });
+        if (lane != 0) continue;
+        if (counted < 0) a.ids[row * a.k] = kUnfinished;
+        else if (a.log_norm) a.log_norm[row] = (float)log((double)counted + k_alpha);
     }
 }
 
-// The rows of this workgroup whose documents have lo .. hi tokens: every gridDim.x-th row is this
-// workgroup's, BLOCK of them are looked at together.  f(row, g0, L) is called for one after the other.
+// The rows of this workgroup that the waves left: every gridDim.x-th row is this workgroup's, BLOCK of
+// them are looked at together.  f(row, g0, L) is called for one after the other.
 template <int BLOCK, class F>
-__device__ __forceinline__ void for_rows_of_length(const TopicArgs& a, int32_t lo, int32_t hi, int32_t* mine, int32_t* n_mine,
-                                                   F f)
+__device__ __forceinline__ void for_rows_left(const TopicArgs& a, int32_t* mine, int32_t* n_mine, F f)
 {
     for (int64_t r0 = blockIdx.x; r0 < a.rows; r0 += (int64_t)gridDim.x * BLOCK) {
         __syncthreads();
@@ -229,7 +235,7 @@ __device__ __forceinline__ void for_rows_of_length(const TopicArgs& a, int32_t l
         if (row < a.rows) {
             int64_t g0, g1;
             document_of(a, row, g0, g1);
-            if (g1 - g0 >= lo && g1 - g0 <= hi) mine[atomicAdd(n_mine, 1)] = (int32_t)threadIdx.x;
+            if (g1 - g0 > kWaveTokens || (g1 - g0 > kWaveTopics && a.ids[row * a.k] == kUnfinished)) mine[atomicAdd(n_mine, 1)] = (int32_t)threadIdx.x;
         }
         __syncthreads();
         const int32_t n = *n_mine;
@@ -272,9 +278,9 @@ __device__ __forceinline__ int32_t block_prefix(int32_t v, int32_t* part, int32_
 }
 
 struct TableLds {
-    uint32_t table[2 * (kTableTokens + 1)];
-    uint32_t keys[kTableTokens + 5];
-    uint16_t used[kTableTokens + 1];
+    uint32_t topic[kTableSlots];  // kInverted: empty
+    uint32_t count[kTableSlots];
+    uint16_t used[kTableTopics];
 };
 struct LongLds {
     union {
@@ -286,152 +292,404 @@ struct LongLds {
     uint32_t histogram[1 << kDigit];
     int32_t mine[kLongBlock];
     int32_t part[kLongBlock / kWave];
-    int32_t n_mine, n_keys, digit, over;
+    int32_t n_mine, n_keys, n_used, digit, over;
 };
 static_assert(sizeof(LongLds) <= 160 * 1024, "LDS of a CU");
+
+// The `need`-th largest of the workgroup's values (all below 2^most_bits, need of them or more), and
+// how many values equal to it are among the `need` largest.  each(f) calls f(value) for the thread's own.
+template <class Each>
+__device__ __forceinline__ uint32_t nth_largest(LongLds& lds, int32_t most_bits, int32_t& need, Each each)
+{
+    const int32_t tid = (int32_t)threadIdx.x;
+    int32_t shift = max(0, most_bits - kDigit), bits = most_bits - shift;
+    uint32_t prefix = 0;
+    bool first = true;
+    for (;;) {
+        __syncthreads();
+        for (int32_t i = tid; i < 1 << kDigit; i += kLongBlock) lds.histogram[i] = 0;
+        __syncthreads();
+        each([&](uint32_t v) {
+            const bool in = first || (v >> (shift + bits)) == prefix;
+            const uint32_t digit = (v >> shift) & ((1u << bits) - 1u);
+            // most counts are small: the wave's 0s and 1s are added up first
+            const uint64_t zeros = __ballot(in && digit == 0), ones = __ballot(in && digit == 1);
+            const int32_t leader = (int32_t)__builtin_ctzll(__ballot(true));
+            if ((int32_t)(threadIdx.x % kWave) == leader) {
+                if (zeros) atomicAdd(&lds.histogram[0], (uint32_t)__popcll(zeros));
+                if (ones) atomicAdd(&lds.histogram[1], (uint32_t)__popcll(ones));
+            }
+            if (in && digit > 1) atomicAdd(&lds.histogram[digit], 1u);
+        });
+        __syncthreads();
+        // digit d is the one when fewer than `need` lie above it and no fewer with its own
+        const int32_t d = (1 << kDigit) - 1 - tid;
+        const int32_t here = (int32_t)lds.histogram[d];
+        int32_t all;
+        const int32_t above = block_prefix<kLongBlock>(here, lds.part, all);
+        if (above < need && above + here >= need) {
+            lds.digit = d;
+            lds.over = above;
+        }
+        __syncthreads();
+        prefix = (prefix << bits) | (uint32_t)lds.digit;
+        need -= lds.over;
+        if (shift == 0) return prefix;
+        first = false;
+        bits = min(shift, kDigit);
+        shift -= bits;
+    }
+}
+static_assert(1 << kDigit == kLongBlock, "a thread a digit");
+
+__device__ __forceinline__ int32_t block_max(int32_t v, int32_t* part)
+{
+    v = wave_reduce(v, [](int32_t x, int32_t y) { return max(x, y); });
+    __syncthreads();
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+    __syncthreads();
+    for (int w = 0; w < kLongBlock / kWave; ++w) v = max(v, part[w]);
+    return v;
+}
+__device__ __forceinline__ int32_t bits_of(uint32_t v) { return v == 0 ? 1 : 32 - (int32_t)__builtin_clz(v); }
+
+// The n keys in order of size, the best k of them to `best`.  A key's place is the number of larger ones,
+// which some threads of a wave count together where there are few keys.
+__device__ __forceinline__ void order_keys(const uint64_t* keys, int32_t n, int32_t k, uint64_t* best)
+{
+    int32_t together = 1;
+    while (together < kWave && 2 * together * n <= kLongBlock) together *= 2;
+    const int32_t q = (int32_t)threadIdx.x % together;
+    for (int32_t i = (int32_t)threadIdx.x / together; i < n; i += kLongBlock / together) {
+        const uint64_t key = keys[i];
+        int32_t place = 0;
+#pragma unroll 4
+        for (int32_t j = q; j < n; j += together) place += keys[j] > key;
+        for (int32_t d = together / 2; d > 0; d /= 2) place += __shfl_xor(place, d, kWave);
+        if (q == 0 && place < k) best[place] = key;
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ void write_keys(const TopicArgs& a, int64_t row, const uint64_t* best, int32_t n, int32_t counted)
+{
+    for (int32_t i = (int32_t)threadIdx.x; i < a.k; i += kLongBlock) {
+        const uint64_t key = i < n ? best[i] : 0;
+        a.ids[row * a.k + i] = i < n ? (int32_t)(kInverted - (uint32_t)(key & kInverted)) : -1;
+        a.logits[row * a.k + i] = i < n ? (float)log((double)(key >> kMixTopicBits) + a.alpha) : -INFINITY;
+    }
+    if (threadIdx.x == 0 && a.log_norm) a.log_norm[row] = (float)log((double)counted + (double)a.K * a.alpha);
+}
+
+// A document's few frequent topics would have their lanes wait for each other at one counter in every
+// round.  A wave counts those that stand out among its first tokens in scalar registers.
+struct HotTopics {
+    static constexpr int kHot = 2;
+    int32_t topic[kHot], tokens[kHot];
+    __device__ __forceinline__ HotTopics(int32_t t, bool open)
+    {
+        uint64_t left = __ballot(open);
+#pragma unroll
+        for (int q = 0; q < kHot; ++q) {
+            topic[q] = -1;
+            tokens[q] = 0;
+            for (int tries = 0; tries < 4 && left; ++tries) {
+                const int32_t own = __builtin_amdgcn_readlane(t, (int)__builtin_ctzll(left));
+                const uint64_t same = __ballot(t == own);
+                left &= ~same;
+                if (__popcll(same) < 4) continue;
+                topic[q] = own;
+                break;
+            }
+        }
+    }
+    // what is left to count of a round's tokens
+    __device__ __forceinline__ bool left(int32_t t, bool open)
+    {
+#pragma unroll
+        for (int q = 0; q < kHot; ++q) {
+            const uint64_t same = __ballot(open && t == topic[q]);
+            tokens[q] += (int32_t)__popcll(same);
+            open = open && t != topic[q];
+        }
+        return open;
+    }
+};
+
+// Counts in buckets that keep their order: one each below 64, then 32 for every power of two
+__device__ __forceinline__ uint32_t bucket_of(uint32_t c)
+{
+    if (c < 64) return c;
+    const uint32_t e = 31 - (uint32_t)__builtin_clz(c);
+    return 64 + ((e - 6) << 5) + ((c >> (e - 5)) & 31u);
+}
+
+// The k-th largest count of more than k, and into `ties` how many of the topics that have it are among
+// the best k.  each(f) calls f(count) for the thread's share.
+template <class Each>
+__device__ __forceinline__ uint32_t least_count(LongLds& lds, int32_t k, int32_t& ties, Each each)
+{
+    ties = k;
+    const uint32_t bucket = nth_largest(lds, kDigit, ties, [&](auto f) { each([&](uint32_t c) { f(bucket_of(c)); }); });
+    if (bucket < 64) return bucket;
+    const int32_t bits = (int32_t)((bucket - 64) >> 5) + 1;  // of a count that its bucket leaves open
+    const uint32_t low = (32u + (bucket & 31u)) << bits;
+    return low + nth_largest(lds, bits, ties, [&](auto f) {
+               each([&](uint32_t c) {
+                   if (c - low < 1u << bits) f(c - low);
+               });
+           });
+}
+
+// The document's counts in a table; false, and nothing written, if it has too many topics for one
+__device__ __forceinline__ bool topics_by_table(const TopicArgs& a, int64_t row, int64_t g0, int32_t L, LongLds& lds)
+{
+    constexpr int kLoads = 8;
+    const int32_t tid = (int32_t)threadIdx.x, lane = tid % kWave;
+    const uint64_t below = (1ull << lane) - 1;
+    TableLds& table = lds.table;
+    __syncthreads();
+    for (int32_t i = tid; i < kTableSlots; i += kLongBlock) {
+        table.topic[i] = kInverted;
+        table.count[i] = 0;
+    }
+    if (tid == 0) lds.n_used = 0;
+    __syncthreads();
+    int32_t counted = 0;
+    int32_t next[kLoads];
+#pragma unroll
+    for (int e = 0; e < kLoads; ++e) next[e] = e * kLongBlock + tid < L ? a.z[g0 + e * kLongBlock + tid] : -1;
+    HotTopics hot(next[0], next[0] >= 0 && next[0] < a.K);
+    // n tokens of topic t, where open
+    const auto insert = [&](int32_t t, uint32_t tokens, bool open) {
+        uint32_t h = __umulhi((uint32_t)t * 0x9E3779B1u, (uint32_t)kTableSlots);
+        bool full = false;
+        while (__ballot(open)) {
+            bool mine = false;
+            if (open) {
+                uint32_t v = table.topic[h];
+                if (v == kInverted) {
+                    v = atomicCAS(&table.topic[h], kInverted, (uint32_t)t);
+                    mine = v == kInverted;
+                }
+                if (mine || v == (uint32_t)t) {
+                    atomicAdd(&table.count[h], tokens);
+                    open = false;
+                } else {
+                    h = h + 1 == (uint32_t)kTableSlots ? 0 : h + 1;
+                }
+            }
+            const uint64_t fresh = __ballot(mine);
+            if (fresh) {
+                int32_t at = 0;
+                if (lane == 0) at = atomicAdd(&lds.n_used, (int32_t)__popcll(fresh));
+                at = __builtin_amdgcn_readfirstlane(at);
+                const int32_t own = at + (int32_t)__popcll(fresh & below);
+                if (mine && own < kTableTopics) table.used[own] = (uint16_t)h;
+                // given up: a wave takes 64 slots at most after that
+                full = at + (int32_t)__popcll(fresh) > kTableTopics;
+                if (full) break;
+            }
+        }
+        return full;
+    };
+    bool full = false;
+    for (int64_t i0 = 0; i0 < L && !full; i0 += kLoads * kLongBlock) {
+        int32_t topic[kLoads];
+#pragma unroll
+        for (int e = 0; e < kLoads; ++e) {
+            const int64_t i = i0 + (e + kLoads) * kLongBlock + tid;
+            topic[e] = next[e];
+            next[e] = i < L ? a.z[g0 + i] : -1;
+        }
+#pragma unroll
+        for (int e = 0; e < kLoads; ++e) {
+            const int32_t t = topic[e];
+            if (i0 + e * kLongBlock >= L || full) break;
+            const bool open = t >= 0 && t < a.K;
+            counted += open;
+            full = insert(t, 1u, hot.left(t, open));
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < HotTopics::kHot; ++q)
+        if (hot.tokens[q] > 0) full = insert(hot.topic[q], (uint32_t)hot.tokens[q], lane == 0) || full;
+    counted = block_sum<kLongBlock>(counted, lds.part);
+    const int32_t n = lds.n_used;
+    if (n > kTableTopics) return false;
+    uint32_t least = 1, after = 0;  // of the topics with the least count, those whose inverse is at least `after`
+    const auto each = [&](auto f) {
+        for (int32_t i = tid; i < n; i += kLongBlock) {
+            const uint32_t h = table.used[i];
+            f(table.count[h], table.topic[h]);
+        }
+    };
+    if (n > a.k) {
+        int32_t ties;
+        least = least_count(lds, a.k, ties, [&](auto f) { each([&](uint32_t c, uint32_t) { f(c); }); });
+        after = nth_largest(lds, (int32_t)kMixTopicBits, ties, [&](auto f) {
+            each([&](uint32_t c, uint32_t t) {
+                if (c == least) f(kInverted - t);
+            });
+        });
+    }
+    __syncthreads();
+    if (tid == 0) lds.n_keys = 0;
+    __syncthreads();
+    each([&](uint32_t c, uint32_t t) {
+        if (c > least || (c == least && kInverted - t >= after)) lds.keys[atomicAdd(&lds.n_keys, 1)] = long_key(c, (int32_t)t);
+    });
+    __syncthreads();
+    const int32_t n_best = min(n, a.k);
+    order_keys(lds.keys, n_best, a.k, lds.best);
+    write_keys(a, row, lds.best, n_best, counted);
+    return true;
+}
 
 // Counters are 16-bit for documents of less than 2^16 tokens (twice the topics a range), else 32-bit.
 template <bool WIDE>
 __device__ __forceinline__ void topics_by_counters(const TopicArgs& a, int64_t row, int64_t g0, int32_t L, LongLds& lds)
 {
-    constexpr int32_t kRange = (WIDE ? 1 : 2) * kLongWords * kLongBlock, kPer = WIDE ? 1 : 2;
+    constexpr int32_t kPer = WIDE ? 1 : 2, kRange = kPer * kLongWords * kLongBlock;
+    constexpr int kLoads = 2;
     const int32_t tid = (int32_t)threadIdx.x;
-    uint32_t* own = lds.count + tid * kLongWords;  // topics [tid * kLongWords * kPer, ..) of the range
-    // f(count, topic of the range) for the thread's own topics in ascending order
-    auto each = [&](auto f) {
-#pragma unroll 1
-        for (int32_t j = 0; j < kLongWords; ++j) {
-            const uint32_t w = own[j];
-            if (w == 0) continue;
-            const int32_t t = (tid * kLongWords + j) * kPer;
-            if (WIDE) {
-                f(w, t);
-            } else {
-                if (w & 0xFFFFu) f(w & 0xFFFFu, t);
-                if (w >> 16) f(w >> 16, t + 1);
-            }
-        }
-    };
+    const int32_t* const z = a.z + g0;
     int32_t n_best = 0, counted = 0;
     for (int32_t t0 = 0; t0 < a.K; t0 += kRange) {
         const int32_t nt = min(kRange, a.K - t0);
+        // words of a thread, an odd number for their banks; topics [tid * each * kPer, ..) of the range
+        const int32_t each_words = ((nt + kPer - 1) / kPer + kLongBlock - 1) / kLongBlock | 1;
+        uint32_t* const own = lds.count + tid * each_words;
+        // f(count, topic of the range) for the thread's own topics in ascending order
+        const auto each = [&](auto f) {
+#pragma unroll 1
+            for (int32_t j = 0; j < each_words; ++j) {
+                const uint32_t w = own[j];
+                if (w == 0) continue;
+                const int32_t t = (tid * each_words + j) * kPer;
+                if (WIDE) {
+                    f(w, t);
+                } else {
+                    if (w & 0xFFFFu) f(w & 0xFFFFu, t);
+                    if (w >> 16) f(w >> 16, t + 1);
+                }
+            }
+        };
+        // four neighbours a load
+        int4 next[kLoads];
+        const auto load = [&](int32_t i0, int32_t e) {
+            const int64_t i = (int64_t)i0 + (e * kLongBlock + tid) * 4;
+            int4 v;
+            if (i + 4 <= L) {
+                __builtin_memcpy(&v, z + i, 16);
+            } else {
+                v.x = i < L ? z[i] : -1;
+                v.y = i + 1 < L ? z[i + 1] : -1;
+                v.z = i + 2 < L ? z[i + 2] : -1;
+                v.w = -1;
+            }
+            return v;
+        };
+#pragma unroll
+        for (int e = 0; e < kLoads; ++e) next[e] = load(0, e);
         __syncthreads();
-        for (int32_t i = tid; i < kLongWords * kLongBlock; i += kLongBlock) lds.count[i] = 0;
+        for (int32_t i = tid; i < each_words * kLongBlock; i += kLongBlock) lds.count[i] = 0;
         __syncthreads();
-        constexpr int kLoads = 16;  // in flight together
-        for (int64_t i0 = 0; i0 < L; i0 += kLoads * kLongBlock) {
-            int32_t t[kLoads];
+        const auto count = [&](uint32_t at, uint32_t tokens) {
+            if (WIDE) atomicAdd(&lds.count[at], tokens);
+            else atomicAdd(&lds.count[at / 2], tokens << (16 * (at & 1)));
+        };
+        HotTopics hot((int32_t)((uint32_t)next[0].x - (uint32_t)t0), (uint32_t)next[0].x - (uint32_t)t0 < (uint32_t)nt);
+        for (int64_t i0 = 0; i0 < L; i0 += kLoads * kLongBlock * 4) {
+            int4 topic[kLoads];
 #pragma unroll
             for (int e = 0; e < kLoads; ++e) {
-                const int64_t i = i0 + e * kLongBlock + tid;
-                t[e] = i < L ? a.z[g0 + i] : -1;
+                topic[e] = next[e];
+                if (i0 + kLoads * kLongBlock * 4 < L) next[e] = load((int32_t)(i0 + kLoads * kLongBlock * 4), e);
             }
 #pragma unroll
             for (int e = 0; e < kLoads; ++e) {
-                const uint32_t at = (uint32_t)t[e] - (uint32_t)t0;
-                if (t[e] < 0 || at >= (uint32_t)nt) continue;
-                if (WIDE) atomicAdd(&lds.count[at], 1u);
-                else atomicAdd(&lds.count[at / 2], 1u << (16 * (at & 1)));
+                const int32_t four[4] = {topic[e].x, topic[e].y, topic[e].z, topic[e].w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t at = (uint32_t)four[q] - (uint32_t)t0;  // (-1 and topics of other ranges lie beyond)
+                    const bool open = at < (uint32_t)nt;
+                    if (hot.left((int32_t)at, open)) count(at, 1u);
+                }
             }
         }
+#pragma unroll
+        for (int q = 0; q < HotTopics::kHot; ++q)
+            if (hot.tokens[q] > 0 && tid % kWave == 0) count((uint32_t)hot.topic[q], (uint32_t)hot.tokens[q]);
         __syncthreads();
-        int32_t some = 0, most = 0, tokens = 0;
+        int32_t some = 0;
         each([&](uint32_t c, int32_t) {
             ++some;
-            tokens += (int32_t)c;
-            most = max(most, (int32_t)c);
+            counted += (int32_t)c;
         });
-        some = block_sum<kLongBlock>(some, lds.part);
-        counted += block_sum<kLongBlock>(tokens, lds.part);
-        most = wave_reduce(most, [](int32_t x, int32_t y) { return max(x, y); });
-        __syncthreads();
-        if (tid % kWave == 0) lds.part[tid / kWave] = most;
-        __syncthreads();
-        for (int w = 0; w < kLongBlock / kWave; ++w) most = max(most, lds.part[w]);
-        // the smallest count among the best k of the range, digit by digit from the top, and how many of
-        // the topics that have just that count are among them
-        int32_t least = 1, ties = some;
-        if (some > a.k) {
-            int32_t need = a.k;   // of the topics whose count has the prefix found so far
-            int32_t shift = max(0, 32 - (int32_t)__builtin_clz((uint32_t)most) - kDigit), bits = 32 - shift;
-            uint32_t prefix = 0;
-            for (;;) {
-                __syncthreads();
-                for (int32_t i = tid; i < 1 << kDigit; i += kLongBlock) lds.histogram[i] = 0;
-                __syncthreads();
-                const uint32_t mask = (1u << min(bits, kDigit)) - 1u;
-                each([&](uint32_t c, int32_t) {
-                    const bool in = bits > kDigit ? true : ((uint64_t)c >> (shift + bits)) == prefix;
-                    if (in) atomicAdd(&lds.histogram[(c >> shift) & mask], 1u);
-                });
-                __syncthreads();
-                // digit d is the one when fewer than `need` lie above it and no fewer with its own
-                const int32_t d = (1 << kDigit) - 1 - tid;
-                const int32_t here = (int32_t)lds.histogram[d];
-                int32_t all;
-                const int32_t above = block_prefix<kLongBlock>(here, lds.part, all);
-                if (above < need && above + here >= need) {
-                    lds.digit = d;
-                    lds.over = above;
-                }
-                __syncthreads();
-                prefix = (prefix << min(bits, kDigit)) | (uint32_t)lds.digit;
-                need -= lds.over;
-                if (shift == 0) break;
-                bits = min(shift, kDigit);
-                shift -= bits;
+        int32_t all;
+        int32_t at = block_prefix<kLongBlock>(some, lds.part, all);
+        // the range's best to lds.keys, behind those of the ranges before; topics come in ascending order
+        const auto best_of = [&](auto each_topic) {
+            uint32_t least = 0;
+            int32_t ties = 0, equal = 0, before = 0, total;
+            if (all > a.k) {
+                least = least_count(lds, a.k, ties, [&](auto f) { each_topic([&](uint32_t c, int32_t) { f(c); }); });
+                each_topic([&](uint32_t c, int32_t) { equal += c == least; });
+                before = block_prefix<kLongBlock>(equal, lds.part, total);
             }
-            least = (int32_t)prefix;
-            ties = need;
+            __syncthreads();
+            if (tid == 0) lds.n_keys = n_best;
+            __syncthreads();
+            each_topic([&](uint32_t c, int32_t t) {
+                if (c > least || (c == least && before++ < ties)) lds.keys[atomicAdd(&lds.n_keys, 1)] = long_key(c, t);
+            });
+            __syncthreads();
+        };
+        if (all <= kListTopics) {
+            // the keys side by side in the counters' room
+            uint32_t word[kLongWords];
+#pragma unroll
+            for (int j = 0; j < kLongWords; ++j) word[j] = j < each_words ? own[j] : 0u;
+            __syncthreads();
+            uint2* const list = reinterpret_cast<uint2*>(lds.count);
+#pragma unroll
+            for (int j = 0; j < kLongWords; ++j) {
+                const int32_t t = t0 + (tid * each_words + j) * kPer;
+                const uint32_t low = WIDE ? word[j] : word[j] & 0xFFFFu, high = WIDE ? 0u : word[j] >> 16;
+                if (low) list[at++] = make_uint2((uint32_t)t, low);
+                if (high) list[at++] = make_uint2((uint32_t)t + 1u, high);
+            }
+            __syncthreads();
+            // a run of neighbours a thread: ties go to the first
+            const int32_t run = (all + kLongBlock - 1) / kLongBlock | 1;
+            const int32_t i0 = min(tid * run, all), i1 = min(i0 + run, all);
+            best_of([&](auto f) {
+                for (int32_t i = i0; i < i1; ++i) {
+                    const uint2 v = list[i];
+                    f(v.y, (int32_t)v.x);
+                }
+            });
+        } else {
+            best_of([&](auto f) { each([&](uint32_t c, int32_t t) { f(c, t0 + t); }); });
         }
-        // the range's best behind those of the ranges before: ties by their order
-        __syncthreads();
-        if (tid == 0) lds.n_keys = n_best;
-        int32_t equal = 0, all;
-        each([&](uint32_t c, int32_t) { equal += (int32_t)c == least; });
-        int32_t at = block_prefix<kLongBlock>(equal, lds.part, all);
-        each([&](uint32_t c, int32_t t) {
-            bool in = (int32_t)c > least;
-            if ((int32_t)c == least) in = at++ < ties;
-            if (in) lds.keys[atomicAdd(&lds.n_keys, 1)] = long_key(c, t0 + t);
-        });
-        __syncthreads();
-        // their places, and the best k of them in order
         const int32_t n = lds.n_keys;
-        for (int32_t i = tid; i < n; i += kLongBlock) {
-            const uint64_t key = lds.keys[i];
-            int32_t place = 0;
-            for (int32_t j = 0; j < n; ++j) place += lds.keys[j] > key;
-            if (place < a.k) lds.best[place] = key;
-        }
-        __syncthreads();
+        order_keys(lds.keys, n, a.k, lds.best);
         n_best = min(n, a.k);
         for (int32_t i = tid; i < n_best; i += kLongBlock) lds.keys[i] = lds.best[i];
     }
-    for (int32_t i = tid; i < a.k; i += kLongBlock) {
-        const uint64_t key = i < n_best ? lds.best[i] : 0;
-        a.ids[row * a.k + i] = i < n_best ? (int32_t)(kInverted - (uint32_t)(key & kInverted)) : -1;
-        a.logits[row * a.k + i] = i < n_best ? (float)log((double)(key >> kMixTopicBits) + a.alpha) : -INFINITY;
-    }
-    if (tid == 0 && a.log_norm) a.log_norm[row] = (float)log((double)counted + (double)a.K * a.alpha);
+    counted = block_sum<kLongBlock>(counted, lds.part);
+    write_keys(a, row, lds.best, n_best, counted);
 }
 
 __global__ __launch_bounds__(kLongBlock) void long_topics_kernel(TopicArgs a)
 {
     extern __shared__ __align__(16) unsigned char raw[];
     LongLds& lds = *reinterpret_cast<LongLds*>(raw);
-    for_rows_of_length<kLongBlock>(a, kWaveTokens + 1, INT32_MAX, lds.mine, &lds.n_mine,
-                                   [&](int64_t row, int64_t g0, int32_t L) {
-        if (L <= kTableTokens) {
-            constexpr int kSlots = 2 * (kTableTokens + 1);
-            TableLds& t = lds.table;
-            __syncthreads();
-            for (int32_t i = (int32_t)threadIdx.x; i < kSlots; i += kLongBlock) t.table[i] = 0;
-            const int32_t counted = topics_by_table<kLongBlock, kSlots>(
-                a, row, g0, L, t.table, t.keys, t.used, &lds.n_keys, lds.part,
-                [&](int32_t n) { return (float)log((double)n + a.alpha); });
-            if (threadIdx.x == 0 && a.log_norm) a.log_norm[row] = (float)log((double)counted + (double)a.K * a.alpha);
-        } else if (L < 65536) {
+    for_rows_left<kLongBlock>(a, lds.mine, &lds.n_mine, [&](int64_t row, int64_t g0, int32_t L) {
+        const int32_t range = (L < 65536 ? 2 : 1) * kLongWords * kLongBlock;
+        if (a.K > kFewRanges * range && topics_by_table(a, row, g0, L, lds)) return;
+        if (L < 65536) {
             topics_by_counters<false>(a, row, g0, L, lds);
         } else {
             topics_by_counters<true>(a, row, g0, L, lds);
@@ -447,8 +705,8 @@ static int launch_top_topics(lda_ctx* c, const TopicArgs& a, hipStream_t stream)
         return (unsigned)(n < most ? n : most);
     };
     // documents cannot be longer than all of z
-    wave_topics_kernel<<<grid(kWaveBlock / kWave, 256 * 5), kWaveBlock, 0, stream>>>(a);
-    if (a.tokens > kWaveTokens) {
+    wave_topics_kernel<<<grid(kWaveBlock / kWave, 256 * 7), kWaveBlock, 0, stream>>>(a);
+    if (a.tokens > kWaveTopics) {
         LDA_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(long_topics_kernel),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(LongLds)));
         long_topics_kernel<<<grid(1, 256), kLongBlock, sizeof(LongLds), stream>>>(a);
