@@ -6,8 +6,8 @@
 //   a wave, with a table of counts in LDS, takes documents of up to kWaveTokens tokens and kWaveTopics
 //     topics (all that have at most so many tokens, and most of the others);
 //   a workgroup of 1024 takes the rest, with a counter a topic in LDS, a range of topics at a time, and
-//     the best k chosen by histograms of the counts' digits.  In a very large K (more than
-//     kFewRanges ranges) a table comes first, which holds up to kTableTopics topics whatever K is.
+//     the best k chosen by histograms of the counts; or with a table, which holds up to kTableTopics topics
+//     whatever K is.
 // The first kernel leaves a mark in the rows that the second has to take.
 #include "rows.hpp"
 
@@ -23,8 +23,10 @@ constexpr int32_t kWaveTokens = 4095;    // the count of a 32-bit key has 12 bit
 constexpr int kLongBlock = 1024;
 constexpr int32_t kTableSlots = 12288, kTableTopics = 8192;
 constexpr int32_t kLongWords = 31;       // words of counters in LDS, a thread at most
-constexpr int32_t kFewRanges = 4;
-constexpr int32_t kListTopics = kLongWords * kLongBlock / 2;  // keys that fit the counters' room
+// Where a document's topics take several ranges, a table is the faster one up to so many tokens a range:
+// it takes some 15 us and 2.8 us per 1000 tokens whatever K is (8000 topics among 40 000 tokens), a
+// range of counters some 30 us and 0.2 us per 1000 tokens.
+constexpr int32_t kTableTokens = 4096;
 constexpr int32_t kDigit = 10;           // bits of a key that a histogram takes at a time
 
 struct TopicArgs {
@@ -627,13 +629,12 @@ __device__ __forceinline__ void topics_by_counters(const TopicArgs& a, int64_t r
             ++some;
             counted += (int32_t)c;
         });
-        int32_t all;
-        int32_t at = block_prefix<kLongBlock>(some, lds.part, all);
+        some = block_sum<kLongBlock>(some, lds.part);
         // the range's best to lds.keys, behind those of the ranges before; topics come in ascending order
         const auto best_of = [&](auto each_topic) {
             uint32_t least = 0;
             int32_t ties = 0, equal = 0, before = 0, total;
-            if (all > a.k) {
+            if (some > a.k) {
                 least = least_count(lds, a.k, ties, [&](auto f) { each_topic([&](uint32_t c, int32_t) { f(c); }); });
                 each_topic([&](uint32_t c, int32_t) { equal += c == least; });
                 before = block_prefix<kLongBlock>(equal, lds.part, total);
@@ -646,33 +647,7 @@ __device__ __forceinline__ void topics_by_counters(const TopicArgs& a, int64_t r
             });
             __syncthreads();
         };
-        if (all <= kListTopics) {
-            // the keys side by side in the counters' room
-            uint32_t word[kLongWords];
-#pragma unroll
-            for (int j = 0; j < kLongWords; ++j) word[j] = j < each_words ? own[j] : 0u;
-            __syncthreads();
-            uint2* const list = reinterpret_cast<uint2*>(lds.count);
-#pragma unroll
-            for (int j = 0; j < kLongWords; ++j) {
-                const int32_t t = t0 + (tid * each_words + j) * kPer;
-                const uint32_t low = WIDE ? word[j] : word[j] & 0xFFFFu, high = WIDE ? 0u : word[j] >> 16;
-                if (low) list[at++] = make_uint2((uint32_t)t, low);
-                if (high) list[at++] = make_uint2((uint32_t)t + 1u, high);
-            }
-            __syncthreads();
-            // a run of neighbours a thread: ties go to the first
-            const int32_t run = (all + kLongBlock - 1) / kLongBlock | 1;
-            const int32_t i0 = min(tid * run, all), i1 = min(i0 + run, all);
-            best_of([&](auto f) {
-                for (int32_t i = i0; i < i1; ++i) {
-                    const uint2 v = list[i];
-                    f(v.y, (int32_t)v.x);
-                }
-            });
-        } else {
-            best_of([&](auto f) { each([&](uint32_t c, int32_t t) { f(c, t0 + t); }); });
-        }
+        best_of([&](auto f) { each([&](uint32_t c, int32_t t) { f(c, t0 + t); }); });
         const int32_t n = lds.n_keys;
         order_keys(lds.keys, n, a.k, lds.best);
         n_best = min(n, a.k);
@@ -687,8 +662,8 @@ __global__ __launch_bounds__(kLongBlock) void long_topics_kernel(TopicArgs a)
     extern __shared__ __align__(16) unsigned char raw[];
     LongLds& lds = *reinterpret_cast<LongLds*>(raw);
     for_rows_left<kLongBlock>(a, lds.mine, &lds.n_mine, [&](int64_t row, int64_t g0, int32_t L) {
-        const int32_t range = (L < 65536 ? 2 : 1) * kLongWords * kLongBlock;
-        if (a.K > kFewRanges * range && topics_by_table(a, row, g0, L, lds)) return;
+        const int32_t range = (L < 65536 ? 2 : 1) * kLongWords * kLongBlock, ranges = (a.K + range - 1) / range;
+        if (ranges > 1 && L / kTableTokens < ranges && topics_by_table(a, row, g0, L, lds)) return;
         if (L < 65536) {
             topics_by_counters<false>(a, row, g0, L, lds);
         } else {
