@@ -29,11 +29,11 @@ struct RowPart {
     int32_t ninf, pad;
 };
 
-// What the slots say: masses are exp(t / T - z), their sum, sum p log p; the floor of the other
-// classes and their number.
+// What the slots say: masses are exp(t / T - z), their sum; the floor of the other classes and their
+// number.
 struct TeacherPart {
-    double mass, entropy, z, floor;
-    int32_t others, pad[3];
+    double mass, z, floor;
+    int32_t others, pad;
 };
 
 // A row's softmax and teacher, all that its gradient needs
@@ -83,11 +83,9 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2, flo
 }
 __device__ __forceinline__ void wave_join(float& m, float& s, float c)
 {
-#pragma unroll
-    for (int d = kWave / 2; d > 0; d >>= 1) {
-        const float m2 = __shfl_xor(m, d, kWave), s2 = __shfl_xor(s, d, kWave);
-        join(m, s, m2, s2, c);
-    }
+    const float top = wave_max(m);
+    s = wave_sum(s * exp_above(m, base_of(top), c));
+    m = top;
 }
 template <int BLOCK>
 __device__ __forceinline__ void block_join(float& m, float& s, float c, float2* part)
@@ -169,64 +167,68 @@ struct Running {
     }
 };
 
-// ids [k] and masses [k] of a row in LDS; head: TeacherPart of the row
+// A row's slots in LDS
 struct Slots {
     TeacherPart* head;
     int32_t* id;  // -1: empty
-    float* p;     // the slot's mass, then the mass of its class (all its slots)
-    float* x;     // the student's logit
+    float* p;     // mass of the slot
+    float* t;     // the teacher's logit
+    float* x;     // the student's
     __device__ __forceinline__ Slots(unsigned char* lds, int32_t k)
     {
+        const int32_t n = (k + 3) / 4 * 4;
         head = reinterpret_cast<TeacherPart*>(lds);
         id = reinterpret_cast<int32_t*>(lds + sizeof(TeacherPart));
-        p = reinterpret_cast<float*>(id + (k + 3) / 4 * 4);
-        x = p + (k + 3) / 4 * 4;
+        p = reinterpret_cast<float*>(id + n);
+        t = p + n;
+        x = t + n;
     }
 };
-inline size_t slots_lds(int32_t k) { return sizeof(TeacherPart) + 12 * ((size_t)(k + 3) / 4 * 4); }
+static_assert(sizeof(TeacherPart) % 16 == 0, "vectors behind it");
+inline size_t slots_lds(int32_t k) { return sizeof(TeacherPart) + 16 * ((size_t)(k + 3) / 4 * 4); }
 
-__device__ __forceinline__ int32_t slot_id(const DistillArgs& a, int64_t row, int32_t j)
-{
-    const int64_t id = index_at(a.ids, a.ids_type, row * a.ids_stride + j);
-    return id >= 0 && id < a.V ? (int32_t)id : -1;
-}
-
-// One wave's work: ids, masses, their sum and entropy.
-__device__ __forceinline__ void read_teacher(const DistillArgs& a, int64_t row, const Slots& slots)
+// One wave's work: ids, logits of both sides and masses of a row's slots.
+template <class T>
+__device__ __forceinline__ void read_teacher(const DistillArgs& a, int64_t row, const T* logits, const Slots& slots)
 {
     const int lane = threadIdx.x % kWave;
     const double inv_t = 1.0 / (double)a.T;
     float top = -INFINITY;
+    double z = a.log_norm ? (double)a.log_norm[row] : 0.0;
     for (int32_t j = lane; j < (a.k + 3) / 4 * 4; j += kWave) {
-        const int32_t id = j < a.k ? slot_id(a, row, j) : -1;
-        const float t = id >= 0 ? element_at(a.teacher, a.teacher_type, row * a.teacher_stride + j) : -INFINITY;
+        int32_t id = -1;
+        float t = -INFINITY;
+        if (j < a.k) {
+            const int64_t at = index_at(a.ids, a.ids_type, row * a.ids_stride + j);
+            t = element_at(a.teacher, a.teacher_type, row * a.teacher_stride + j);
+            if (at >= 0 && at < a.V) id = (int32_t)at;
+            else t = -INFINITY;
+        }
         slots.id[j] = id;
-        slots.p[j] = t;
+        slots.t[j] = t;
+        slots.x[j] = id >= 0 ? Row<T>::one(logits + id) : 0.0f;
         top = fmaxf(top, t);
     }
-    double z;
+    double mass;
     if (a.log_norm) {
-        z = (double)a.log_norm[row];
+        mass = 0.0;
+        for (int32_t j = lane; j < (a.k + 3) / 4 * 4; j += kWave) {
+            const double p = exp((double)slots.t[j] * inv_t - z);
+            slots.p[j] = (float)p;
+            mass += p;
+        }
+        mass = wave_sum(mass);
     } else {
-        top = wave_reduce(top, [](float x, float y) { return fmaxf(x, y); });
-        z = (double)base_of(top) * inv_t;
+        top = base_of(wave_max(top));
         double sum = 0.0;
-        for (int32_t j = lane; j < a.k; j += kWave) sum += exp((double)slots.p[j] * inv_t - z);
+        for (int32_t j = lane; j < a.k; j += kWave) sum += exp(((double)slots.t[j] - (double)top) * inv_t);
         sum = wave_sum(sum);
-        z += sum == 0.0 ? 0.0 : log(sum);
+        z = (double)top * inv_t + (sum == 0.0 ? 0.0 : log(sum));
+        for (int32_t j = lane; j < (a.k + 3) / 4 * 4; j += kWave) slots.p[j] = (float)exp((double)slots.t[j] * inv_t - z);
+        mass = sum == 0.0 ? 0.0 : sum / sum;  // 1, or what is not a number
     }
-    double mass = 0.0, entropy = 0.0;
-    for (int32_t j = lane; j < a.k; j += kWave) {
-        const double log_p = (double)slots.p[j] * inv_t - z, p = exp(log_p);
-        slots.p[j] = (float)p;
-        mass += p;
-        if (p != 0.0) entropy += p * log_p;
-    }
-    mass = wave_sum(mass);
-    entropy = wave_sum(entropy);
     if (lane == 0) {
         slots.head->mass = mass;
-        slots.head->entropy = entropy;
         slots.head->z = z;
     }
 }
@@ -279,32 +281,57 @@ __device__ __forceinline__ void store_chunk(T* g, const float (&x)[Row<T>::kChun
     __builtin_memcpy(g, &r, 16);  // from any element on: the hardware takes unaligned addresses
 }
 
-// The loss from its sums over the slots, by one thread
+// A thread's share of a row's loss: sum of p (log p - log q) over the slots; and where there is a floor, what
+// lies beside them: c S over the finite logits, and how many are -infinity.
 struct LossSums {
-    double cross = 0.0, named_sum = 0.0;  // sum p log q; c S over the finite logits of named classes
-    int32_t named = 0, named_inf = 0, infinite = 0;
+    double slots, beside;
+    int32_t ninf;
+
+    __device__ __forceinline__ void add_slot(float p, float t, float x, double z, double base, double inv_t, double log_s)
+    {
+        if (p == 0.0f) return;
+        const double log_q = x == -INFINITY ? -(double)INFINITY : ((double)x - base) * inv_t - log_s;
+        slots += (double)p * ((double)t * inv_t - z - log_q);
+    }
+    __device__ __forceinline__ void leave_out(float x, float c)  // a named class
+    {
+        if (x == -INFINITY) --ninf;
+        else beside -= (double)x * (double)c;
+    }
+    template <bool REST, int BLOCK>
+    __device__ __forceinline__ void sum(LossSums* part)
+    {
+        slots = wave_sum(slots);
+        if (REST) {
+            beside = wave_sum(beside);
+            ninf = wave_sum(ninf);
+        }
+        if (BLOCK == kWave) return;
+        __syncthreads();
+        if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = *this;
+        __syncthreads();
+        if (threadIdx.x != 0) return;  // one thread writes the loss
+#pragma unroll 1
+        for (int w = 1; w < BLOCK / kWave; ++w) {
+            slots += part[w].slots;
+            if (REST) {
+                beside += part[w].beside;
+                ninf += part[w].ninf;
+            }
+        }
+    }
 };
 
-__device__ __forceinline__ void add_slot(LossSums& l, double p, float x, double base, double inv_t, double log_s)
-{
-    if (p == 0.0) return;
-    if (x == -INFINITY) l.infinite = 1;
-    else l.cross += p * (((double)x - base) * inv_t - log_s);
-}
-
 template <bool REST>
-__device__ __forceinline__ float loss_of(const DistillArgs& a, const LossSums& l, const TeacherPart& t, float m, float s,
-                                         double scaled_sum, int32_t ninf)
+__device__ __forceinline__ float loss_of(const DistillArgs& a, const LossSums& l, const TeacherPart& t, float m, float s, double log_s)
 {
-    const double T = (double)a.T, log_s = log((double)s), base = (double)base_of(m);
-    double rest = 0.0;
-    bool infinite = l.infinite != 0;
+    const double T = (double)a.T, base = (double)base_of(m);
+    double sum = l.slots;
     if (REST && t.floor > 0.0) {
-        const double beside = (scaled_sum - l.named_sum) / ((double)a.c * T) - (double)t.others * base / T;
-        rest = t.floor * ((double)t.others * (log(t.floor) + log_s) - beside);
-        infinite = infinite || ninf > l.named_inf;
+        const double beside = l.beside / ((double)a.c * T) - (double)t.others * base / T;
+        sum += l.ninf > 0 ? (double)INFINITY : t.floor * ((double)t.others * (log(t.floor) + log_s) - beside);
     }
-    double loss = infinite ? (double)INFINITY : T * T * (t.entropy - l.cross + rest);
+    double loss = T * T * sum;
     if (!(s == s) || !(t.mass == t.mass)) loss = (double)NAN;
     if (t.mass + t.floor * (double)t.others == 0.0) loss = 0.0;
     return (float)loss;
@@ -314,10 +341,12 @@ __device__ __forceinline__ float loss_of(const DistillArgs& a, const LossSums& l
 template <class T, bool REST, int BLOCK, int CHUNKS>
 __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
 {
-    constexpr int E = Row<T>::kChunk;
+    constexpr int E = Row<T>::kChunk, kSlotsEach = (kMostSlots + BLOCK - 1) / BLOCK;
+    // short rows are read before it is known whether they are left out: the weight's latency is theirs too
+    constexpr bool kEager = BLOCK * CHUNKS <= 1024;
     extern __shared__ __align__(16) unsigned char lds[];
     __shared__ float2 part2[BLOCK / kWave];
-    __shared__ double partd[BLOCK / kWave];
+    __shared__ LossSums parts[BLOCK / kWave];
     __shared__ int32_t parti[BLOCK / kWave];
     const Slots slots(lds, a.k);
     const int32_t tid = (int32_t)threadIdx.x;
@@ -325,20 +354,23 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
     const SplitRow<T> r(static_cast<const T*>(a.logits) + row * a.logits_stride, a.V);
     T* const g = static_cast<T*>(a.grad) + row * a.grad_stride;
     const float w = a.weight ? a.weight[row * a.weight_stride] : 1.0f;
-    bool out = a.grad && w == 0.0f;  // left out
-    float m = -INFINITY, s = 0.0f;
-    double scaled_sum = 0.0;
-    int32_t ninf = 0;
     uint4 raw[CHUNKS];
     float extra[1] = {-INFINITY};
-    if (!out) {
-        if (tid < kWave) read_teacher(a, row, slots);
+    const auto load = [&]() {
 #pragma unroll
         for (int j = 0; j < CHUNKS; ++j) {
             const int32_t i = j * BLOCK + tid;
             if (i < r.whole) raw[j] = r.load(i);
         }
         if (tid < r.extras) extra[0] = Row<T>::one(r.p + r.extra(tid));
+    };
+    if (kEager) load();
+    bool out = a.grad && w == 0.0f;  // left out
+    float m = -INFINITY, s = 0.0f;
+    LossSums l{0.0, 0.0, 0};
+    if (!out) {
+        if (tid < kWave) read_teacher(a, row, r.p, slots);
+        if (!kEager) load();
         Running<T, REST> run;
 #pragma unroll
         for (int j = 0; j < CHUNKS; ++j) {
@@ -347,44 +379,38 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
                 Row<T>::unpack(raw[j], x);
                 run.add(x, a.c);
             }
-            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_sched_barrier(0);  // else all of the row is unpacked before it is used
         }
         if (tid < r.extras) run.add(extra, a.c);
         m = run.m;
         s = run.s;
+        l.beside = run.scaled_sum;
+        l.ninf = run.ninf;
         block_join<BLOCK>(m, s, a.c, part2);
-        if (REST) {
-            scaled_sum = block_sum<BLOCK>(run.scaled_sum, partd);
-            ninf = block_sum<BLOCK>(run.ninf, parti);
-        }
     }
     __syncthreads();
     TeacherPart t = *slots.head;
-    LossSums l;
-    float all[(kMostSlots + BLOCK - 1) / BLOCK];
-    if (!out) {
+    float all[kSlotsEach];
+    int32_t named = 0;
+    if (!out && (REST || a.grad)) {
 #pragma unroll
-        for (int q = 0; q < (kMostSlots + BLOCK - 1) / BLOCK; ++q) {
+        for (int q = 0; q < kSlotsEach; ++q) {
             const int32_t j = q * BLOCK + tid;
             all[q] = 0.0f;
             if (q * BLOCK >= a.k) continue;
             const int32_t id = j < a.k ? slots.id[j] : -1;
-            const float x = id >= 0 ? Row<T>::one(r.p + id) : 0.0f;
-            if (j < a.k) slots.x[j] = x;
-            if ((REST || a.grad) && id >= 0) {
-                const bool first = first_of_class(slots, a.k, j, id, all[q]);
-                if (REST && first) {
-                    ++l.named;
-                    if (x == -INFINITY) ++l.named_inf;
-                    else l.named_sum += (double)x * (double)a.c;
-                }
+            if (id < 0) continue;
+            const bool first = first_of_class(slots, a.k, j, id, all[q]);
+            if (REST && first) {
+                ++named;
+                l.leave_out(slots.x[j], a.c);
             }
         }
     }
     t.floor = 0.0;
     t.others = 0;
     if (REST) {
-        t.others = a.V - block_sum<BLOCK>(l.named, parti);
+        t.others = a.V - block_sum<BLOCK>(named, parti);
         t.floor = floor_of(t.mass, t.others);
     }
     const double mass = t.mass + t.floor * (double)t.others;
@@ -405,26 +431,22 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
         if (tid < r.extras) g[r.extra(tid)] = Row<T>::from(out ? 0.0f : f.dense(extra[0]));
         __syncthreads();  // the places of the slots are written again, by other threads
     }
-    const double inv_t = 1.0 / (double)a.T, base = (double)base_of(m), log_s = log((double)s);
+    const double log_s = log((double)s);
     if (!out) {
+        const double inv_t = 1.0 / (double)a.T, base = (double)base_of(m);
 #pragma unroll
-        for (int q = 0; q < (kMostSlots + BLOCK - 1) / BLOCK; ++q) {
+        for (int q = 0; q < kSlotsEach; ++q) {
             const int32_t j = q * BLOCK + tid;
             const int32_t id = j < a.k ? slots.id[j] : -1;
             if (id < 0) continue;
             const float x = slots.x[j];
-            add_slot(l, (double)slots.p[j], x, base, inv_t, log_s);
             if (a.grad) g[id] = Row<T>::from(f.slot(x, all[q]));
+            if (a.loss) l.add_slot(slots.p[j], slots.t[j], x, t.z, base, inv_t, log_s);
         }
     }
-    l.cross = block_sum<BLOCK>(l.cross, partd);
-    l.infinite = block_sum<BLOCK>(l.infinite, parti);
-    if (REST) {
-        l.named_sum = block_sum<BLOCK>(l.named_sum, partd);
-        l.named_inf = block_sum<BLOCK>(l.named_inf, parti);
-    }
+    l.sum<REST, BLOCK>(parts);
     if (tid == 0) {
-        a.loss[row] = out ? 0.0f : loss_of<REST>(a, l, t, m, s, scaled_sum, ninf);
+        a.loss[row] = out ? 0.0f : loss_of<REST>(a, l, t, m, s, log_s);
         if (a.stats)
             *reinterpret_cast<RowStats*>(a.stats + row * kStatFloats) = RowStats{m, s, (float)mass, (float)t.floor, t.z};
     }
@@ -444,7 +466,8 @@ __global__ __launch_bounds__(kPartBlock) void distill_part_kernel(DistillArgs a)
     const int64_t row = a.row0 + blockIdx.x;
     if (a.grad && a.weight && a.weight[row * a.weight_stride] == 0.0f) return;
     if (blockIdx.y == 0) {
-        if (tid < kWave) read_teacher(a, row, slots);
+        if (tid < kWave)
+            read_teacher(a, row, static_cast<const T*>(a.logits) + row * a.logits_stride, slots);
         __syncthreads();
         int32_t named = 0;
         if (REST) {
@@ -498,8 +521,7 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
 {
     constexpr int E = Row<T>::kChunk;
     extern __shared__ __align__(16) unsigned char lds[];
-    __shared__ double partd[kPartBlock / kWave];
-    __shared__ int32_t parti[kPartBlock / kWave];
+    __shared__ LossSums parts[kPartBlock / kWave];
     const Slots slots(lds, a.k);
     const int32_t tid = (int32_t)threadIdx.x, lane = tid % kWave;
     const double inv_t = 1.0 / (double)a.T;
@@ -532,7 +554,7 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
             wave_join(m, s, a.c);
             if (REST) {
                 scaled_sum = wave_sum(scaled_sum);
-                ninf = wave_reduce(ninf, [](int32_t x, int32_t y) { return x + y; });
+                ninf = wave_sum(ninf);
             }
             mass = (float)(t.mass + t.floor * (double)t.others);
             floor = (float)t.floor;
@@ -543,38 +565,40 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
     const Gradient f(m, s, mass, floor, w, a.T, a.c);
     if (!out) {
         for (int32_t j = tid; j < (a.k + 3) / 4 * 4; j += kPartBlock) {
-            const int32_t id = j < a.k ? slot_id(a, row, j) : -1;
-            double p = 0.0;
-            if (id >= 0) p = exp((double)element_at(a.teacher, a.teacher_type, row * a.teacher_stride + j) * inv_t - z);
+            int32_t id = -1;
+            float tl = -INFINITY;
+            if (j < a.k) {
+                const int64_t at = index_at(a.ids, a.ids_type, row * a.ids_stride + j);
+                tl = element_at(a.teacher, a.teacher_type, row * a.teacher_stride + j);
+                if (at >= 0 && at < a.V) id = (int32_t)at;
+            }
             slots.id[j] = id;
-            slots.p[j] = (float)p;
+            slots.t[j] = tl;
+            slots.p[j] = id >= 0 ? (float)exp((double)tl * inv_t - z) : 0.0f;
         }
         __syncthreads();
     }
     if (a.loss && blockIdx.y == 0) {
-        LossSums l;
+        LossSums l{0.0, 0.0, 0};
+        const double log_s = log((double)s);
         if (!out) {
-            const double base = (double)base_of(m), log_s = log((double)s);
+            const double base = (double)base_of(m);
+            if (REST && tid == 0) {
+                l.beside = scaled_sum;
+                l.ninf = ninf;
+            }
             for (int32_t j = tid; j < a.k; j += kPartBlock) {
                 const int32_t id = slots.id[j];
                 if (id < 0) continue;
                 const float x = Row<T>::one(r.p + id);
-                add_slot(l, (double)slots.p[j], x, base, inv_t, log_s);
+                l.add_slot(slots.p[j], slots.t[j], x, z, base, inv_t, log_s);
                 float all;
-                if (REST && first_of_class(slots, a.k, j, id, all)) {
-                    if (x == -INFINITY) ++l.named_inf;
-                    else l.named_sum += (double)x * (double)a.c;
-                }
+                if (REST && first_of_class(slots, a.k, j, id, all)) l.leave_out(x, a.c);
             }
         }
-        l.cross = block_sum<kPartBlock>(l.cross, partd);
-        l.infinite = block_sum<kPartBlock>(l.infinite, parti);
-        if (REST) {
-            l.named_sum = block_sum<kPartBlock>(l.named_sum, partd);
-            l.named_inf = block_sum<kPartBlock>(l.named_inf, parti);
-        }
+        l.sum<REST, kPartBlock>(parts);
         if (tid == 0) {
-            a.loss[row] = out ? 0.0f : loss_of<REST>(a, l, t, m, s, scaled_sum, ninf);
+            a.loss[row] = out ? 0.0f : loss_of<REST>(a, l, t, m, s, log_s);
             if (a.stats)
                 *reinterpret_cast<RowStats*>(a.stats + row * kStatFloats) = RowStats{m, s, mass, floor, z};
         }

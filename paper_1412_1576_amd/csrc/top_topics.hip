@@ -260,12 +260,7 @@ template <int BLOCK>
 __device__ __forceinline__ int32_t block_prefix(int32_t v, int32_t* part, int32_t& total)
 {
     const int32_t lane = (int32_t)threadIdx.x % kWave, wave = (int32_t)threadIdx.x / kWave;
-    int32_t sum = v;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const int32_t o = __shfl_up(sum, d, kWave);
-        if (lane >= d) sum += o;
-    }
+    const int32_t sum = wave_prefix(v);
     __syncthreads();
     if (lane == kWave - 1) part[wave] = sum;
     __syncthreads();

@@ -110,17 +110,6 @@ __device__ __forceinline__ void load_run(const T* p, int64_t v, int32_t V, float
     }
 }
 
-__device__ __forceinline__ double wave_prefix(double v)  // inclusive
-{
-    const int lane = threadIdx.x % kWave;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-        const double o = __shfl_up(v, d, kWave);
-        if (lane >= d) v += o;
-    }
-    return v;
-}
-
 // The draw among a thread's neighbours: the first of mass past the place, and the last of mass
 __device__ __forceinline__ void look_through(const double (&mass)[kEach], double run, double place, int32_t& hit, int32_t& last)
 {
@@ -283,9 +272,9 @@ __global__ __launch_bounds__(kWave) void verify_draw_kernel(VerifyArgs a)
             if (past) {
                 const int at = __builtin_ctzll(past);
                 segment = s0 + at;
-                before += __shfl(sum - own, at, kWave);
+                before += lane_value(sum - own, at);
             } else {
-                before += __shfl(sum, kWave - 1, kWave);
+                before += lane_value(sum, kWave - 1);
             }
         }
         const bool inside = segment >= 0;
