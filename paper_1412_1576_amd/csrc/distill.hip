@@ -672,22 +672,25 @@ static int32_t distill_slices(const lda_distill_rows* d)
     return (int32_t)(slices < 1 ? 1 : slices);
 }
 
-// Threads and chunks of a thread that hold a row in registers; 0: none do, or slices are better.
+// Threads and chunks of a thread that hold a row in registers; 0: slices instead.  A workgroup of 1024 has a
+// CU to itself, so that loss and gradient of one row take turns on it: a gradient gains by the one
+// read (4000 x 141043 bf16: 500 us, slices 730) unless too few rows fill the GPU (20000 f32: always; 49000 f32: 64 rows
+// 15.6 us, slices 15.0, 96 rows 16.5 and 19.0; 141043 bf16: 96 rows 28.5 and 23.1, 192 rows 31.7 and 38.8); the loss
+// alone is as fast in slices or faster (4000 x 141043: 264 us, slices 232; 64 rows: 15.6 and 10.7).
 struct RowShape {
-    int block, chunks;
+    int block, chunks, least_rows;
 };
-static RowShape row_shape(const lda_distill_rows* d)
+static RowShape row_shape(const lda_distill_rows* d, bool grad)
 {
-    static constexpr RowShape kShapes[] = {{64, 4}, {256, 4}, {256, 12}, {1024, 6}, {1024, 12}, {1024, 18}};
+    static constexpr RowShape kShapes[] = {{64, 4, 1}, {256, 4, 1}, {256, 12, 1}, {1024, 6, 1}, {1024, 12, 64}, {1024, 18, 128}};
     const int64_t chunk = 16 / (int64_t)type_bytes(d->logits_type);
     const int64_t whole = d->classes / chunk;
     for (const RowShape& shape : kShapes) {
         if (whole > (int64_t)shape.block * shape.chunks) continue;
-        const char* e = getenv("DROWS");
-        if (shape.block == 1024 && d->rows < (e ? atoi(e) : 128)) return {0, 0};
+        if (shape.block == 1024 && (!grad || d->rows < shape.least_rows)) break;
         return shape;
     }
-    return {0, 0};
+    return {0, 0, 0};
 }
 
 template <class T, bool REST>
@@ -717,7 +720,7 @@ static void launch_distill_typed(const DistillArgs& a, unsigned gx, RowShape sha
 
 static int64_t distill_bytes(const lda_distill_rows* d)
 {
-    if (d->rows == 0 || row_shape(d).block != 0) return 0;
+    if (d->rows == 0 || row_shape(d, false).block != 0) return 0;
     return d->rows * (distill_slices(d) * (int64_t)sizeof(RowPart) + (int64_t)sizeof(TeacherPart));
 }
 
@@ -751,7 +754,7 @@ static int launch_distill(const lda_distill_rows* d, const char* call, float* lo
     a.grad = grad;
     a.grad_stride = grad_stride;
     a.slices = distill_slices(d);
-    const RowShape shape = row_shape(d);
+    const RowShape shape = row_shape(d, grad != nullptr);
     if (shape.block == 0 && !stats_in) {
         const int64_t need = distill_bytes(d);
         if (!d->workspace || d->workspace_bytes < need || !aligned_to(d->workspace, 16))

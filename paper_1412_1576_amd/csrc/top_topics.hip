@@ -56,12 +56,15 @@ __device__ __forceinline__ void document_of(const TopicArgs& a, int64_t row, int
 }
 
 // One document's counts in a table of 2 kWaveTopics keys (0: empty), and its best k topics, by one wave.
-// `used` has room for kWaveTopics slots; the table is empty before and after.
+// `used` has room for kWaveTopics slots; the table is empty before and after.  A key has the topic, inverted
+// within the bits that K takes, below the count.
 // Returns the number of tokens counted, -1 if there are too many topics.
 template <class LogCount>
 __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t row, int64_t g0, int32_t L, uint32_t* table,
                                                   uint16_t* used, LogCount log_count)
 {
+    const uint32_t bits = 32u - (uint32_t)__builtin_clz((uint32_t)a.K);
+    const uint32_t inverted = (1u << bits) - 1u, one = 1u << bits;
     constexpr int32_t kSlots = 2 * kWaveTopics, kEach = kWaveTopics / kWave, kAhead = 4;
     const int32_t lane = (int32_t)threadIdx.x % kWave;
     const int32_t* z = a.z + g0;
@@ -84,11 +87,11 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
             const uint32_t t = (uint32_t)topic[e];
             bool open = t < (uint32_t)a.K;
             counted += (int32_t)__popcll(__ballot(open));
-            const uint32_t inv = kInverted - t;
+            const uint32_t inv = inverted - t;
             int32_t mine = -1;
             if (a.K <= kSlots) {  // a slot a topic: no search
                 if (open) {
-                    const uint32_t before = atomicAdd(&table[t], 1u << kMixTopicBits);
+                    const uint32_t before = atomicAdd(&table[t], one);
                     if (before == 0) mine = (int32_t)t;
                 }
             } else {
@@ -96,12 +99,12 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
                 while (__ballot(open)) {  // half the slots stay empty: every search ends
                     if (open) {
                         uint32_t v = table[h];
-                        if (v == 0) v = atomicCAS(&table[h], 0u, (1u << kMixTopicBits) | inv);
+                        if (v == 0) v = atomicCAS(&table[h], 0u, one | inv);
                         if (v == 0) {
                             mine = (int32_t)h;
                             open = false;
-                        } else if ((v & kInverted) == inv) {
-                            atomicAdd(&table[h], 1u << kMixTopicBits);
+                        } else if ((v & inverted) == inv) {
+                            atomicAdd(&table[h], one);
                             open = false;
                         } else {
                             h = (h + 1) & (kSlots - 1);
@@ -127,7 +130,7 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
         if (e * kWave < n && i < n) {
             const uint32_t h = used[i];
             key[e] = table[h];
-            if (a.K <= kSlots) key[e] |= kInverted - h;
+            if (a.K <= kSlots) key[e] |= inverted - h;
             table[h] = 0;
         }
     }
@@ -140,7 +143,7 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
     if (n > kWave && n > a.k) {
         // too many to rank them all: a border below which lie all but k, bit by bit
         least = 0;
-        const int top = 31 - __builtin_clz((uint32_t)L) + (int)kMixTopicBits;
+        const int top = 31 - __builtin_clz((uint32_t)L) + (int)bits;
         if (n <= 2 * kWave) {  // most documents
             for (int bit = top; bit >= 0; --bit) {
                 const uint32_t at = least | (1u << bit);
@@ -186,8 +189,8 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
             place += (v.x > own) + (v.y > own) + (v.z > own) + (v.w > own);
         }
         if (place < a.k) {
-            ids[place] = (int32_t)(kInverted - (own & kInverted));
-            logits[place] = log_count((int32_t)(own >> kMixTopicBits));
+            ids[place] = (int32_t)(inverted - (own & inverted));
+            logits[place] = log_count((int32_t)(own >> bits));
         }
     }
     for (int32_t i = n_best + lane; i < a.k; i += kWave) {
@@ -205,12 +208,16 @@ __global__ __launch_bounds__(kWaveBlock) void wave_topics_kernel(TopicArgs a)
     constexpr int kWaves = kWaveBlock / kWave;
     __shared__ __align__(16) uint32_t table[kWaves][2 * kWaveTopics];
     __shared__ uint16_t used[kWaves][kWaveTopics];
-    __shared__ float log_of[kWaveTopics + 1];  // of count + alpha
-    const int32_t tid = (int32_t)threadIdx.x, wave = tid / kWave, lane = tid % kWave;
+    __shared__ float log_of[kWaveTopics + 1], norm_of[kWaveTopics + 1];  // of count + alpha, of tokens + K alpha
+    const int32_t tid = (int32_t)threadIdx.x, lane = tid % kWave;
+    const int32_t wave = __builtin_amdgcn_readfirstlane(tid / kWave);  // what is a wave's is scalar
     for (int32_t i = tid; i < kWaves * 2 * kWaveTopics; i += kWaveBlock) (&table[0][0])[i] = 0;
-    for (int32_t i = tid; i <= kWaveTopics; i += kWaveBlock) log_of[i] = (float)log((double)i + a.alpha);
-    __syncthreads();
     const double k_alpha = (double)a.K * a.alpha;
+    for (int32_t i = tid; i <= kWaveTopics; i += kWaveBlock) {
+        log_of[i] = (float)log((double)i + a.alpha);
+        norm_of[i] = (float)log((double)i + k_alpha);
+    }
+    __syncthreads();
     for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < a.rows; row += (int64_t)gridDim.x * kWaves) {
         int64_t g0, g1;
         document_of(a, row, g0, g1);
@@ -220,7 +227,7 @@ __global__ __launch_bounds__(kWaveBlock) void wave_topics_kernel(TopicArgs a)
         });
         if (lane != 0) continue;
         if (counted < 0) a.ids[row * a.k] = kUnfinished;
-        else if (a.log_norm) a.log_norm[row] = (float)log((double)counted + k_alpha);
+        else if (a.log_norm) a.log_norm[row] = counted <= kWaveTopics ? norm_of[counted] : (float)log((double)counted + k_alpha);
     }
 }
 
