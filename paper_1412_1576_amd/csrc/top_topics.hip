@@ -57,21 +57,26 @@ __device__ __forceinline__ void document_of(const TopicArgs& a, int64_t row, int
 
 // One document's counts in a table of 2 kWaveTopics keys (0: empty), and its best k topics, by one wave.
 // `used` has room for kWaveTopics slots; the table is empty before and after.  A key has the topic, inverted
-// within the bits that K takes, below the count.
+// within the bits that K takes, below the count.  `next` holds the document's first tokens; all_read()
+// is called when they are read, for the next document's to be on their way while this one's topics are chosen.
 // Returns the number of tokens counted, -1 if there are too many topics.
-template <class LogCount>
-__device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t row, int64_t g0, int32_t L, uint32_t* table,
-                                                  uint16_t* used, LogCount log_count)
+constexpr int kAhead = 4;  // rounds of 64 tokens that are read ahead
+__device__ __forceinline__ void first_tokens(const int32_t* z, int32_t L, int32_t (&next)[kAhead])
+{
+    const int32_t lane = (int32_t)threadIdx.x % kWave;
+#pragma unroll
+    for (int e = 0; e < kAhead; ++e) next[e] = e * kWave + lane < L ? z[e * kWave + lane] : -1;
+}
+
+template <class Read, class LogCount>
+__device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t row, const int32_t* z, int32_t L, int32_t (&next)[kAhead],
+                                                  uint32_t* table, uint16_t* used, Read all_read, LogCount log_count)
 {
     const uint32_t bits = 32u - (uint32_t)__builtin_clz((uint32_t)a.K);
     const uint32_t inverted = (1u << bits) - 1u, one = 1u << bits;
-    constexpr int32_t kSlots = 2 * kWaveTopics, kEach = kWaveTopics / kWave, kAhead = 4;
+    constexpr int32_t kSlots = 2 * kWaveTopics, kEach = kWaveTopics / kWave;
     const int32_t lane = (int32_t)threadIdx.x % kWave;
-    const int32_t* z = a.z + g0;
     int32_t n = 0, counted = 0;
-    int32_t next[kAhead];
-#pragma unroll
-    for (int e = 0; e < kAhead; ++e) next[e] = e * kWave + lane < L ? z[e * kWave + lane] : -1;
     bool many = false;
     for (int32_t i0 = 0; i0 < L && !many; i0 += kAhead * kWave) {
         int32_t topic[kAhead];
@@ -120,6 +125,7 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
             if (many) break;
         }
     }
+    all_read();
     wave_lds_order();
     // the keys, into registers; the table is cleared behind them
     uint32_t key[kEach];
@@ -218,11 +224,24 @@ __global__ __launch_bounds__(kWaveBlock) void wave_topics_kernel(TopicArgs a)
         norm_of[i] = (float)log((double)i + k_alpha);
     }
     __syncthreads();
-    for (int64_t row = (int64_t)blockIdx.x * kWaves + wave; row < a.rows; row += (int64_t)gridDim.x * kWaves) {
-        int64_t g0, g1;
-        document_of(a, row, g0, g1);
-        if (g1 - g0 > kWaveTokens) continue;
-        const int32_t counted = topics_by_wave(a, row, g0, (int32_t)(g1 - g0), table[wave], used[wave], [&](int32_t n) {
+    const int64_t step = (int64_t)gridDim.x * kWaves;
+    int64_t row = (int64_t)blockIdx.x * kWaves + wave, g0 = 0, g1 = 0;
+    int32_t next[kAhead];
+    const auto tokens = [&]() { return g1 - g0 > kWaveTokens ? 0 : (int32_t)(g1 - g0); };
+    if (row < a.rows) document_of(a, row, g0, g1);
+    first_tokens(a.z + g0, tokens(), next);
+    for (; row < a.rows; row += step) {
+        const int32_t L = tokens();
+        const bool longer = g1 - g0 > kWaveTokens;
+        const int32_t* const z = a.z + g0;
+        g0 = g1 = 0;
+        if (row + step < a.rows) document_of(a, row + step, g0, g1);
+        const auto read_next = [&]() { first_tokens(a.z + g0, tokens(), next); };
+        if (longer) {
+            read_next();
+            continue;
+        }
+        const int32_t counted = topics_by_wave(a, row, z, L, next, table[wave], used[wave], read_next, [&](int32_t n) {
             return n <= kWaveTopics ? log_of[n] : (float)log((double)n + a.alpha);
         });
         if (lane != 0) continue;
@@ -682,7 +701,7 @@ static int launch_top_topics(lda_ctx* c, const TopicArgs& a, hipStream_t stream)
         return (unsigned)(n < most ? n : most);
     };
     // documents cannot be longer than all of z
-    wave_topics_kernel<<<grid(kWaveBlock / kWave, 256 * 7), kWaveBlock, 0, stream>>>(a);
+    wave_topics_kernel<<<grid(kWaveBlock / kWave, 256 * 6), kWaveBlock, 0, stream>>>(a);
     if (a.tokens > kWaveTopics) {
         LDA_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(long_topics_kernel),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(LongLds)));
