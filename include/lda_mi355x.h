@@ -383,9 +383,15 @@ typedef struct lda_topic_rows {
     int32_t slots;           /* 1 .. 1024 (more: LDA_ERR_UNSUPPORTED) */
     int32_t reserved_word;   /* must be zero */
     double alpha;            /* > 0 */
+    void* workspace;         /* NULL, or aligned to 16: with lda_topics_workspace() bytes documents of many tokens
+                                are shared by several workgroups; with less, fewer of them are, with
+                                the same results */
+    int64_t workspace_bytes;
     void* hip_stream;
     int32_t reserved[4];     /* must be zero */
 } lda_topic_rows;
+
+int64_t lda_topics_workspace(const lda_topic_rows* rows);
 
 /* ids [rows][slots], logits [rows][slots], log_norm [rows] or NULL */
 int lda_top_topics(const lda_topic_rows* rows, int32_t* ids, float* logits, float* log_norm);

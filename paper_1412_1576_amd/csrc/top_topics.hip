@@ -8,7 +8,9 @@
 //   a workgroup of 1024 takes the rest, with a counter a topic in LDS, a range of topics at a time, and
 //     the best k chosen by histograms of the counts; or with a table, which holds up to kTableTopics topics
 //     whatever K is.
-// The first kernel leaves a mark in the rows that the second has to take.
+//   Of the longest documents every range is a workgroup's, and their best are put together afterwards, where
+//     the caller has given a workspace for that.
+// The first kernel leaves marks in the rows that the others have to take.
 #include "rows.hpp"
 
 namespace lda {
@@ -16,6 +18,7 @@ namespace lda {
 constexpr int32_t kMostTopSlots = 1024;
 constexpr uint32_t kInverted = (1u << kMixTopicBits) - 1u;  // a key's topic is kInverted - (key & kInverted)
 constexpr int32_t kUnfinished = -2;      // in a row's first id, between the kernels
+constexpr int32_t kSplit = -3;           // the same; kSplit - i: place i of the workspace has its ranges
 
 constexpr int kWaveBlock = 256;          // four documents at a time
 constexpr int32_t kWaveTopics = 512;     // the table has twice as many slots
@@ -27,6 +30,11 @@ constexpr int32_t kLongWords = 31;       // words of counters in LDS, a thread a
 // it takes some 15 us and 2.8 us per 1000 tokens whatever K is (8000 topics among 40 000 tokens), a
 // range of counters some 30 us and 0.2 us per 1000 tokens.
 constexpr int32_t kTableTokens = 4096;
+constexpr int32_t kNarrowRange = 2 * kLongWords * kLongBlock;  // topics with 16-bit counters
+constexpr int32_t kWideRange = kLongWords * kLongBlock;
+constexpr int32_t kWideTokens = 65536;   // from here on 32-bit counters
+constexpr int32_t kSplitTokens = 16384;  // shorter documents are not split
+constexpr int64_t kSplitBytes = 64 << 20;  // of workspace at most
 constexpr int32_t kDigit = 10;           // bits of a key that a histogram takes at a time
 
 struct TopicArgs {
@@ -43,7 +51,26 @@ struct TopicArgs {
     int32_t* ids;
     float* logits;
     float* log_norm;
+    // documents that are split: how many, their rows; per document and range (topics, tokens) and the keys
+    int32_t places, ranges;  // 0 places: none is
+    int32_t* n_split;
+    int64_t* split_rows;     // [places]
+    int2* split_n;           // [places][ranges]
+    uint64_t* split_keys;    // [places][ranges][k]
 };
+
+__host__ __device__ __forceinline__ int32_t ranges_of(int32_t K, int64_t L)
+{
+    const int32_t range = L < kWideTokens ? kNarrowRange : kWideRange;
+    return (K + range - 1) / range;
+}
+// Split where a workgroup would take long: where 32-bit counters are needed, or a few ranges (where there
+// are more, a table is the better one).
+__device__ __forceinline__ bool split_document(const TopicArgs& a, int64_t L)
+{
+    if (a.places == 0 || L < kSplitTokens) return false;
+    return L >= kWideTokens ? a.ranges > 1 : (ranges_of(a.K, L) > 1 && ranges_of(a.K, L) <= 4);
+}
 
 __device__ __forceinline__ void document_of(const TopicArgs& a, int64_t row, int64_t& g0, int64_t& g1)
 {
@@ -232,12 +259,24 @@ __global__ __launch_bounds__(kWaveBlock) void wave_topics_kernel(TopicArgs a)
     first_tokens(a.z + g0, tokens(), next);
     for (; row < a.rows; row += step) {
         const int32_t L = tokens();
-        const bool longer = g1 - g0 > kWaveTokens;
+        const int64_t length = g1 - g0;
+        const bool longer = length > kWaveTokens;
         const int32_t* const z = a.z + g0;
         g0 = g1 = 0;
         if (row + step < a.rows) document_of(a, row + step, g0, g1);
         const auto read_next = [&]() { first_tokens(a.z + g0, tokens(), next); };
         if (longer) {
+            if (lane == 0) {
+                int32_t mark = kUnfinished;
+                if (split_document(a, length)) {
+                    const int32_t place = atomicAdd(a.n_split, 1);
+                    if (place < a.places) {
+                        a.split_rows[place] = row;
+                        mark = kSplit - place;
+                    }
+                }
+                a.ids[row * a.k] = mark;
+            }
             read_next();
             continue;
         }
@@ -569,112 +608,169 @@ __device__ __forceinline__ bool topics_by_table(const TopicArgs& a, int64_t row,
     return true;
 }
 
-// Counters are 16-bit for documents of less than 2^16 tokens (twice the topics a range), else 32-bit.
+// The best k topics of one range, of topics from t0 on, to lds.keys, n_first on; returns the thread's
+// share of the tokens counted.  Counters are 16-bit for documents of less than 2^16 tokens (twice the
+// topics a range), else 32-bit.
+template <bool WIDE>
+__device__ __forceinline__ int32_t best_of_range(const TopicArgs& a, const int32_t* z, int32_t L, int32_t t0, int32_t n_first,
+                                                 LongLds& lds)
+{
+    constexpr int32_t kPer = WIDE ? 1 : 2, kRange = WIDE ? kWideRange : kNarrowRange;
+    constexpr int kLoads = 2;
+    const int32_t tid = (int32_t)threadIdx.x;
+    int32_t counted = 0;
+    const int32_t nt = min(kRange, a.K - t0);
+    // words of a thread, an odd number for their banks; topics [tid * each * kPer, ..) of the range
+    const int32_t each_words = ((nt + kPer - 1) / kPer + kLongBlock - 1) / kLongBlock | 1;
+    uint32_t* const own = lds.count + tid * each_words;
+    // f(count, topic of the range) for the thread's own topics in ascending order
+    const auto each = [&](auto f) {
+#pragma unroll 1
+        for (int32_t j = 0; j < each_words; ++j) {
+            const uint32_t w = own[j];
+            if (w == 0) continue;
+            const int32_t t = (tid * each_words + j) * kPer;
+            if (WIDE) {
+                f(w, t);
+            } else {
+                if (w & 0xFFFFu) f(w & 0xFFFFu, t);
+                if (w >> 16) f(w >> 16, t + 1);
+            }
+        }
+    };
+    // four neighbours a load
+    int4 next[kLoads];
+    const auto load = [&](int32_t i0, int32_t e) {
+        const int64_t i = (int64_t)i0 + (e * kLongBlock + tid) * 4;
+        int4 v;
+        if (i + 4 <= L) {
+            __builtin_memcpy(&v, z + i, 16);
+        } else {
+            v.x = i < L ? z[i] : -1;
+            v.y = i + 1 < L ? z[i + 1] : -1;
+            v.z = i + 2 < L ? z[i + 2] : -1;
+            v.w = -1;
+        }
+        return v;
+    };
+#pragma unroll
+    for (int e = 0; e < kLoads; ++e) next[e] = load(0, e);
+    __syncthreads();
+    for (int32_t i = tid; i < each_words * kLongBlock; i += kLongBlock) lds.count[i] = 0;
+    __syncthreads();
+    const auto count = [&](uint32_t at, uint32_t tokens) {
+        if (WIDE) atomicAdd(&lds.count[at], tokens);
+        else atomicAdd(&lds.count[at / 2], tokens << (16 * (at & 1)));
+    };
+    HotTopics hot((int32_t)((uint32_t)next[0].x - (uint32_t)t0), (uint32_t)next[0].x - (uint32_t)t0 < (uint32_t)nt);
+    for (int64_t i0 = 0; i0 < L; i0 += kLoads * kLongBlock * 4) {
+        int4 topic[kLoads];
+#pragma unroll
+        for (int e = 0; e < kLoads; ++e) {
+            topic[e] = next[e];
+            if (i0 + kLoads * kLongBlock * 4 < L) next[e] = load((int32_t)(i0 + kLoads * kLongBlock * 4), e);
+        }
+#pragma unroll
+        for (int e = 0; e < kLoads; ++e) {
+            const int32_t four[4] = {topic[e].x, topic[e].y, topic[e].z, topic[e].w};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t at = (uint32_t)four[q] - (uint32_t)t0;  // (-1 and topics of other ranges lie beyond)
+                const bool open = at < (uint32_t)nt;
+                if (hot.left((int32_t)at, open)) count(at, 1u);
+            }
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < HotTopics::kHot; ++q)
+        if (hot.tokens[q] > 0 && tid % kWave == 0) count((uint32_t)hot.topic[q], (uint32_t)hot.tokens[q]);
+    __syncthreads();
+    int32_t some = 0;
+    each([&](uint32_t c, int32_t) {
+        ++some;
+        counted += (int32_t)c;
+    });
+    some = block_sum<kLongBlock>(some, lds.part);
+    // the range's best to lds.keys, behind those of the ranges before; topics come in ascending order
+    const auto best_of = [&](auto each_topic) {
+        uint32_t least = 0;
+        int32_t ties = 0, equal = 0, before = 0, total;
+        if (some > a.k) {
+            least = least_count(lds, a.k, ties, [&](auto f) { each_topic([&](uint32_t c, int32_t) { f(c); }); });
+            each_topic([&](uint32_t c, int32_t) { equal += c == least; });
+            before = block_prefix<kLongBlock>(equal, lds.part, total);
+        }
+        __syncthreads();
+        if (tid == 0) lds.n_keys = n_first;
+        __syncthreads();
+        each_topic([&](uint32_t c, int32_t t) {
+            if (c > least || (c == least && before++ < ties)) lds.keys[atomicAdd(&lds.n_keys, 1)] = long_key(c, t);
+        });
+        __syncthreads();
+    };
+    best_of([&](auto f) { each([&](uint32_t c, int32_t t) { f(c, t0 + t); }); });
+    return counted;
+}
+
 template <bool WIDE>
 __device__ __forceinline__ void topics_by_counters(const TopicArgs& a, int64_t row, int64_t g0, int32_t L, LongLds& lds)
 {
-    constexpr int32_t kPer = WIDE ? 1 : 2, kRange = kPer * kLongWords * kLongBlock;
-    constexpr int kLoads = 2;
-    const int32_t tid = (int32_t)threadIdx.x;
-    const int32_t* const z = a.z + g0;
     int32_t n_best = 0, counted = 0;
-    for (int32_t t0 = 0; t0 < a.K; t0 += kRange) {
-        const int32_t nt = min(kRange, a.K - t0);
-        // words of a thread, an odd number for their banks; topics [tid * each * kPer, ..) of the range
-        const int32_t each_words = ((nt + kPer - 1) / kPer + kLongBlock - 1) / kLongBlock | 1;
-        uint32_t* const own = lds.count + tid * each_words;
-        // f(count, topic of the range) for the thread's own topics in ascending order
-        const auto each = [&](auto f) {
-#pragma unroll 1
-            for (int32_t j = 0; j < each_words; ++j) {
-                const uint32_t w = own[j];
-                if (w == 0) continue;
-                const int32_t t = (tid * each_words + j) * kPer;
-                if (WIDE) {
-                    f(w, t);
-                } else {
-                    if (w & 0xFFFFu) f(w & 0xFFFFu, t);
-                    if (w >> 16) f(w >> 16, t + 1);
-                }
-            }
-        };
-        // four neighbours a load
-        int4 next[kLoads];
-        const auto load = [&](int32_t i0, int32_t e) {
-            const int64_t i = (int64_t)i0 + (e * kLongBlock + tid) * 4;
-            int4 v;
-            if (i + 4 <= L) {
-                __builtin_memcpy(&v, z + i, 16);
-            } else {
-                v.x = i < L ? z[i] : -1;
-                v.y = i + 1 < L ? z[i + 1] : -1;
-                v.z = i + 2 < L ? z[i + 2] : -1;
-                v.w = -1;
-            }
-            return v;
-        };
-#pragma unroll
-        for (int e = 0; e < kLoads; ++e) next[e] = load(0, e);
-        __syncthreads();
-        for (int32_t i = tid; i < each_words * kLongBlock; i += kLongBlock) lds.count[i] = 0;
-        __syncthreads();
-        const auto count = [&](uint32_t at, uint32_t tokens) {
-            if (WIDE) atomicAdd(&lds.count[at], tokens);
-            else atomicAdd(&lds.count[at / 2], tokens << (16 * (at & 1)));
-        };
-        HotTopics hot((int32_t)((uint32_t)next[0].x - (uint32_t)t0), (uint32_t)next[0].x - (uint32_t)t0 < (uint32_t)nt);
-        for (int64_t i0 = 0; i0 < L; i0 += kLoads * kLongBlock * 4) {
-            int4 topic[kLoads];
-#pragma unroll
-            for (int e = 0; e < kLoads; ++e) {
-                topic[e] = next[e];
-                if (i0 + kLoads * kLongBlock * 4 < L) next[e] = load((int32_t)(i0 + kLoads * kLongBlock * 4), e);
-            }
-#pragma unroll
-            for (int e = 0; e < kLoads; ++e) {
-                const int32_t four[4] = {topic[e].x, topic[e].y, topic[e].z, topic[e].w};
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t at = (uint32_t)four[q] - (uint32_t)t0;  // (-1 and topics of other ranges lie beyond)
-                    const bool open = at < (uint32_t)nt;
-                    if (hot.left((int32_t)at, open)) count(at, 1u);
-                }
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < HotTopics::kHot; ++q)
-            if (hot.tokens[q] > 0 && tid % kWave == 0) count((uint32_t)hot.topic[q], (uint32_t)hot.tokens[q]);
-        __syncthreads();
-        int32_t some = 0;
-        each([&](uint32_t c, int32_t) {
-            ++some;
-            counted += (int32_t)c;
-        });
-        some = block_sum<kLongBlock>(some, lds.part);
-        // the range's best to lds.keys, behind those of the ranges before; topics come in ascending order
-        const auto best_of = [&](auto each_topic) {
-            uint32_t least = 0;
-            int32_t ties = 0, equal = 0, before = 0, total;
-            if (some > a.k) {
-                least = least_count(lds, a.k, ties, [&](auto f) { each_topic([&](uint32_t c, int32_t) { f(c); }); });
-                each_topic([&](uint32_t c, int32_t) { equal += c == least; });
-                before = block_prefix<kLongBlock>(equal, lds.part, total);
-            }
-            __syncthreads();
-            if (tid == 0) lds.n_keys = n_best;
-            __syncthreads();
-            each_topic([&](uint32_t c, int32_t t) {
-                if (c > least || (c == least && before++ < ties)) lds.keys[atomicAdd(&lds.n_keys, 1)] = long_key(c, t);
-            });
-            __syncthreads();
-        };
-        best_of([&](auto f) { each([&](uint32_t c, int32_t t) { f(c, t0 + t); }); });
+    for (int32_t t0 = 0; t0 < a.K; t0 += WIDE ? kWideRange : kNarrowRange) {
+        counted += best_of_range<WIDE>(a, a.z + g0, L, t0, n_best, lds);
         const int32_t n = lds.n_keys;
+        order_keys(lds.keys, n, a.k, lds.best);
+        n_best = min(n, a.k);
+        for (int32_t i = (int32_t)threadIdx.x; i < n_best; i += kLongBlock) lds.keys[i] = lds.best[i];
+    }
+    counted = block_sum<kLongBlock>(counted, lds.part);
+    write_keys(a, row, lds.best, n_best, counted);
+}
+
+// The ranges of the documents that are split, a workgroup each
+__global__ __launch_bounds__(kLongBlock) void range_topics_kernel(TopicArgs a)
+{
+    extern __shared__ __align__(16) unsigned char raw[];
+    LongLds& lds = *reinterpret_cast<LongLds*>(raw);
+    const int32_t tid = (int32_t)threadIdx.x;
+    const int64_t n = (int64_t)min(*a.n_split, a.places) * a.ranges;
+    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+        int64_t g0, g1;
+        document_of(a, a.split_rows[i / a.ranges], g0, g1);
+        const int32_t L = (int32_t)(g1 - g0), range = (int32_t)(i % a.ranges);
+        if (range >= ranges_of(a.K, L)) continue;
+        int32_t counted;
+        if (L < kWideTokens) counted = best_of_range<false>(a, a.z + g0, L, range * kNarrowRange, 0, lds);
+        else counted = best_of_range<true>(a, a.z + g0, L, range * kWideRange, 0, lds);
+        counted = block_sum<kLongBlock>(counted, lds.part);
+        const int32_t n_keys = lds.n_keys;
+        if (tid == 0) a.split_n[i] = make_int2(n_keys, counted);
+        for (int32_t j = tid; j < n_keys; j += kLongBlock) a.split_keys[i * a.k + j] = lds.keys[j];
+        __syncthreads();
+    }
+}
+
+// and put together: as many ranges at a time as are ordered quickly
+__device__ __forceinline__ void join_ranges(const TopicArgs& a, int64_t row, int32_t L, int32_t place, LongLds& lds)
+{
+    const int32_t tid = (int32_t)threadIdx.x, ranges = ranges_of(a.K, L), most = max(2 * a.k, 512);
+    int32_t n_best = 0, counted = 0;
+    for (int32_t r = 0; r < ranges;) {
+        int32_t n = n_best;
+        __syncthreads();
+        for (; r < ranges; ++r) {
+            const int64_t i = (int64_t)place * a.ranges + r;
+            const int2 part = a.split_n[i];
+            if (n + part.x > most) break;
+            for (int32_t j = tid; j < part.x; j += kLongBlock) lds.keys[n + j] = a.split_keys[i * a.k + j];
+            n += part.x;
+            counted += part.y;
+        }
+        __syncthreads();
         order_keys(lds.keys, n, a.k, lds.best);
         n_best = min(n, a.k);
         for (int32_t i = tid; i < n_best; i += kLongBlock) lds.keys[i] = lds.best[i];
     }
-    counted = block_sum<kLongBlock>(counted, lds.part);
     write_keys(a, row, lds.best, n_best, counted);
 }
 
@@ -683,14 +779,37 @@ __global__ __launch_bounds__(kLongBlock) void long_topics_kernel(TopicArgs a)
     extern __shared__ __align__(16) unsigned char raw[];
     LongLds& lds = *reinterpret_cast<LongLds*>(raw);
     for_rows_left<kLongBlock>(a, lds.mine, &lds.n_mine, [&](int64_t row, int64_t g0, int32_t L) {
-        const int32_t range = (L < 65536 ? 2 : 1) * kLongWords * kLongBlock, ranges = (a.K + range - 1) / range;
+        const int32_t mark = a.ids[row * a.k], ranges = ranges_of(a.K, L);
+        if (mark <= kSplit) {
+            join_ranges(a, row, L, kSplit - mark, lds);
+            return;
+        }
         if (ranges > 1 && L / kTableTokens < ranges && topics_by_table(a, row, g0, L, lds)) return;
-        if (L < 65536) {
+        if (L < kWideTokens) {
             topics_by_counters<false>(a, row, g0, L, lds);
         } else {
             topics_by_counters<true>(a, row, g0, L, lds);
         }
     });
+}
+
+__global__ void no_splits_kernel(int32_t* n_split) { *n_split = 0; }
+
+// Places for documents that are split, and their bytes
+static int64_t split_places(const lda_topic_rows* d)
+{
+    if (d->K <= kWideRange || d->tokens < kSplitTokens) return 0;
+    int64_t most = d->rows;
+    if (!d->docs && most > d->tokens / kSplitTokens) most = d->tokens / kSplitTokens;
+    return most;
+}
+static int64_t split_bytes(int64_t places, int64_t ranges, int64_t k) { return 16 + places * (8 + ranges * (8 + 8 * k)); }
+static int64_t topics_bytes(const lda_topic_rows* d)
+{
+    const int64_t places = split_places(d);
+    if (places == 0) return 0;
+    const int64_t ranges = ranges_of(d->K, kWideTokens), each = split_bytes(1, ranges, d->slots) - 16;
+    return 16 + (places < kSplitBytes / each ? places : kSplitBytes / each) * each;
 }
 
 static int launch_top_topics(lda_ctx* c, const TopicArgs& a, hipStream_t stream)
@@ -700,9 +819,15 @@ static int launch_top_topics(lda_ctx* c, const TopicArgs& a, hipStream_t stream)
         const int64_t n = (a.rows + rows_each - 1) / rows_each;
         return (unsigned)(n < most ? n : most);
     };
+    if (a.places > 0) no_splits_kernel<<<1, 1, 0, stream>>>(a.n_split);
     // documents cannot be longer than all of z
     wave_topics_kernel<<<grid(kWaveBlock / kWave, 256 * 6), kWaveBlock, 0, stream>>>(a);
     if (a.tokens > kWaveTopics) {
+        if (a.places > 0) {
+            LDA_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(range_topics_kernel),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(LongLds)));
+            range_topics_kernel<<<256, kLongBlock, sizeof(LongLds), stream>>>(a);
+        }
         LDA_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(long_topics_kernel),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(LongLds)));
         long_topics_kernel<<<grid(1, 256), kLongBlock, sizeof(LongLds), stream>>>(a);
@@ -722,32 +847,50 @@ static int check_outputs(lda_ctx* c, const char* call, int64_t rows, int32_t slo
     return LDA_OK;
 }
 
-}  // namespace lda
-
-using namespace lda;
-
-extern "C" {
-
-int lda_top_topics(const lda_topic_rows* d, int32_t* ids, float* logits, float* log_norm)
-try {
-    const char* call = "lda_top_topics";
+static int check_topics(const lda_topic_rows* d, const char* call)
+{
     if (!d) return fail(nullptr, LDA_ERR_ARG, "%s: NULL rows", call);
     for (int32_t r : d->reserved)
         if (r != 0) return fail(nullptr, LDA_ERR_ARG, "%s: reserved fields must be zero", call);
     if (d->reserved_word != 0) return fail(nullptr, LDA_ERR_ARG, "%s: reserved fields must be zero", call);
-    const int rc = check_outputs(nullptr, call, d->rows, d->slots, ids, logits, log_norm);
-    if (rc != LDA_OK) return rc;
+    if (d->rows < 0 || d->slots < 1) return fail(nullptr, LDA_ERR_ARG, "%s: rows >= 0, slots >= 1 needed", call);
+    if (d->slots > kMostTopSlots) return fail(nullptr, LDA_ERR_UNSUPPORTED, "%s: at most %d slots", call, kMostTopSlots);
     if (d->documents < 0 || d->tokens < 0 || d->K < 1 || (!d->docs && d->documents < d->rows))
         return fail(nullptr, LDA_ERR_ARG, "%s: documents >= 0 (>= rows without docs), tokens >= 0, K >= 1 needed", call);
     if (d->K > (1 << 20) - 2) return fail(nullptr, LDA_ERR_UNSUPPORTED, "%s: K must be at most 2^20 - 2", call);
     if (!(d->alpha > 0.0) || !(d->alpha < 1e300))
         return fail(nullptr, LDA_ERR_ARG, "%s: alpha must be positive and finite", call);
     if (!known_index(d->offsets_type)) return fail(nullptr, LDA_ERR_ARG, "%s: unknown type", call);
+    if (d->workspace_bytes < 0 || !aligned_to(d->workspace, 16))
+        return fail(nullptr, LDA_ERR_ARG, "%s: a workspace aligned to 16 bytes needed, or none", call);
     if (d->rows == 0) return LDA_OK;
     if ((d->documents > 0 && !d->offsets) || (d->tokens > 0 && !d->z))
         return fail(nullptr, LDA_ERR_ARG, "%s: NULL pointer", call);
     if (!aligned_to(d->docs, 4) || !aligned_to(d->offsets, index_bytes(d->offsets_type)) || !aligned_to(d->z, 4))
         return fail(nullptr, LDA_ERR_ARG, "%s: a pointer is not aligned to its type", call);
+    return LDA_OK;
+}
+
+}  // namespace lda
+
+using namespace lda;
+
+extern "C" {
+
+int64_t lda_topics_workspace(const lda_topic_rows* d)
+try {
+    const int rc = check_topics(d, "lda_topics_workspace");
+    return rc != LDA_OK ? rc : topics_bytes(d);
+} catch (...) {
+    return LDA_ERR_OOM;
+}
+
+int lda_top_topics(const lda_topic_rows* d, int32_t* ids, float* logits, float* log_norm)
+try {
+    const char* call = "lda_top_topics";
+    int rc = check_topics(d, call);
+    if (rc == LDA_OK) rc = check_outputs(nullptr, call, d->rows, d->slots, ids, logits, log_norm);
+    if (rc != LDA_OK || d->rows == 0) return rc;
     TopicArgs a{};
     a.rows = d->rows;
     a.docs = d->docs;
@@ -762,6 +905,17 @@ try {
     a.ids = ids;
     a.logits = logits;
     a.log_norm = log_norm;
+    if (d->workspace) {
+        // as many documents as there is room for
+        a.ranges = ranges_of(d->K, kWideTokens);
+        const int64_t each = split_bytes(1, a.ranges, d->slots) - 16, room = (d->workspace_bytes - 16) / each;
+        const int64_t places = split_places(d) < room ? split_places(d) : room;
+        a.places = places < 1 ? 0 : (int32_t)(places < (1 << 24) ? places : 1 << 24);
+        a.n_split = static_cast<int32_t*>(d->workspace);
+        a.split_rows = reinterpret_cast<int64_t*>(a.n_split + 4);
+        a.split_n = reinterpret_cast<int2*>(a.split_rows + a.places);
+        a.split_keys = reinterpret_cast<uint64_t*>(a.split_n + (int64_t)a.places * a.ranges);
+    }
     return launch_top_topics(nullptr, a, static_cast<hipStream_t>(d->hip_stream));
 } catch (...) {
     return LDA_ERR_OOM;

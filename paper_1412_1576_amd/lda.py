@@ -28,7 +28,8 @@ EXPORTS = [
     "lda_get_nkw_row", "lda_get_ndk_row", "lda_get_alias_row", "lda_get_sparse_table",
     "lda_get_beta_table",
     "lda_distill_workspace", "lda_distill_loss", "lda_distill_grad", "lda_distill_step",
-    "lda_verify_workspace", "lda_verify_drafts", "lda_top_topics", "lda_doc_topics", "lda_sync", "lda_last_error", "lda_destroy",
+    "lda_verify_workspace", "lda_verify_drafts", "lda_topics_workspace", "lda_top_topics",
+    "lda_doc_topics", "lda_sync", "lda_last_error", "lda_destroy",
 ]
 
 
@@ -89,7 +90,8 @@ class lda_topic_rows(C.Structure):
         ("rows", C.c_int64), ("docs", C.c_void_p), ("documents", C.c_int64),
         ("offsets", C.c_void_p), ("offsets_type", C.c_int32), ("K", C.c_int32),
         ("z", C.c_void_p), ("tokens", C.c_int64), ("slots", C.c_int32), ("reserved_word", C.c_int32),
-        ("alpha", C.c_double), ("hip_stream", C.c_void_p), ("reserved", C.c_int32 * 4),
+        ("alpha", C.c_double), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64),
+        ("hip_stream", C.c_void_p), ("reserved", C.c_int32 * 4),
     ]
 
 
@@ -150,6 +152,7 @@ def load_library():
         "lda_distill_step": (C.c_int, [C.POINTER(lda_distill_rows), vp, vp, C.c_int64]),
         "lda_verify_workspace": (C.c_int64, [C.POINTER(lda_draft_rows)]),
         "lda_verify_drafts": (C.c_int, [C.POINTER(lda_draft_rows), vp, vp, C.c_int64]),
+        "lda_topics_workspace": (C.c_int64, [C.POINTER(lda_topic_rows)]),
         "lda_top_topics": (C.c_int, [C.POINTER(lda_topic_rows), vp, vp, vp]),
         "lda_doc_topics": (C.c_int, [vp, C.c_int64, vp, C.c_int32, vp, vp, vp]),
         "lda_sync": (C.c_int, [vp]),

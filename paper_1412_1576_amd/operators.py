@@ -251,9 +251,11 @@ def top_topics(z, doc_offsets, K, slots, alpha, *, docs=None):
         # in the order of the struct's fields
         r = lda.lda_topic_rows(n, None if docs is None else docs.data_ptr(), documents, doc_offsets.data_ptr(),
                                _INDEXES[doc_offsets.dtype], _int32(K, "K"), z.data_ptr(), z.numel(), slots, 0,
-                               alpha, _raw_stream(device))
+                               alpha, None, 0, _raw_stream(device))
+        w = _workspace(r, _check(L.lda_topics_workspace(r)), device)
         ids, logits, log_norm = _teacher_rows(n, max(slots, 0), device)
         _check(L.lda_top_topics(r, ids.data_ptr(), logits.data_ptr(), log_norm.data_ptr()))
+        del w
     return ids, logits, log_norm
 
 

@@ -231,3 +231,35 @@ def test_together(ops):
     for i, a in enumerate(accepted.tolist()):
         assert torch.equal(got[i, :a], tokens[i, :a]) and 0 <= got[i, a] < cfg.K and (got[i, a + 1:] == -1).all()
     m.close()
+
+
+@pytest.mark.parametrize("K", [40_000, 100_000, 400_000, 2 ** 20 - 2])
+def test_any_workspace_gives_the_same(ops, K):
+    """None, room for one of the long documents, room for all: rows are equal, what lies around them is as it
+    was; the documents' topics are few (tables, joined ranges) or many (counters)."""
+    import ctypes as C
+    from paper_1412_1576_amd import lda
+    rng = np.random.default_rng(K)
+    lengths = [70_000, 20_000, 3, 65_536, 65_535, 150_000, 16_384, 16_383, 0, 30_000, 90_000]
+    z = some_z(rng, sum(lengths), K, flat=0.3)
+    z[:70_000] = rng.integers(0, 300, 70_000)     # a few topics, many tokens
+    z[70_000:90_000] = rng.integers(0, K, 20_000)
+    offsets = np.concatenate([[0], np.cumsum(lengths)])
+    zt, ot = torch.from_numpy(z.astype(np.int32)).cuda(), torch.from_numpy(offsets).cuda()
+    slots, n = 100, len(lengths)
+    want = reference(z, offsets, K, slots, 0.1, range(n))
+    L = lda.load_library()
+    r = lda.lda_topic_rows(n, None, n, ot.data_ptr(), 1, K, zt.data_ptr(), zt.numel(), slots, 0, 0.1, None, 0,
+                           torch.cuda.current_stream().cuda_stream)
+    need = L.lda_topics_workspace(r)
+    assert need > 0
+    one = 16 + (need - 16) // min(n, zt.numel() // 16_384)
+    for nbytes in (0, 15, one, 2 * one, need):
+        w = torch.full((max(nbytes, 1) + 64,), 255, dtype=torch.uint8, device="cuda")
+        r.workspace, r.workspace_bytes = w.data_ptr() if nbytes else None, nbytes
+        out = [torch.full((n + 1, slots), -77, dtype=torch.int32, device="cuda"),
+               torch.full((n + 1, slots), -77.0, device="cuda"), torch.full((n + 1,), -77.0, device="cuda")]
+        assert L.lda_top_topics(r, *[x.data_ptr() for x in out]) == 0
+        torch.cuda.synchronize()
+        same([x[:n] for x in out], want)
+        assert all((x[n:] == -77).all() for x in out) and (w[nbytes:] == 255).all()

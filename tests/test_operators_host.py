@@ -135,11 +135,13 @@ def topics(**kw):
     ("alpha", float("nan"), lda.LDA_ERR_ARG), ("alpha", float("inf"), lda.LDA_ERR_ARG),
     ("offsets_type", 2, lda.LDA_ERR_ARG), ("offsets", None, lda.LDA_ERR_ARG), ("z", None, lda.LDA_ERR_ARG),
     ("z", (1 << 20) + 1, lda.LDA_ERR_ARG), ("docs", (1 << 20) + 2, lda.LDA_ERR_ARG),
-    ("reserved_word", 1, lda.LDA_ERR_ARG)])
+    ("reserved_word", 1, lda.LDA_ERR_ARG), ("workspace", 8, lda.LDA_ERR_ARG),
+    ("workspace_bytes", -1, lda.LDA_ERR_ARG)])
 def test_top_topics_refuses(lib, field, value, code):
     r = topics(**{field: value})
     assert lib.lda_top_topics(C.byref(r), 1 << 21, 1 << 21, 1 << 21) == code
     assert "lda_top_topics" in message(lib)
+    assert lib.lda_topics_workspace(C.byref(r)) == code
 
 
 def test_topics_refuse_outputs_and_contexts(lib):
@@ -156,7 +158,7 @@ def test_struct_layouts():
     # bytes, stream; reserved) and so on, all fields at their natural alignment
     assert C.sizeof(lda.lda_distill_rows) == 8 + 8 + 6 * 8 + 8 + 16 + 16 + 24 + 16
     assert C.sizeof(lda.lda_draft_rows) == 8 + 8 + 3 * 8 + 3 * 8 + 2 * 8 + 8 + 2 * 8 + 8 + 8 + 24 + 16
-    assert C.sizeof(lda.lda_topic_rows) == 3 * 8 + 8 + 8 + 2 * 8 + 8 + 8 + 8 + 16
+    assert C.sizeof(lda.lda_topic_rows) == 3 * 8 + 8 + 8 + 2 * 8 + 8 + 8 + 2 * 8 + 8 + 16
 
 
 def test_the_binding_refuses_host_tensors():
