@@ -52,8 +52,8 @@ struct TopicArgs {
     float* logits;
     float* log_norm;
     // documents that are split: how many, their rows; per document and range (topics, tokens) and the keys
-    int32_t places, ranges;  // 0 places: none is
-    int32_t* n_split;
+    int32_t wide_places, places, ranges;
+    int32_t* n_split;        // [2] of kWideTokens or more, which take the first wide_places: they begin first; of less
     int64_t* split_rows;     // [places]
     int2* split_n;           // [places][ranges]
     uint64_t* split_keys;    // [places][ranges][k]
@@ -113,44 +113,61 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
             topic[e] = next[e];
             next[e] = i < L ? z[i] : -1;
         }
+        // the rounds' look-ups side by side: one after the other they would wait for LDS each
+        int32_t mine[kAhead];
+        bool open[kAhead];
 #pragma unroll
         for (int e = 0; e < kAhead; ++e) {
-            if (i0 + e * kWave >= L) break;
-            const uint32_t t = (uint32_t)topic[e];
-            bool open = t < (uint32_t)a.K;
-            counted += (int32_t)__popcll(__ballot(open));
-            const uint32_t inv = inverted - t;
-            int32_t mine = -1;
-            if (a.K <= kSlots) {  // a slot a topic: no search
-                if (open) {
-                    const uint32_t before = atomicAdd(&table[t], one);
-                    if (before == 0) mine = (int32_t)t;
-                }
-            } else {
-                uint32_t h = (t * 0x9E3779B1u) >> (32 - __builtin_ctz(kSlots));
-                while (__ballot(open)) {  // half the slots stay empty: every search ends
-                    if (open) {
-                        uint32_t v = table[h];
-                        if (v == 0) v = atomicCAS(&table[h], 0u, one | inv);
-                        if (v == 0) {
-                            mine = (int32_t)h;
-                            open = false;
-                        } else if ((v & inverted) == inv) {
-                            atomicAdd(&table[h], one);
-                            open = false;
-                        } else {
-                            h = (h + 1) & (kSlots - 1);
+            open[e] = (uint32_t)topic[e] < (uint32_t)a.K;
+            counted += (int32_t)__popcll(__ballot(open[e]));
+            mine[e] = -1;
+        }
+        if (a.K <= kSlots) {  // a slot a topic: no search
+            uint32_t was[kAhead];
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) was[e] = open[e] ? atomicAdd(&table[topic[e]], one) : 1u;
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e)
+                if (was[e] == 0) mine[e] = topic[e];
+        } else {
+            uint32_t h[kAhead];
+#pragma unroll
+            for (int e = 0; e < kAhead; ++e) h[e] = ((uint32_t)topic[e] * 0x9E3779B1u) >> (32 - __builtin_ctz(kSlots));
+            // half the slots stay empty: every search ends
+            while (__ballot(open[0] || open[1] || open[2] || open[3])) {
+                uint32_t v[kAhead];
+#pragma unroll
+                for (int e = 0; e < kAhead; ++e) v[e] = open[e] ? table[h[e]] : 1u;
+#pragma unroll
+                for (int e = 0; e < kAhead; ++e)
+                    if (v[e] == 0) {
+                        v[e] = atomicCAS(&table[h[e]], 0u, one | (inverted - (uint32_t)topic[e]));
+                        if (v[e] == 0) {
+                            mine[e] = (int32_t)h[e];
+                            open[e] = false;
                         }
                     }
-                }
+#pragma unroll
+                for (int e = 0; e < kAhead; ++e)
+                    if (open[e]) {
+                        if ((v[e] & inverted) == inverted - (uint32_t)topic[e]) {
+                            atomicAdd(&table[h[e]], one);
+                            open[e] = false;
+                        } else {
+                            h[e] = (h[e] + 1) & (kSlots - 1);
+                        }
+                    }
             }
-            const uint64_t fresh = __ballot(mine >= 0);
-            if (mine >= 0) used[n + (int32_t)__builtin_amdgcn_mbcnt_hi((uint32_t)(fresh >> 32),
-                                                                     __builtin_amdgcn_mbcnt_lo((uint32_t)fresh, 0u))] = (uint16_t)mine;
-            n += (int32_t)__popcll(fresh);
-            many = n > kWaveTopics - kWave && i0 + (e + 1) * kWave < L;
-            if (many) break;
         }
+#pragma unroll
+        for (int e = 0; e < kAhead; ++e) {
+            const uint64_t fresh = __ballot(mine[e] >= 0);
+            if (mine[e] >= 0)
+                used[n + (int32_t)__builtin_amdgcn_mbcnt_hi((uint32_t)(fresh >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)fresh, 0u))] =
+                    (uint16_t)mine[e];
+            n += (int32_t)__popcll(fresh);
+        }
+        many = n + min(kAhead * kWave, L - i0 - kAhead * kWave) > kWaveTopics;
     }
     all_read();
     wave_lds_order();
@@ -236,7 +253,7 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
     return counted;
 }
 
-__global__ __launch_bounds__(kWaveBlock) void wave_topics_kernel(TopicArgs a)
+__global__ __launch_bounds__(kWaveBlock, 6) void wave_topics_kernel(TopicArgs a)
 {
     constexpr int kWaves = kWaveBlock / kWave;
     __shared__ __align__(16) uint32_t table[kWaves][2 * kWaveTopics];
@@ -269,8 +286,9 @@ __global__ __launch_bounds__(kWaveBlock) void wave_topics_kernel(TopicArgs a)
             if (lane == 0) {
                 int32_t mark = kUnfinished;
                 if (split_document(a, length)) {
-                    const int32_t place = atomicAdd(a.n_split, 1);
-                    if (place < a.places) {
+                    const bool wide = length >= kWideTokens;
+                    const int32_t place = (wide ? 0 : a.wide_places) + atomicAdd(&a.n_split[wide ? 0 : 1], 1);
+                    if (place < (wide ? a.wide_places : a.places)) {
                         a.split_rows[place] = row;
                         mark = kSplit - place;
                     }
@@ -358,62 +376,54 @@ struct LongLds {
 };
 static_assert(sizeof(LongLds) <= 160 * 1024, "LDS of a CU");
 
+// After a histogram: the digit where the `need`-th largest value lies, `need` less the values of larger
+// digits; all: the values there are (fewer than need: digit -1).
+__device__ __forceinline__ int32_t find_digit(LongLds& lds, int32_t& need, int32_t& all)
+{
+    const int32_t tid = (int32_t)threadIdx.x;
+    if (tid == 0) lds.digit = -1;
+    __syncthreads();
+    const int32_t d = (1 << kDigit) - 1 - tid;
+    const int32_t here = (int32_t)lds.histogram[d];
+    const int32_t above = block_prefix<kLongBlock>(here, lds.part, all);
+    if (above < need && above + here >= need) {
+        lds.digit = d;
+        lds.over = above;
+    }
+    __syncthreads();
+    const int32_t digit = lds.digit;
+    if (digit >= 0) need -= lds.over;
+    return digit;
+}
+static_assert(1 << kDigit == kLongBlock, "a thread a digit");
+
+__device__ __forceinline__ void clear_histogram(LongLds& lds)
+{
+    __syncthreads();
+    lds.histogram[threadIdx.x] = 0;
+    __syncthreads();
+}
+
 // The `need`-th largest of the workgroup's values (all below 2^most_bits, need of them or more), and
 // how many values equal to it are among the `need` largest.  each(f) calls f(value) for the thread's own.
 template <class Each>
 __device__ __forceinline__ uint32_t nth_largest(LongLds& lds, int32_t most_bits, int32_t& need, Each each)
 {
-    const int32_t tid = (int32_t)threadIdx.x;
-    int32_t shift = max(0, most_bits - kDigit), bits = most_bits - shift;
+    int32_t shift = max(0, most_bits - kDigit), bits = most_bits - shift, all;
     uint32_t prefix = 0;
     bool first = true;
     for (;;) {
-        __syncthreads();
-        for (int32_t i = tid; i < 1 << kDigit; i += kLongBlock) lds.histogram[i] = 0;
-        __syncthreads();
+        clear_histogram(lds);
         each([&](uint32_t v) {
-            const bool in = first || (v >> (shift + bits)) == prefix;
-            const uint32_t digit = (v >> shift) & ((1u << bits) - 1u);
-            // most counts are small: the wave's 0s and 1s are added up first
-            const uint64_t zeros = __ballot(in && digit == 0), ones = __ballot(in && digit == 1);
-            const int32_t leader = (int32_t)__builtin_ctzll(__ballot(true));
-            if ((int32_t)(threadIdx.x % kWave) == leader) {
-                if (zeros) atomicAdd(&lds.histogram[0], (uint32_t)__popcll(zeros));
-                if (ones) atomicAdd(&lds.histogram[1], (uint32_t)__popcll(ones));
-            }
-            if (in && digit > 1) atomicAdd(&lds.histogram[digit], 1u);
+            if (first || (v >> (shift + bits)) == prefix) atomicAdd(&lds.histogram[(v >> shift) & ((1u << bits) - 1u)], 1u);
         });
-        __syncthreads();
-        // digit d is the one when fewer than `need` lie above it and no fewer with its own
-        const int32_t d = (1 << kDigit) - 1 - tid;
-        const int32_t here = (int32_t)lds.histogram[d];
-        int32_t all;
-        const int32_t above = block_prefix<kLongBlock>(here, lds.part, all);
-        if (above < need && above + here >= need) {
-            lds.digit = d;
-            lds.over = above;
-        }
-        __syncthreads();
-        prefix = (prefix << bits) | (uint32_t)lds.digit;
-        need -= lds.over;
+        prefix = (prefix << bits) | (uint32_t)find_digit(lds, need, all);
         if (shift == 0) return prefix;
         first = false;
         bits = min(shift, kDigit);
         shift -= bits;
     }
 }
-static_assert(1 << kDigit == kLongBlock, "a thread a digit");
-
-__device__ __forceinline__ int32_t block_max(int32_t v, int32_t* part)
-{
-    v = wave_reduce(v, [](int32_t x, int32_t y) { return max(x, y); });
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
-    __syncthreads();
-    for (int w = 0; w < kLongBlock / kWave; ++w) v = max(v, part[w]);
-    return v;
-}
-__device__ __forceinline__ int32_t bits_of(uint32_t v) { return v == 0 ? 1 : 32 - (int32_t)__builtin_clz(v); }
 
 // The n keys in order of size, the best k of them to `best`.  A key's place is the number of larger ones,
 // which some threads of a wave count together where there are few keys.
@@ -486,21 +496,47 @@ __device__ __forceinline__ uint32_t bucket_of(uint32_t c)
     return 64 + ((e - 6) << 5) + ((c >> (e - 5)) & 31u);
 }
 
-// The k-th largest count of more than k, and into `ties` how many of the topics that have it are among
-// the best k.  each(f) calls f(count) for the thread's share.
+// The k-th largest count (0: there are no more than k), into `ties` how many of the topics that have it
+// are among the best k, into `equal` how many of them this thread has.  each(f) calls f(count) for the
+// thread's share.
 template <class Each>
-__device__ __forceinline__ uint32_t least_count(LongLds& lds, int32_t k, int32_t& ties, Each each)
+__device__ __forceinline__ uint32_t least_count(LongLds& lds, int32_t k, int32_t& ties, int32_t& equal, Each each)
 {
+    // most topics have a few tokens: their buckets would be everybody's
+    int32_t few[3] = {0, 0, 0};
+    clear_histogram(lds);
+    each([&](uint32_t c) {
+        if (c <= 3) {
+            few[0] += c == 1;
+            few[1] += c == 2;
+            few[2] += c == 3;
+        } else {
+            atomicAdd(&lds.histogram[bucket_of(c)], 1u);
+        }
+    });
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        const int32_t n = wave_sum(few[q]);
+        if (threadIdx.x % kWave == 0 && n > 0) atomicAdd(&lds.histogram[q + 1], (uint32_t)n);
+    }
+    int32_t all;
     ties = k;
-    const uint32_t bucket = nth_largest(lds, kDigit, ties, [&](auto f) { each([&](uint32_t c) { f(bucket_of(c)); }); });
-    if (bucket < 64) return bucket;
-    const int32_t bits = (int32_t)((bucket - 64) >> 5) + 1;  // of a count that its bucket leaves open
-    const uint32_t low = (32u + (bucket & 31u)) << bits;
-    return low + nth_largest(lds, bits, ties, [&](auto f) {
-               each([&](uint32_t c) {
-                   if (c - low < 1u << bits) f(c - low);
-               });
-           });
+    const int32_t bucket = find_digit(lds, ties, all);
+    equal = 0;
+    if (all <= k) return 0;
+    uint32_t least = (uint32_t)bucket;
+    if (bucket >= 64) {
+        const int32_t bits = ((bucket - 64) >> 5) + 1;  // of a count that its bucket leaves open
+        const uint32_t low = (32u + ((uint32_t)bucket & 31u)) << bits;
+        least = low + nth_largest(lds, bits, ties, [&](auto f) {
+                    each([&](uint32_t c) {
+                        if (c - low < 1u << bits) f(c - low);
+                    });
+                });
+    }
+    if (least <= 3) equal = least == 1 ? few[0] : least == 2 ? few[1] : few[2];
+    else each([&](uint32_t c) { equal += c == least; });
+    return least;
 }
 
 // The document's counts in a table; false, and nothing written, if it has too many topics for one
@@ -579,16 +615,16 @@ __device__ __forceinline__ bool topics_by_table(const TopicArgs& a, int64_t row,
     counted = block_sum<kLongBlock>(counted, lds.part);
     const int32_t n = lds.n_used;
     if (n > kTableTopics) return false;
-    uint32_t least = 1, after = 0;  // of the topics with the least count, those whose inverse is at least `after`
     const auto each = [&](auto f) {
         for (int32_t i = tid; i < n; i += kLongBlock) {
             const uint32_t h = table.used[i];
             f(table.count[h], table.topic[h]);
         }
     };
-    if (n > a.k) {
-        int32_t ties;
-        least = least_count(lds, a.k, ties, [&](auto f) { each([&](uint32_t c, uint32_t) { f(c); }); });
+    int32_t ties, equal;
+    const uint32_t least = least_count(lds, a.k, ties, equal, [&](auto f) { each([&](uint32_t c, uint32_t) { f(c); }); });
+    uint32_t after = 0;  // of the topics with the least count, those whose inverse is at least this
+    if (least > 0) {
         after = nth_largest(lds, (int32_t)kMixTopicBits, ties, [&](auto f) {
             each([&](uint32_t c, uint32_t t) {
                 if (c == least) f(kInverted - t);
@@ -625,9 +661,11 @@ __device__ __forceinline__ int32_t best_of_range(const TopicArgs& a, const int32
     uint32_t* const own = lds.count + tid * each_words;
     // f(count, topic of the range) for the thread's own topics in ascending order
     const auto each = [&](auto f) {
+        uint32_t next_word = own[0];
 #pragma unroll 1
         for (int32_t j = 0; j < each_words; ++j) {
-            const uint32_t w = own[j];
+            const uint32_t w = next_word;
+            next_word = own[min(j + 1, each_words - 1)];
             if (w == 0) continue;
             const int32_t t = (tid * each_words + j) * kPer;
             if (WIDE) {
@@ -677,6 +715,7 @@ __device__ __forceinline__ int32_t best_of_range(const TopicArgs& a, const int32
             for (int q = 0; q < 4; ++q) {
                 const uint32_t at = (uint32_t)four[q] - (uint32_t)t0;  // (-1 and topics of other ranges lie beyond)
                 const bool open = at < (uint32_t)nt;
+                counted += open;
                 if (hot.left((int32_t)at, open)) count(at, 1u);
             }
         }
@@ -685,30 +724,21 @@ __device__ __forceinline__ int32_t best_of_range(const TopicArgs& a, const int32
     for (int q = 0; q < HotTopics::kHot; ++q)
         if (hot.tokens[q] > 0 && tid % kWave == 0) count((uint32_t)hot.topic[q], (uint32_t)hot.tokens[q]);
     __syncthreads();
-    int32_t some = 0;
-    each([&](uint32_t c, int32_t) {
-        ++some;
-        counted += (int32_t)c;
-    });
-    some = block_sum<kLongBlock>(some, lds.part);
-    // the range's best to lds.keys, behind those of the ranges before; topics come in ascending order
-    const auto best_of = [&](auto each_topic) {
-        uint32_t least = 0;
-        int32_t ties = 0, equal = 0, before = 0, total;
-        if (some > a.k) {
-            least = least_count(lds, a.k, ties, [&](auto f) { each_topic([&](uint32_t c, int32_t) { f(c); }); });
-            each_topic([&](uint32_t c, int32_t) { equal += c == least; });
-            before = block_prefix<kLongBlock>(equal, lds.part, total);
-        }
-        __syncthreads();
-        if (tid == 0) lds.n_keys = n_first;
-        __syncthreads();
-        each_topic([&](uint32_t c, int32_t t) {
-            if (c > least || (c == least && before++ < ties)) lds.keys[atomicAdd(&lds.n_keys, 1)] = long_key(c, t);
+    // topics come in ascending order: ties go to the first
+    int32_t ties, equal, total;
+    const uint32_t least = least_count(lds, a.k, ties, equal, [&](auto f) {
+        each([&](uint32_t c, int32_t) {
+            f(c);
         });
-        __syncthreads();
-    };
-    best_of([&](auto f) { each([&](uint32_t c, int32_t t) { f(c, t0 + t); }); });
+    });
+    int32_t before = least > 0 ? block_prefix<kLongBlock>(equal, lds.part, total) : 0;
+    __syncthreads();
+    if (tid == 0) lds.n_keys = n_first;
+    __syncthreads();
+    each([&](uint32_t c, int32_t t) {
+        if (c > least || (c == least && before++ < ties)) lds.keys[atomicAdd(&lds.n_keys, 1)] = long_key(c, t0 + t);
+    });
+    __syncthreads();
     return counted;
 }
 
@@ -733,11 +763,15 @@ __global__ __launch_bounds__(kLongBlock) void range_topics_kernel(TopicArgs a)
     extern __shared__ __align__(16) unsigned char raw[];
     LongLds& lds = *reinterpret_cast<LongLds*>(raw);
     const int32_t tid = (int32_t)threadIdx.x;
-    const int64_t n = (int64_t)min(*a.n_split, a.places) * a.ranges;
-    for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+    const int32_t wide = min(a.n_split[0], a.wide_places), others = min(a.n_split[1], a.places - a.wide_places);
+    const int64_t n = ((int64_t)wide + others) * a.ranges;
+    for (int64_t q = blockIdx.x; q < n; q += gridDim.x) {
+        const int32_t at = (int32_t)(q / a.ranges), range = (int32_t)(q % a.ranges);
+        const int32_t place = at < wide ? at : a.wide_places + at - wide;
+        const int64_t i = (int64_t)place * a.ranges + range;
         int64_t g0, g1;
-        document_of(a, a.split_rows[i / a.ranges], g0, g1);
-        const int32_t L = (int32_t)(g1 - g0), range = (int32_t)(i % a.ranges);
+        document_of(a, a.split_rows[place], g0, g1);
+        const int32_t L = (int32_t)(g1 - g0);
         if (range >= ranges_of(a.K, L)) continue;
         int32_t counted;
         if (L < kWideTokens) counted = best_of_range<false>(a, a.z + g0, L, range * kNarrowRange, 0, lds);
@@ -793,23 +827,29 @@ __global__ __launch_bounds__(kLongBlock) void long_topics_kernel(TopicArgs a)
     });
 }
 
-__global__ void no_splits_kernel(int32_t* n_split) { *n_split = 0; }
+__global__ void no_splits_kernel(int32_t* n_split) { n_split[0] = n_split[1] = 0; }
 
-// Places for documents that are split, and their bytes
-static int64_t split_places(const lda_topic_rows* d)
+// Places for documents that are split: those of kWideTokens, the others; at most `room` in all
+struct SplitPlaces {
+    int64_t wide, others;
+};
+static SplitPlaces split_places(const lda_topic_rows* d, int64_t room)
 {
-    if (d->K <= kWideRange || d->tokens < kSplitTokens) return 0;
-    int64_t most = d->rows;
-    if (!d->docs && most > d->tokens / kSplitTokens) most = d->tokens / kSplitTokens;
-    return most;
+    if (d->K <= kWideRange) return {0, 0};
+    const auto most = [&](int64_t tokens) {
+        if (d->tokens < tokens) return (int64_t)0;
+        return d->docs || d->rows < d->tokens / tokens ? d->rows : d->tokens / tokens;
+    };
+    SplitPlaces p{most(kWideTokens), most(kSplitTokens)};
+    if (p.wide > room / 2 && p.wide + p.others > room) p.wide = room / 2;
+    if (p.others > room - p.wide) p.others = room - p.wide;
+    return p;
 }
-static int64_t split_bytes(int64_t places, int64_t ranges, int64_t k) { return 16 + places * (8 + ranges * (8 + 8 * k)); }
+static int64_t place_bytes(const lda_topic_rows* d) { return 8 + (int64_t)ranges_of(d->K, kWideTokens) * (8 + 8 * d->slots); }
 static int64_t topics_bytes(const lda_topic_rows* d)
 {
-    const int64_t places = split_places(d);
-    if (places == 0) return 0;
-    const int64_t ranges = ranges_of(d->K, kWideTokens), each = split_bytes(1, ranges, d->slots) - 16;
-    return 16 + (places < kSplitBytes / each ? places : kSplitBytes / each) * each;
+    const SplitPlaces p = split_places(d, kSplitBytes / place_bytes(d));
+    return p.wide + p.others == 0 ? 0 : 16 + (p.wide + p.others) * place_bytes(d);
 }
 
 static int launch_top_topics(lda_ctx* c, const TopicArgs& a, hipStream_t stream)
@@ -907,10 +947,11 @@ try {
     a.log_norm = log_norm;
     if (d->workspace) {
         // as many documents as there is room for
+        const int64_t room = d->workspace_bytes < 16 ? 0 : (d->workspace_bytes - 16) / place_bytes(d);
+        const SplitPlaces p = split_places(d, room < (1 << 24) ? room : 1 << 24);
+        a.wide_places = (int32_t)p.wide;
+        a.places = (int32_t)(p.wide + p.others);
         a.ranges = ranges_of(d->K, kWideTokens);
-        const int64_t each = split_bytes(1, a.ranges, d->slots) - 16, room = (d->workspace_bytes - 16) / each;
-        const int64_t places = split_places(d) < room ? split_places(d) : room;
-        a.places = places < 1 ? 0 : (int32_t)(places < (1 << 24) ? places : 1 << 24);
         a.n_split = static_cast<int32_t*>(d->workspace);
         a.split_rows = reinterpret_cast<int64_t*>(a.n_split + 4);
         a.split_n = reinterpret_cast<int2*>(a.split_rows + a.places);

@@ -253,7 +253,7 @@ def test_any_workspace_gives_the_same(ops, K):
                            torch.cuda.current_stream().cuda_stream)
     need = L.lda_topics_workspace(r)
     assert need > 0
-    one = 16 + (need - 16) // min(n, zt.numel() // 16_384)
+    one = 16 + 8 + -(-K // 31_744) * (8 + 8 * slots)
     for nbytes in (0, 15, one, 2 * one, need):
         w = torch.full((max(nbytes, 1) + 64,), 255, dtype=torch.uint8, device="cuda")
         r.workspace, r.workspace_bytes = w.data_ptr() if nbytes else None, nbytes
