@@ -3,9 +3,9 @@
 //
 // The accept tests touch two numbers a draft; the draw reads one row of the target, and the draft's
 // row beside it after a rejection.  Rows of up to kDirectClasses classes are one workgroup's, which
-// holds the masses in registers.  Longer ones are summed in segments of kSegment classes by as many waves as
-// there are, and in a second kernel a wave walks a sequence's sums to the segment that holds the
-// draw's place and looks only through that.  Masses and sums are 64-bit: p - q of two floats is
+// holds the masses in registers.  Longer ones are summed in segments of kSegment classes, and a wave walks
+// the sums to the segment that holds the draw's place and looks only through that: inside a workgroup, or for long rows
+// and many sequences the sums by as many waves as fill the GPU and the draws in a second kernel.  Masses and sums are 64-bit: p - q of two floats is
 // then all but exact, and a draw's place differs from another order of summation by some 2^-50 of the
 // row's mass.
 #include "rows.hpp"
@@ -17,6 +17,9 @@ constexpr int kVerifyBlock = 256;
 constexpr int32_t kSegment = 1024;
 constexpr int kEach = kSegment / kWave;                       // neighbours a lane holds in a draw
 constexpr int32_t kDirectClasses = kVerifyBlock * kEach;
+constexpr int kRowBlock = 1024;
+constexpr int64_t kRowBytes = 81920;
+constexpr int32_t kRowSegments = (int32_t)(kRowBytes / 2 / kSegment);
 
 struct Mass {
     double left, target;  // of max(0, p - q), of p
@@ -37,7 +40,7 @@ struct VerifyArgs {
     const float* draw_u;
     int32_t tokens_type;
     int32_t segments, each;  // of a row; of them, a wave's
-    Mass* sums;              // [sequences][segments]
+    Mass* sums;              // [sequences][segments]; NULL: a row is one workgroup's
     int2* found;             // [sequences] accepted drafts, drafts there are
     int32_t* accepted;
     void* out;
@@ -200,11 +203,111 @@ __global__ __launch_bounds__(kVerifyBlock) void verify_direct_kernel(VerifyArgs 
     }
 }
 
+// A wave's sums of segment s, in every lane
+template <class T>
+__device__ __forceinline__ Mass sum_segment(const VerifyArgs& a, const DrawRows<T>& rows, int32_t s)
+{
+    constexpr int E = Row<T>::kChunk, kLoads = kSegment / kWave / E;
+    const int32_t lane = (int32_t)threadIdx.x % kWave;
+    double left = 0.0, target = 0.0;
+    float p[kLoads][E], q[kLoads][E] = {};
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load_run<T, E>(rows.p, (int64_t)s * kSegment + (j * kWave + lane) * E, a.V, p[j]);
+    if (rows.q) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) load_run<T, E>(rows.q, (int64_t)s * kSegment + (j * kWave + lane) * E, a.V, q[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            target += mass_of((double)p[j][e]);
+            left += mass_of((double)p[j][e] - (double)q[j][e]);
+        }
+    return Mass{wave_sum(left), wave_sum(target)};
+}
+
+// A wave's draw: the segment of its place, then the element in it
+template <class T>
+__device__ __forceinline__ int64_t draw(const VerifyArgs& a, DrawRows<T> rows, const Mass* sums, double u)
+{
+    const int32_t lane = (int32_t)threadIdx.x % kWave;
+    double left = 0.0, target = 0.0;
+    for (int32_t s = lane; s < a.segments; s += kWave) {
+        left += sums[s].left;
+        target += sums[s].target;
+    }
+    left = wave_sum(left);
+    target = wave_sum(target);
+    const bool whole = !(left > 0.0);
+    if (whole) rows.q = nullptr;
+    const double place = u * (whole ? target : left);
+    // 64 sums at a time, in order
+    double before = 0.0;
+    int32_t segment = -1, last = -1;
+    for (int32_t s0 = 0; s0 < a.segments && segment < 0; s0 += kWave) {
+        const int32_t s = s0 + lane;
+        const double own = s < a.segments ? (whole ? sums[s].target : sums[s].left) : 0.0;
+        const double sum = wave_prefix(own);
+        const uint64_t some = __ballot(own > 0.0);
+        const uint64_t past = __ballot(own > 0.0 && before + sum > place);
+        if (some) last = s0 + 63 - (int32_t)__builtin_clzll(some);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            segment = s0 + at;
+            before += lane_value(sum - own, at);
+        } else {
+            before += lane_value(sum, kWave - 1);
+        }
+    }
+    const bool inside = segment >= 0;
+    if (!inside) segment = last;  // the last element of any mass
+    if (segment < 0) return -1;
+    const int64_t v = (int64_t)segment * kSegment + lane * kEach;
+    float p[kEach], q[kEach] = {};
+    load_run<T, kEach>(rows.p, v, a.V, p);
+    if (rows.q) load_run<T, kEach>(rows.q, v, a.V, q);
+    double mass[kEach], sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+        mass[e] = mass_of((double)p[e] - (double)q[e]);
+        sum += mass[e];
+    }
+    const double upto = wave_prefix(sum);
+    int32_t hit, most;
+    look_through(mass, before + (upto - sum), place, hit, most);
+    const uint64_t hits = __ballot(inside && hit >= 0), some = __ballot(most >= 0);
+    if (!hits && !some) return -1;
+    const int at = hits ? __builtin_ctzll(hits) : 63 - (int)__builtin_clzll(some);
+    return (int64_t)segment * kSegment + at * kEach + lane_value(hits ? hit : most, at);
+}
+
+// A workgroup a sequence, a row longer than its registers: the segments' sums in LDS
+template <class T>
+__global__ __launch_bounds__(kRowBlock) void verify_row_kernel(VerifyArgs a)
+{
+    constexpr int kWaves = kRowBlock / kWave;
+    __shared__ Mass sums[kRowSegments];
+    const int32_t wave = __builtin_amdgcn_readfirstlane((int32_t)threadIdx.x / kWave), lane = (int32_t)threadIdx.x % kWave;
+    for (int64_t b = blockIdx.x; b < a.sequences; b += gridDim.x) {
+        const double u = (double)a.draw_u[b];
+        int32_t n;
+        const int32_t k = count_accepted<T>(a, b, n);
+        const DrawRows<T> rows(a, b, k, n);
+        __syncthreads();  // the last sequence's sums are read
+        for (int32_t s = wave; s < a.segments; s += kWaves) {
+            const Mass m = sum_segment(a, rows, s);
+            if (lane == 0) sums[s] = m;
+        }
+        __syncthreads();
+        if (wave == 0) write_result(a, b, k, draw(a, rows, sums, u), lane, kWave);
+    }
+}
+
 // sums[b][segment] of the masses; blockIdx.y walks the segments, each wave of it `each` of them
 template <class T>
 __global__ __launch_bounds__(kVerifyBlock) void verify_sums_kernel(VerifyArgs a)
 {
-    constexpr int E = Row<T>::kChunk, kLoads = kSegment / kWave / E;
     const int32_t lane = (int32_t)threadIdx.x % kWave;
     const int32_t s0 = (int32_t)(blockIdx.y * (kVerifyBlock / kWave) + threadIdx.x / kWave) * a.each;
     const int32_t s1 = min(a.segments, s0 + a.each);
@@ -215,95 +318,21 @@ __global__ __launch_bounds__(kVerifyBlock) void verify_sums_kernel(VerifyArgs a)
         if (s0 == 0 && lane == 0) a.found[b] = make_int2(k, n);
         const DrawRows<T> rows(a, b, k, n);
         for (int32_t s = s0; s < s1; ++s) {
-            double left = 0.0, target = 0.0;
-            float p[kLoads][E], q[kLoads][E] = {};
-#pragma unroll
-            for (int j = 0; j < kLoads; ++j)
-                load_run<T, E>(rows.p, (int64_t)s * kSegment + (j * kWave + lane) * E, a.V, p[j]);
-            if (rows.q) {
-#pragma unroll
-                for (int j = 0; j < kLoads; ++j)
-                    load_run<T, E>(rows.q, (int64_t)s * kSegment + (j * kWave + lane) * E, a.V, q[j]);
-            }
-#pragma unroll
-            for (int j = 0; j < kLoads; ++j)
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    target += mass_of((double)p[j][e]);
-                    left += mass_of((double)p[j][e] - (double)q[j][e]);
-                }
-            target = wave_sum(target);
-            left = wave_sum(left);
-            if (lane == 0) a.sums[b * a.segments + s] = Mass{left, target};
+            const Mass m = sum_segment(a, rows, s);
+            if (lane == 0) a.sums[b * a.segments + s] = m;
         }
     }
 }
 
-// A wave a sequence: the segment of the draw's place, the element in it, the outputs.
+// A wave a sequence
 template <class T>
 __global__ __launch_bounds__(kWave) void verify_draw_kernel(VerifyArgs a)
 {
-    const int32_t lane = (int32_t)threadIdx.x;
     for (int64_t b = blockIdx.x; b < a.sequences; b += gridDim.x) {
         const int2 found = a.found[b];
-        const double u = (double)a.draw_u[b];
-        const Mass* sums = a.sums + b * a.segments;
-        double left = 0.0, target = 0.0;
-        for (int32_t s = lane; s < a.segments; s += kWave) {
-            left += sums[s].left;
-            target += sums[s].target;
-        }
-        left = wave_sum(left);
-        target = wave_sum(target);
-        DrawRows<T> rows(a, b, found.x, found.y);
-        const bool whole = !(left > 0.0);
-        if (whole) rows.q = nullptr;
-        const double place = u * (whole ? target : left);
-        // 64 sums at a time, in order
-        double before = 0.0;
-        int32_t segment = -1, last = -1;
-        for (int32_t s0 = 0; s0 < a.segments && segment < 0; s0 += kWave) {
-            const int32_t s = s0 + lane;
-            const double own = s < a.segments ? (whole ? sums[s].target : sums[s].left) : 0.0;
-            const double sum = wave_prefix(own);
-            const uint64_t some = __ballot(own > 0.0);
-            const uint64_t past = __ballot(own > 0.0 && before + sum > place);
-            if (some) last = s0 + 63 - (int32_t)__builtin_clzll(some);
-            if (past) {
-                const int at = __builtin_ctzll(past);
-                segment = s0 + at;
-                before += lane_value(sum - own, at);
-            } else {
-                before += lane_value(sum, kWave - 1);
-            }
-        }
-        const bool inside = segment >= 0;
-        if (!inside) segment = last;  // the last element of any mass
-        int64_t token = -1;
-        if (segment >= 0) {
-            const int64_t v = (int64_t)segment * kSegment + lane * kEach;
-            float p[kEach], q[kEach] = {};
-            load_run<T, kEach>(rows.p, v, a.V, p);
-            if (rows.q) load_run<T, kEach>(rows.q, v, a.V, q);
-            double mass[kEach], sum = 0.0;
-#pragma unroll
-            for (int e = 0; e < kEach; ++e) {
-                mass[e] = mass_of((double)p[e] - (double)q[e]);
-                sum += mass[e];
-            }
-            const double upto = wave_prefix(sum);
-            int32_t hit, most;
-            look_through(mass, before + (upto - sum), place, hit, most);
-            const uint64_t hits = __ballot(inside && hit >= 0), some = __ballot(most >= 0);
-            if (hits) {
-                const int at = __builtin_ctzll(hits);
-                token = (int64_t)segment * kSegment + at * kEach + __shfl(hit, at, kWave);
-            } else if (some) {
-                const int at = 63 - (int)__builtin_clzll(some);
-                token = (int64_t)segment * kSegment + at * kEach + __shfl(most, at, kWave);
-            }
-        }
-        write_result(a, b, found.x, token, lane, kWave);
+        const DrawRows<T> rows(a, b, found.x, found.y);
+        const int64_t token = draw(a, rows, a.sums + b * a.segments, (double)a.draw_u[b]);
+        write_result(a, b, found.x, token, (int32_t)threadIdx.x, kWave);
     }
 }
 
@@ -311,10 +340,17 @@ static int64_t verify_segments(const lda_draft_rows* d)
 {
     return d->classes <= kDirectClasses ? 0 : ((int64_t)d->classes + kSegment - 1) / kSegment;
 }
+// One launch costs the host some 4 us less than two, and rows of up to 80 KB take a workgroup hardly longer
+// than the two kernels (20000 f32, 2 steps: 1 sequence 8.1 us, in two 7.3; 64: 10.7 and 9.4; 256: 12.9 and 13.2; but
+// 512: 23 and 20; 60000 f32, 64 sequences: 18 and 11).
+static bool row_in_one(const lda_draft_rows* d)
+{
+    return (int64_t)d->classes * (int64_t)type_bytes(d->probs_type) <= kRowBytes && d->sequences <= 256;
+}
 static int64_t verify_bytes(const lda_draft_rows* d)
 {
     const int64_t segments = verify_segments(d);
-    return segments == 0 ? 0 : d->sequences * (segments * (int64_t)sizeof(Mass) + (int64_t)sizeof(int2));
+    return segments == 0 || row_in_one(d) ? 0 : d->sequences * (segments * (int64_t)sizeof(Mass) + (int64_t)sizeof(int2));
 }
 
 static int check_verify(const lda_draft_rows* d, const char* call)
@@ -344,6 +380,10 @@ static void launch_verify_typed(VerifyArgs& a, hipStream_t stream)
     const unsigned gx = (unsigned)(a.sequences < (1 << 20) ? a.sequences : (1 << 20));
     if (a.segments == 0) {
         verify_direct_kernel<T><<<gx, kVerifyBlock, 0, stream>>>(a);
+        return;
+    }
+    if (a.sums == nullptr) {
+        verify_row_kernel<T><<<gx, kRowBlock, 0, stream>>>(a);
         return;
     }
     // some 8 workgroups a CU, as every wave begins with the accept tests
@@ -405,8 +445,10 @@ try {
     const int64_t need = verify_bytes(d);
     if (need > 0 && (!d->workspace || d->workspace_bytes < need || !aligned_to(d->workspace, 16)))
         return fail(nullptr, LDA_ERR_ARG, "%s: needs a workspace of %lld bytes, aligned to 16", call, (long long)need);
-    a.sums = static_cast<Mass*>(d->workspace);
-    a.found = reinterpret_cast<int2*>(a.sums + a.sequences * a.segments);
+    if (need > 0) {
+        a.sums = static_cast<Mass*>(d->workspace);
+        a.found = reinterpret_cast<int2*>(a.sums + a.sequences * a.segments);
+    }
     a.accepted = accepted;
     a.out = out;
     a.out_stride = out_stride;
