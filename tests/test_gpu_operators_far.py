@@ -1,0 +1,59 @@
+"""The operators on rows where positions pass 31 and 32 bits, with what is far against the same data near."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ops():
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_1412_1576_amd import operators
+    return operators
+
+
+def test_distillation_rows_far_into_memory(ops):
+    n, v, k = 15_500, 141_043, 7    # 2.19 * 10^9 logits
+    x = torch.zeros(n, v, dtype=torch.bfloat16, device="cuda")
+    ids = torch.randint(0, v, (n, k), device="cuda")
+    t = torch.randn(n, k, device="cuda")
+    x[-3:] = torch.randn(3, v, device="cuda").to(x.dtype)
+    loss, grad = ops.distill_loss_and_grad(x, ids, t)
+    near = ops.distill_loss_and_grad(x[-200:].clone(), ids[-200:], t[-200:])   # the same kernel
+    assert torch.equal(loss[-200:], near[0]) and torch.equal(grad[-200:], near[1])
+    leaf = x.requires_grad_(True)
+    loss = ops.distill_loss(leaf, ids, t)
+    got, = torch.autograd.grad(loss, leaf, torch.ones_like(loss))
+    part = x.detach()[-200:].clone().requires_grad_(True)
+    loss_near = ops.distill_loss(part, ids[-200:], t[-200:])
+    want, = torch.autograd.grad(loss_near, part, torch.ones_like(loss_near))
+    assert torch.equal(loss.detach()[-200:], loss_near.detach()) and torch.equal(got[-200:], want)
+
+
+def test_sequences_far_apart(ops):
+    t, v, stride = 3, 30_011, (1 << 32) + 5
+    g = torch.Generator().manual_seed(1)
+    target = torch.softmax(torch.randn(2, t + 1, v, generator=g) * 2, 2).bfloat16().cuda()
+    draft = torch.softmax(torch.randn(2, t, v, generator=g) * 2, 2).bfloat16().cuda()
+    tokens = torch.multinomial(draft.float().cpu().view(2 * t, v), 1, generator=g).view(2, t).cuda()
+    u, d = torch.rand(2, t, generator=g).cuda(), torch.rand(2, generator=g).cuda()
+    store = torch.zeros(stride + (t + 1) * v, dtype=torch.bfloat16, device="cuda")
+    far = store.as_strided((2, t + 1, v), (stride, v, 1))
+    far.copy_(target)
+    want = ops.verify_drafts(target, draft, tokens, u, d)
+    got = ops.verify_drafts(far, draft, tokens, u, d)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_documents_far_into_an_assignment(ops):
+    n = (1 << 31) + 300_000
+    z = torch.full((n,), 5, dtype=torch.int32, device="cuda")
+    z[-200_000:] = torch.randint(0, 40_000, (200_000,), dtype=torch.int32, device="cuda")
+    ends = torch.tensor([0, 90, 4_000, 24_000, 200_000], device="cuda")
+    near = ops.top_topics(z[-200_000:].clone(), ends, 40_000, 30, 0.1)
+    far = ops.top_topics(z, ends + (n - 200_000), 40_000, 30, 0.1)
+    for a, b in zip(far, near):
+        assert torch.equal(a, b)
+    # a document of 2^31 + 300000 tokens is cut at 2^31 - 1
+    ids, logits, norm = ops.top_topics(z, torch.tensor([0, n], device="cuda"), 40_000, 2, 0.1)
+    assert ids[0, 0] == 5 and abs(float(logits[0, 0].exp()) / (2 ** 31 - 1) - 1) < 1e-5
