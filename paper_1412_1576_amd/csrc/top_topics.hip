@@ -82,11 +82,6 @@ __device__ __forceinline__ void document_of(const TopicArgs& a, int64_t row, int
     g1 = min(g1, g0 + INT32_MAX);
 }
 
-// One document's counts in a table of 2 kWaveTopics keys (0: empty), and its best k topics, by one wave.
-// `used` has room for kWaveTopics slots; the table is empty before and after.  A key has the topic, inverted
-// within the bits that K takes, below the count.  `next` holds the document's first tokens; all_read()
-// is called when they are read, for the next document's to be on their way while this one's topics are chosen.
-// Returns the number of tokens counted, -1 if there are too many topics.
 constexpr int kAhead = 4;  // rounds of 64 tokens that are read ahead
 __device__ __forceinline__ void first_tokens(const int32_t* z, int32_t L, int32_t (&next)[kAhead])
 {
@@ -95,6 +90,11 @@ __device__ __forceinline__ void first_tokens(const int32_t* z, int32_t L, int32_
     for (int e = 0; e < kAhead; ++e) next[e] = e * kWave + lane < L ? z[e * kWave + lane] : -1;
 }
 
+// One document's counts in a table of 2 kWaveTopics keys (0: empty), and its best k topics, by one wave.
+// `used` has room for kWaveTopics slots; the table is empty before and after.  A key has the topic, inverted
+// within the bits that K takes, below the count.  `next` holds the document's first tokens; all_read()
+// is called when they are read, for the next document's to be on their way while this one's topics are chosen.
+// Returns the number of tokens counted, -1 if there are too many topics.
 template <class Read, class LogCount>
 __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t row, const int32_t* z, int32_t L, int32_t (&next)[kAhead],
                                                   uint32_t* table, uint16_t* used, Read all_read, LogCount log_count)
@@ -253,6 +253,10 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
     return counted;
 }
 
+// Bound by the number of instructions: 300 000 documents of 330 tokens in 1000 topics, 32 slots, take 400 us (1.2 TB/s of
+// z and outputs), some 280 vector and 550 scalar instructions a document, more than one in every issue
+// slot of the SIMDs.  (Ranking all keys instead of finding a border first, 530 vector and 440 scalar: 407 us.)
+// 100 000 documents of 100 tokens in 10 000 topics: 105 us.
 __global__ __launch_bounds__(kWaveBlock, 6) void wave_topics_kernel(TopicArgs a)
 {
     constexpr int kWaves = kWaveBlock / kWave;
@@ -757,7 +761,9 @@ __device__ __forceinline__ void topics_by_counters(const TopicArgs& a, int64_t r
     write_keys(a, row, lds.best, n_best, counted);
 }
 
-// The ranges of the documents that are split, a workgroup each
+// The ranges of the documents that are split, a workgroup each.  A document of 440 000 tokens in 100 000 topics: 100 us
+// for all that it takes (340 with its four ranges one after the other); counting takes 75 us of them, some
+// 25 instructions a round of 64 tokens on the four SIMDs of one CU.
 __global__ __launch_bounds__(kLongBlock) void range_topics_kernel(TopicArgs a)
 {
     extern __shared__ __align__(16) unsigned char raw[];
