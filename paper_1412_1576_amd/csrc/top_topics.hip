@@ -502,22 +502,14 @@ __device__ __forceinline__ uint32_t bucket_of(uint32_t c)
 
 // The k-th largest count (0: there are no more than k), into `ties` how many of the topics that have it
 // are among the best k, into `equal` how many of them this thread has.  each(f) calls f(count) for the
-// thread's share.
-template <class Each>
-__device__ __forceinline__ uint32_t least_count(LongLds& lds, int32_t k, int32_t& ties, int32_t& equal, Each each)
+// thread's share; first(few, f) the same for counts above 3 only, and counts those of 1, 2 and 3.
+template <class First, class Each>
+__device__ __forceinline__ uint32_t least_count(LongLds& lds, int32_t k, int32_t& ties, int32_t& equal, First first, Each each)
 {
     // most topics have a few tokens: their buckets would be everybody's
     int32_t few[3] = {0, 0, 0};
     clear_histogram(lds);
-    each([&](uint32_t c) {
-        if (c <= 3) {
-            few[0] += c == 1;
-            few[1] += c == 2;
-            few[2] += c == 3;
-        } else {
-            atomicAdd(&lds.histogram[bucket_of(c)], 1u);
-        }
-    });
+    first(few, [&](uint32_t c) { atomicAdd(&lds.histogram[bucket_of(c)], 1u); });
 #pragma unroll
     for (int q = 0; q < 3; ++q) {
         const int32_t n = wave_sum(few[q]);
@@ -626,7 +618,17 @@ __device__ __forceinline__ bool topics_by_table(const TopicArgs& a, int64_t row,
         }
     };
     int32_t ties, equal;
-    const uint32_t least = least_count(lds, a.k, ties, equal, [&](auto f) { each([&](uint32_t c, uint32_t) { f(c); }); });
+    const uint32_t least = least_count(
+        lds, a.k, ties, equal,
+        [&](int32_t(&few)[3], auto f) {
+            each([&](uint32_t c, uint32_t) {
+                few[0] += c == 1;
+                few[1] += c == 2;
+                few[2] += c == 3;
+                if (c > 3) f(c);
+            });
+        },
+        [&](auto f) { each([&](uint32_t c, uint32_t) { f(c); }); });
     uint32_t after = 0;  // of the topics with the least count, those whose inverse is at least this
     if (least > 0) {
         after = nth_largest(lds, (int32_t)kMixTopicBits, ties, [&](auto f) {
@@ -728,20 +730,44 @@ __device__ __forceinline__ int32_t best_of_range(const TopicArgs& a, const int32
     for (int q = 0; q < HotTopics::kHot; ++q)
         if (hot.tokens[q] > 0 && tid % kWave == 0) count((uint32_t)hot.topic[q], (uint32_t)hot.tokens[q]);
     __syncthreads();
+    const auto parts = [&](uint32_t w, uint32_t& low, uint32_t& high) {
+        low = WIDE ? w : w & 0xFFFFu;
+        high = WIDE ? 0u : w >> 16;
+    };
     // topics come in ascending order: ties go to the first
     int32_t ties, equal, total;
-    const uint32_t least = least_count(lds, a.k, ties, equal, [&](auto f) {
-        each([&](uint32_t c, int32_t) {
-            f(c);
-        });
-    });
-    int32_t before = least > 0 ? block_prefix<kLongBlock>(equal, lds.part, total) : 0;
+    const uint32_t least = least_count(
+        lds, a.k, ties, equal,
+        [&](int32_t(&few)[3], auto f) {
+#pragma unroll 2
+            for (int32_t j = 0; j < each_words; ++j) {  // without a branch for the many words of nothing or little
+                uint32_t low, high;
+                parts(own[j], low, high);
+#pragma unroll
+                for (uint32_t q = 0; q < 3; ++q) few[q] += (int32_t)(low == q + 1) + (int32_t)(high == q + 1);
+                if (max(low, high) > 3) {
+                    if (low > 3) f(low);
+                    if (high > 3) f(high);
+                }
+            }
+        },
+        [&](auto f) { each([&](uint32_t c, int32_t) { f(c); }); });
+    const int32_t before = least > 0 ? block_prefix<kLongBlock>(equal, lds.part, total) : 0;
+    int32_t take = min(max(ties - before, 0), equal);  // of the thread's topics with the least count
     __syncthreads();
     if (tid == 0) lds.n_keys = n_first;
     __syncthreads();
-    each([&](uint32_t c, int32_t t) {
-        if (c > least || (c == least && before++ < ties)) lds.keys[atomicAdd(&lds.n_keys, 1)] = long_key(c, t0 + t);
-    });
+    const uint32_t from = least > 0 && take > 0 ? least : least + 1;
+#pragma unroll 2
+    for (int32_t j = 0; j < each_words; ++j) {
+        uint32_t c[2];
+        parts(own[j], c[0], c[1]);
+        if (max(c[0], c[1]) < from) continue;
+        for (int32_t q = 0; q < kPer; ++q) {
+            if (c[q] > least || (c[q] == least && least > 0 && take-- > 0))
+                lds.keys[atomicAdd(&lds.n_keys, 1)] = long_key(c[q], t0 + (tid * each_words + j) * kPer + q);
+        }
+    }
     __syncthreads();
     return counted;
 }
