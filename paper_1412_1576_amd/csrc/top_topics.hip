@@ -11,6 +11,8 @@
 //   Of the longest documents every range is a workgroup's, and their best are put together afterwards, where
 //     the caller has given a workspace for that.
 // The first kernel leaves marks in the rows that the others have to take.
+#include <algorithm>
+
 #include "rows.hpp"
 
 namespace lda {
@@ -898,11 +900,11 @@ static int launch_top_topics(lda_ctx* c, const TopicArgs& a, hipStream_t stream)
         if (a.places > 0) {
             LDA_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(range_topics_kernel),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(LongLds)));
-            range_topics_kernel<<<256, kLongBlock, sizeof(LongLds), stream>>>(a);
+            range_topics_kernel<<<(unsigned)std::min<int64_t>((int64_t)a.places * a.ranges, 1024), kLongBlock, sizeof(LongLds), stream>>>(a);
         }
         LDA_HIP(c, hipFuncSetAttribute(reinterpret_cast<const void*>(long_topics_kernel),
                                        hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(LongLds)));
-        long_topics_kernel<<<grid(1, 256), kLongBlock, sizeof(LongLds), stream>>>(a);
+        long_topics_kernel<<<a.rows <= 1024 ? (unsigned)a.rows : 256u, kLongBlock, sizeof(LongLds), stream>>>(a);
     }
     LDA_HIP(c, hipGetLastError());
     return LDA_OK;
