@@ -117,44 +117,45 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
         }
         // the rounds' look-ups side by side: one after the other they would wait for LDS each
         int32_t mine[kAhead];
-        bool open[kAhead];
-#pragma unroll
-        for (int e = 0; e < kAhead; ++e) {
-            open[e] = (uint32_t)topic[e] < (uint32_t)a.K;
-            counted += (int32_t)__popcll(__ballot(open[e]));
-            mine[e] = -1;
-        }
         if (a.K <= kSlots) {  // a slot a topic: no search
             uint32_t was[kAhead];
 #pragma unroll
-            for (int e = 0; e < kAhead; ++e) was[e] = open[e] ? atomicAdd(&table[topic[e]], one) : 1u;
+            for (int e = 0; e < kAhead; ++e) {
+                const bool open = (uint32_t)topic[e] < (uint32_t)a.K;
+                counted += (int32_t)__popcll(__ballot(open));
+                was[e] = open ? atomicAdd(&table[topic[e]], one) : 1u;
+            }
 #pragma unroll
-            for (int e = 0; e < kAhead; ++e)
-                if (was[e] == 0) mine[e] = topic[e];
+            for (int e = 0; e < kAhead; ++e) mine[e] = was[e] == 0 ? topic[e] : -1;
         } else {
-            uint32_t h[kAhead];
+            int32_t h[kAhead];  // -1: found
 #pragma unroll
-            for (int e = 0; e < kAhead; ++e) h[e] = ((uint32_t)topic[e] * 0x9E3779B1u) >> (32 - __builtin_ctz(kSlots));
+            for (int e = 0; e < kAhead; ++e) {
+                const bool open = (uint32_t)topic[e] < (uint32_t)a.K;
+                counted += (int32_t)__popcll(__ballot(open));
+                h[e] = open ? (int32_t)(((uint32_t)topic[e] * 0x9E3779B1u) >> (32 - __builtin_ctz(kSlots))) : -1;
+                mine[e] = -1;
+            }
             // half the slots stay empty: every search ends
-            while (__ballot(open[0] || open[1] || open[2] || open[3])) {
+            while (__ballot(max(max(h[0], h[1]), max(h[2], h[3])) >= 0)) {
                 uint32_t v[kAhead];
 #pragma unroll
-                for (int e = 0; e < kAhead; ++e) v[e] = open[e] ? table[h[e]] : 1u;
+                for (int e = 0; e < kAhead; ++e) v[e] = table[max(h[e], 0)];
 #pragma unroll
                 for (int e = 0; e < kAhead; ++e)
-                    if (v[e] == 0) {
+                    if (h[e] >= 0 && v[e] == 0) {
                         v[e] = atomicCAS(&table[h[e]], 0u, one | (inverted - (uint32_t)topic[e]));
                         if (v[e] == 0) {
-                            mine[e] = (int32_t)h[e];
-                            open[e] = false;
+                            mine[e] = h[e];
+                            h[e] = -1;
                         }
                     }
 #pragma unroll
                 for (int e = 0; e < kAhead; ++e)
-                    if (open[e]) {
+                    if (h[e] >= 0) {
                         if ((v[e] & inverted) == inverted - (uint32_t)topic[e]) {
                             atomicAdd(&table[h[e]], one);
-                            open[e] = false;
+                            h[e] = -1;
                         } else {
                             h[e] = (h[e] + 1) & (kSlots - 1);
                         }
@@ -195,22 +196,20 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
     if (n > kWave && n > a.k) {
         // too many to rank them all: a border below which lie all but k, bit by bit
         least = 0;
-        const int top = 31 - __builtin_clz((uint32_t)L) + (int)bits;
+        uint32_t step = one << (31 - __builtin_clz((uint32_t)L));
         if (n <= 2 * kWave) {  // most documents
-            for (int bit = top; bit >= 0; --bit) {
-                const uint32_t at = least | (1u << bit);
+            for (; step != 0; step >>= 1) {
+                const uint32_t at = least | step;
                 const int32_t above = (int32_t)__popcll(__ballot(key[0] >= at)) + (int32_t)__popcll(__ballot(key[1] >= at));
-                if (above >= a.k) least = at;
-                if (above == a.k) break;
+                least = above >= a.k ? at : least;
             }
         } else {
-            for (int bit = top; bit >= 0; --bit) {
-                const uint32_t at = least | (1u << bit);
+            for (; step != 0; step >>= 1) {
+                const uint32_t at = least | step;
                 int32_t above = 0;
 #pragma unroll
                 for (int e = 0; e < kEach; ++e) above += (int32_t)__popcll(__ballot(key[e] >= at));
-                if (above >= a.k) least = at;
-                if (above == a.k) break;
+                least = above >= a.k ? at : least;
             }
         }
         n_best = a.k;
