@@ -266,15 +266,19 @@ def doc_topics(sampler, slots, docs=None):
     if docs is not None:
         _tensor(docs, "docs", 1, (torch.int32,), device)
     n = sampler.D if docs is None else docs.numel()
-    current = torch.cuda.current_stream(device)
-    own = torch.cuda.ExternalStream(sampler.stream, device=device) if sampler.stream else \
-        torch.cuda.default_stream(device)
+    apart = _raw_stream(device) != sampler.stream
+    if apart and torch.cuda.is_current_stream_capturing():
+        raise ValueError("doc_topics in a captured stream: only where it is the sampler's own stream")
+    if apart:
+        current = torch.cuda.current_stream(device)
+        own = torch.cuda.ExternalStream(sampler.stream, device=device) if sampler.stream else \
+            torch.cuda.default_stream(device)
     ids, logits, log_norm = _teacher_rows(n, max(slots, 0), device)
-    if own != current:  # docs may still be on their way, and the outputs' memory in use
+    if apart:  # docs may still be on their way, and the outputs' memory in use
         own.wait_stream(current)
     sampler._ck(lda.load_library().lda_doc_topics(
         sampler._h, n, None if docs is None else docs.data_ptr(), slots, ids.data_ptr(),
         logits.data_ptr(), log_norm.data_ptr()))
-    if own != current:
+    if apart:
         current.wait_stream(own)
     return ids, logits, log_norm

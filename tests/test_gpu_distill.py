@@ -80,6 +80,9 @@ def bounds(x, tau, sizes, q, P, weight, dtype, out):
         w = np.ones(len(x)) if weight is None else np.abs(weight)
         mq = P.sum(1, keepdims=True) * q
         grad = w[:, None] * tau * (mq * rel + 8 * U * (P + mq))
+        # an exponential below the smallest normal number of 32 bits keeps fewer bits or is 0: off by that number
+        # at most, times T w M / s with s >= 1 (the base of the sum is one of its logits)
+        grad = grad + w[:, None] * tau * np.maximum(P.sum(1, keepdims=True), 1.0) * 2.0 ** -126
         half = torch.finfo(dtype).eps / 2
         # (half a step below the smallest normal number too)
         grad = grad + np.abs(out) * half * 1.01 + torch.finfo(dtype).smallest_normal * 2 * half
@@ -263,6 +266,42 @@ def test_masked_and_odd_logits(ops):
     check(ops, y, ids[:2], u, log_norm=norm[:2])
 
 
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("V,times", [(3000, 1), (10_001, 1), (20_001, 1), (30_001, 1), (30_001, 6), (60_003, 11)])
+def test_masked_and_odd_logits_of_longer_rows(ops, V, times, rest):
+    """The same through a workgroup's registers of every shape, and through slices; masks that leave a
+    slice, or all but one, without anything."""
+    inf, low = float("inf"), torch.finfo(torch.float32).min
+    x, ids, t = make(10, V, 6, torch.float32, seed=V)
+    ids = torch.tensor([0, 1, 2, V // 2, V - 2, V - 1], device="cuda").expand(10, 6).contiguous()
+    x[0, : V // 2] = low
+    x[1, 10:] = low
+    x[2, :] = low
+    x[3, :] = -inf
+    x[4, 2] = -inf
+    x[5, V // 3] = float("nan")
+    x[6, V - 7] = inf
+    x[7, 20: V - 20] = -inf
+    x[8, :] = -inf
+    x[8, V // 2] = 1.0
+    x[9, V // 5] = float("nan")
+    ids[9] = -1
+    t.clamp_(max=2.0)
+    norm = torch.full((10,), 4.0, device="cuda") if rest else None
+    if times == 1:
+        check(ops, x, ids, t, log_norm=norm)
+        return
+    # more rows take another kernel: the rows are those of the first ten
+    want = ops.distill_loss_and_grad(x, ids, t, log_norm=norm)
+    got = ops.distill_loss_and_grad(x.repeat(times, 1), ids.repeat(times, 1), t.repeat(times, 1),
+                                    log_norm=None if norm is None else norm.repeat(times))
+    for g, w in zip(got, want):
+        g, w = g.view(times, *w.shape), w.expand(times, *w.shape)
+        assert torch.equal(g.isnan(), w.isnan()) and torch.equal(g.isinf(), w.isinf())
+        some = torch.isfinite(w)
+        assert torch.allclose(g[some], w[some], rtol=1e-5, atol=1e-7)
+
+
 def test_weights(ops):
     x, ids, t = make(9, 300, 10, torch.float32, seed=7)
     x[2] = float("nan")
@@ -404,3 +443,27 @@ def test_the_backward_captured(ops):
         torch.cuda.synchronize()
         lw, gw = ops.distill_loss_and_grad(leaf.detach(), ids, t, weight=w)
         assert torch.equal(loss.detach(), lw) and torch.equal(grad, gw)
+
+
+@pytest.mark.parametrize("tau", [1 / 1024, 0.05, 30.0, 1024.0])
+@pytest.mark.parametrize("rest", [False, True])
+def test_temperatures(ops, tau, rest):
+    x, ids, t = make(5, 3001, 40, torch.float32, seed=15)
+    norm = None
+    if rest:
+        norm = (torch.logsumexp(t.double() / tau, 1) + 0.4).float()
+        # (a norm of thousands is itself good to 2^-24 of that only: the masses are those of the float)
+    check(ops, x, ids, t, tau=tau, log_norm=norm)
+
+
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("V,k", [(100, 1024), (1000, 1000), (3000, 700), (30_000, 1024)])
+def test_many_slots_of_few_classes(ops, V, k, rest):
+    """More slots than threads, most classes several times, some slots empty."""
+    x, ids, t = make(3, V, min(k, V), torch.float32, seed=16)
+    g = torch.Generator().manual_seed(V)
+    ids = torch.randint(-20, min(V, 300) + 20, (3, k), generator=g).cuda()
+    t = torch.randn(3, k, generator=g).cuda()
+    full = torch.where((ids >= 0) & (ids < V), t.double(), -torch.inf)
+    norm = (torch.logsumexp(full, 1) + 0.3).float() if rest else None
+    check(ops, x, ids, t, log_norm=norm)

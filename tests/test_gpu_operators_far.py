@@ -57,3 +57,29 @@ def test_documents_far_into_an_assignment(ops):
     # a document of 2^31 + 300000 tokens is cut at 2^31 - 1
     ids, logits, norm = ops.top_topics(z, torch.tensor([0, n], device="cuda"), 40_000, 2, 0.1)
     assert ids[0, 0] == 5 and abs(float(logits[0, 0].exp()) / (2 ** 31 - 1) - 1) < 1e-5
+
+
+def test_more_rows_than_a_launch_has(ops):
+    n, v = (1 << 20) + 5, 9
+    x = torch.randn(n, v, device="cuda")
+    ids, t = torch.randint(-1, v, (n, 3), device="cuda"), torch.randn(n, 3, device="cuda")
+    loss, grad = ops.distill_loss_and_grad(x, ids, t)
+    y = torch.log_softmax(x.double(), 1)
+    p = torch.softmax(torch.where(ids >= 0, t.double(), -torch.inf), 1).nan_to_num(0.0)
+    want = torch.where(p > 0, p * (p.log() - y.gather(1, ids.clamp(min=0))), 0.0).sum(1)
+    assert (loss - want).abs().max() <= 64 * 2.0 ** -24 * 10   # logarithms below 10, some tens of roundings
+    q = torch.zeros_like(y).scatter_add_(1, ids.clamp(min=0), p)
+    want = (p.sum(1, keepdim=True) * y.exp() - q)
+    assert (grad - want).abs().max() <= 64 * 2.0 ** -24
+
+
+@pytest.mark.parametrize("v", [7, 5_000])
+def test_more_sequences_than_a_launch_has(ops, v):
+    n = (1 << 20) + 5
+    p = torch.softmax(torch.randn(1, 1, v, device="cuda") * 2, 2)
+    u = torch.rand(n, device="cuda")
+    none = torch.zeros(n, 0, device="cuda")
+    accepted, out = ops.verify_drafts(p.expand(n, 1, v), p[:, :0].expand(n, 0, v), none.long(), none, u)
+    c = p[0, 0].double().cumsum(0)
+    want = torch.searchsorted(c, u.double() * c[-1], right=True).clamp_(max=v - 1)
+    assert (accepted == 0).all() and torch.equal(out[:, 0], want)

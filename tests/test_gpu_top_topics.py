@@ -263,3 +263,30 @@ def test_any_workspace_gives_the_same(ops, K):
         torch.cuda.synchronize()
         same([x[:n] for x in out], want)
         assert all((x[n:] == -77).all() for x in out) and (w[nbytes:] == 255).all()
+
+
+def test_a_sampler_captured(ops):
+    """On the sampler's own stream the call is captured and replayed; on another one it is refused."""
+    from paper_1412_1576_amd import corpus, lda
+    cfg = corpus.scaled(corpus.CONFIGS["c1"], D=150)
+    doff, words = corpus.make_corpus(cfg)
+    stream, other = torch.cuda.Stream(), torch.cuda.Stream()
+    m = lda.Lda(doff, words, cfg.V, cfg.K, cfg.alpha, cfg.beta, seed=4, stream=stream.cuda_stream)
+    docs = torch.tensor([3, 0, 149], dtype=torch.int32, device="cuda")
+    with torch.cuda.stream(stream):
+        m.doc_topics(10, docs)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        got = m.doc_topics(10, docs)
+    for picked in ([3, 0, 149], [7, 7, 8], [100, -1, 150]):
+        docs.copy_(torch.tensor(picked, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        same(got, reference(m.get_z(), doff, cfg.K, 10, cfg.alpha, picked))
+    with pytest.raises(ValueError, match="captured"):
+        with torch.cuda.graph(torch.cuda.CUDAGraph(), stream=other):
+            m.doc_topics(10, docs)
+    torch.cuda.synchronize()
+    same(m.doc_topics(10, docs), reference(m.get_z(), doff, cfg.K, 10, cfg.alpha, [100, -1, 150]))
+    m.close()
