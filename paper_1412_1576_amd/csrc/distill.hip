@@ -21,12 +21,12 @@ constexpr int32_t kSliceChunks = kPartBlock * kSliceLoads;    // 32 KB
 constexpr int32_t kStatFloats = 8;
 constexpr float kFar = 16.0f;  // a base is left where it is until a logit exceeds it by this, in powers of 2
 
-// What a slice of a row tells about its softmax.  scaled_sum (of c S over the finite logits) and
-// ninf (the logits of -infinity) are only there where the teacher has a floor.
+// What a slice of a row tells about its softmax.  scaled_sum (of c (S - m) over the logits above -infinity) and
+// n (their number) are only there where the teacher has a floor.
 struct RowPart {
     float m, s;
     double scaled_sum;
-    int32_t ninf, pad;
+    int32_t n, pad;
 };
 
 // What the slots say: masses are exp(t / T - z), their sum; the floor of the other classes and their
@@ -101,6 +101,13 @@ __device__ __forceinline__ void block_join(float& m, float& s, float c, float2* 
     for (int w = 1; w < BLOCK / kWave; ++w) join(m, s, part[w].x, part[w].y, c);
 }
 
+// What a sum of c (S - from) over n logits is with another base.  Sums of the logits themselves would lose
+// everything in a row of the type's lowest value, whose differences are 0.
+__device__ __forceinline__ double rebased(double scaled_sum, int32_t n, float from, float to, float c)
+{
+    return n > 0 ? scaled_sum + (double)n * (((double)from - (double)to) * (double)c) : scaled_sum;
+}
+
 // A row as the whole 16-byte chunks of memory inside it, and the elements before and behind
 // those (fewer than two chunks), which a thread each takes.
 template <class T>
@@ -127,7 +134,7 @@ struct Running {
     static constexpr int E = Row<T>::kChunk;
     float m = -INFINITY, s = 0.0f;
     double scaled_sum = 0.0;
-    int32_t ninf = 0;
+    int32_t n = 0;
 
     template <int N>
     __device__ __forceinline__ void add(const float (&x)[N], float c)
@@ -137,6 +144,7 @@ struct Running {
         for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
         if ((top - m) * c > kFar) {
             s *= exp_above(m, top, c);
+            if (REST) scaled_sum = rebased(scaled_sum, n, m, top, c);
             m = top;
         }
         const float base = base_of(m);
@@ -155,12 +163,14 @@ struct Running {
                 ysum += y[e];
             }
             if (least > -INFINITY) {
-                scaled_sum += (double)ysum + (double)N * ((double)base * (double)c);
+                scaled_sum += (double)ysum;
+                n += N;
             } else {
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    if (x[e] == -INFINITY) ++ninf;
-                    else scaled_sum += (double)x[e] * (double)c;
+                    if (x[e] == -INFINITY) continue;
+                    scaled_sum += ((double)x[e] - (double)base) * (double)c;
+                    ++n;
                 }
             }
         }
@@ -282,10 +292,10 @@ __device__ __forceinline__ void store_chunk(T* g, const float (&x)[Row<T>::kChun
 }
 
 // A thread's share of a row's loss: sum of p (log p - log q) over the slots; and where there is a floor, what
-// lies beside them: c S over the finite logits, and how many are -infinity.
+// lies beside them: c (S - m) over the logits above -infinity, and their number.
 struct LossSums {
     double slots, beside;
-    int32_t ninf;
+    int32_t n;
 
     __device__ __forceinline__ void add_slot(float p, float t, float x, double z, double base, double inv_t, double log_s)
     {
@@ -293,10 +303,11 @@ struct LossSums {
         const double log_q = x == -INFINITY ? -(double)INFINITY : ((double)x - base) * inv_t - log_s;
         slots += (double)p * ((double)t * inv_t - z - log_q);
     }
-    __device__ __forceinline__ void leave_out(float x, float c)  // a named class
+    __device__ __forceinline__ void leave_out(float x, float base, float c)  // a named class
     {
-        if (x == -INFINITY) --ninf;
-        else beside -= (double)x * (double)c;
+        if (x == -INFINITY) return;
+        beside -= ((double)x - (double)base) * (double)c;
+        --n;
     }
     template <bool REST, int BLOCK>
     __device__ __forceinline__ void sum(LossSums* part)
@@ -304,7 +315,7 @@ struct LossSums {
         slots = wave_sum(slots);
         if (REST) {
             beside = wave_sum(beside);
-            ninf = wave_sum(ninf);
+            n = wave_sum(n);
         }
         if (BLOCK == kWave) return;
         __syncthreads();
@@ -316,20 +327,20 @@ struct LossSums {
             slots += part[w].slots;
             if (REST) {
                 beside += part[w].beside;
-                ninf += part[w].ninf;
+                n += part[w].n;
             }
         }
     }
 };
 
 template <bool REST>
-__device__ __forceinline__ float loss_of(const DistillArgs& a, const LossSums& l, const TeacherPart& t, float m, float s, double log_s)
+__device__ __forceinline__ float loss_of(const DistillArgs& a, const LossSums& l, const TeacherPart& t, float s, double log_s)
 {
-    const double T = (double)a.T, base = (double)base_of(m);
+    const double T = (double)a.T;
     double sum = l.slots;
     if (REST && t.floor > 0.0) {
-        const double beside = l.beside / ((double)a.c * T) - (double)t.others * base / T;
-        sum += l.ninf > 0 ? (double)INFINITY : t.floor * ((double)t.others * (log(t.floor) + log_s) - beside);
+        const double beside = l.beside / ((double)a.c * T);
+        sum += l.n < t.others ? (double)INFINITY : t.floor * ((double)t.others * (log(t.floor) + log_s) - beside);
     }
     double loss = T * T * sum;
     if (!(s == s) || !(t.mass == t.mass)) loss = (double)NAN;
@@ -391,9 +402,11 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
         if (tid < r.extras) run.add(extra, a.c);
         m = run.m;
         s = run.s;
-        l.beside = run.scaled_sum;
-        l.ninf = run.ninf;
         block_join<BLOCK>(m, s, a.c, part2);
+        if (REST) {
+            l.beside = rebased(run.scaled_sum, run.n, run.m, m, a.c);
+            l.n = run.n;
+        }
     }
     __syncthreads();
     TeacherPart t = *slots.head;
@@ -410,7 +423,7 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
             const bool first = first_of_class(slots, a.k, j, id, all[q]);
             if (REST && first) {
                 ++named;
-                l.leave_out(slots.x[j], a.c);
+                l.leave_out(slots.x[j], base_of(m), a.c);
             }
         }
     }
@@ -453,7 +466,7 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
     }
     l.sum<REST, BLOCK>(parts);
     if (tid == 0) {
-        a.loss[row] = out ? 0.0f : loss_of<REST>(a, l, t, m, s, log_s);
+        a.loss[row] = out ? 0.0f : loss_of<REST>(a, l, t, s, log_s);
         if (a.stats)
             *reinterpret_cast<RowStats*>(a.stats + row * kStatFloats) = RowStats{m, s, (float)mass, (float)t.floor, t.z};
     }
@@ -513,12 +526,13 @@ __global__ __launch_bounds__(kPartBlock) void distill_part_kernel(DistillArgs a)
                 run.add(x, a.c);
             }
         }
+        const float own = run.m;
         block_join<kPartBlock>(run.m, run.s, a.c, part2);
         if (REST) {
-            run.scaled_sum = block_sum<kPartBlock>(run.scaled_sum, partd);
-            run.ninf = block_sum<kPartBlock>(run.ninf, parti);
+            run.scaled_sum = block_sum<kPartBlock>(rebased(run.scaled_sum, run.n, own, run.m, a.c), partd);
+            run.n = block_sum<kPartBlock>(run.n, parti);
         }
-        if (tid == 0) a.parts[row * a.slices + slice] = RowPart{run.m, run.s, run.scaled_sum, run.ninf, 0};
+        if (tid == 0) a.parts[row * a.slices + slice] = RowPart{run.m, run.s, run.scaled_sum, run.n, 0};
     }
 }
 
@@ -540,7 +554,7 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
     bool out = a.grad && w == 0.0f;
     float m = -INFINITY, s = 0.0f, mass = 0.0f, floor = 0.0f;
     double scaled_sum = 0.0, z = 0.0;
-    int32_t ninf = 0;
+    int32_t n = 0;
     TeacherPart t{};
     if (!out) {
         if (a.stats_in) {
@@ -555,15 +569,16 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
             for (int32_t q = lane; q < a.slices; q += kWave) {  // every wave for itself
                 const RowPart part = a.parts[row * a.slices + q];
                 join(m, s, part.m, part.s, a.c);
-                if (REST) {
-                    scaled_sum += part.scaled_sum;
-                    ninf += part.ninf;
-                }
             }
             wave_join(m, s, a.c);
             if (REST) {
+                for (int32_t q = lane; q < a.slices; q += kWave) {
+                    const RowPart part = a.parts[row * a.slices + q];
+                    scaled_sum += rebased(part.scaled_sum, part.n, part.m, m, a.c);
+                    n += part.n;
+                }
                 scaled_sum = wave_sum(scaled_sum);
-                ninf = wave_sum(ninf);
+                n = wave_sum(n);
             }
             mass = (float)(t.mass + t.floor * (double)t.others);
             floor = (float)t.floor;
@@ -594,7 +609,7 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
             const double base = (double)base_of(m);
             if (REST && tid == 0) {
                 l.beside = scaled_sum;
-                l.ninf = ninf;
+                l.n = n;
             }
             for (int32_t j = tid; j < a.k; j += kPartBlock) {
                 const int32_t id = slots.id[j];
@@ -602,12 +617,12 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
                 const float x = Row<T>::one(r.p + id);
                 l.add_slot(slots.p[j], slots.t[j], x, z, base, inv_t, log_s);
                 float all;
-                if (REST && first_of_class(slots, a.k, j, id, all)) l.leave_out(x, a.c);
+                if (REST && first_of_class(slots, a.k, j, id, all)) l.leave_out(x, base_of(m), a.c);
             }
         }
         l.sum<REST, kPartBlock>(parts);
         if (tid == 0) {
-            a.loss[row] = out ? 0.0f : loss_of<REST>(a, l, t, m, s, log_s);
+            a.loss[row] = out ? 0.0f : loss_of<REST>(a, l, t, s, log_s);
             if (a.stats)
                 *reinterpret_cast<RowStats*>(a.stats + row * kStatFloats) = RowStats{m, s, mass, floor, z};
         }
