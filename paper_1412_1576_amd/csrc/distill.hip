@@ -184,6 +184,8 @@ struct Slots {
     float* p;     // mass of the slot
     float* t;     // the teacher's logit
     float* x;     // the student's
+    int32_t* table;  // [2^log2 >= 2 k] for find_twice, with k > kPairs
+    int32_t* twice;
     __device__ __forceinline__ Slots(unsigned char* lds, int32_t k)
     {
         const int32_t n = (k + 3) / 4 * 4;
@@ -192,10 +194,18 @@ struct Slots {
         p = reinterpret_cast<float*>(id + n);
         t = p + n;
         x = t + n;
+        twice = reinterpret_cast<int32_t*>(x + n);
+        table = twice + 1;
     }
 };
 static_assert(sizeof(TeacherPart) % 16 == 0, "vectors behind it");
-inline size_t slots_lds(int32_t k) { return sizeof(TeacherPart) + 16 * ((size_t)(k + 3) / 4 * 4); }
+// Up to so many slots, slots of one class are found by comparing all with all.
+constexpr int32_t kPairs = 64;
+__host__ __device__ __forceinline__ int32_t table_bits(int32_t k) { return 33 - __builtin_clz((uint32_t)k - 1u); }  // k >= 2
+inline size_t slots_lds(int32_t k)
+{
+    return sizeof(TeacherPart) + 16 * ((size_t)(k + 3) / 4 * 4) + (k > kPairs ? 4 + ((size_t)4 << table_bits(k)) : 0);
+}
 
 // One wave's work: ids, logits of both sides and masses of a row's slots.
 template <class T>
@@ -243,10 +253,43 @@ __device__ __forceinline__ void read_teacher(const DistillArgs& a, int64_t row, 
     }
 }
 
+// Does any class have two slots?  The whole workgroup; the answer is the same in every thread.  Nearly
+// always none has, and then no slot needs to look at the others: 256 slots of 4000 rows of 700 classes take 19 us, 41 when
+// they do (8 slots: 14); 64 slots 15.0, by the table 15.6.
+template <int BLOCK>
+__device__ __forceinline__ bool find_twice(const Slots& slots, int32_t k)
+{
+    if (k <= kPairs) return true;  // they may
+    const int32_t tid = (int32_t)threadIdx.x, bits = table_bits(k), size = 1 << bits;
+    for (int32_t i = tid; i < size; i += BLOCK) slots.table[i] = -1;
+    if (tid == 0) *slots.twice = 0;
+    __syncthreads();
+    for (int32_t j = tid; j < k; j += BLOCK) {
+        const int32_t id = slots.id[j];
+        if (id < 0) continue;
+        int32_t h = (int32_t)(((uint32_t)id * 0x9E3779B1u) >> (32 - bits));
+        for (;;) {  // half the table stays empty
+            const int32_t other = atomicCAS(&slots.table[h], -1, id);
+            if (other == -1) break;
+            if (other == id) {
+                atomicOr(slots.twice, 1);
+                break;
+            }
+            h = (h + 1) & (size - 1);
+        }
+    }
+    __syncthreads();
+    return *slots.twice != 0;
+}
+
 // Is slot j the first of its class, and what is the mass of all of them?  Read from LDS by
 // the whole workgroup in step, four at a time.
-__device__ __forceinline__ bool first_of_class(const Slots& slots, int32_t k, int32_t j, int32_t id, float& all)
+__device__ __forceinline__ bool first_of_class(const Slots& slots, bool twice, int32_t k, int32_t j, int32_t id, float& all)
 {
+    if (!twice) {
+        all = slots.p[j];
+        return true;
+    }
     all = 0.0f;
     bool first = true;
     for (int32_t i = 0; i < k; i += 4) {
@@ -413,6 +456,7 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
     float all[kSlotsEach];
     int32_t named = 0;
     if (!out && (REST || a.grad)) {
+        const bool twice = find_twice<BLOCK>(slots, a.k);
 #pragma unroll
         for (int q = 0; q < kSlotsEach; ++q) {
             const int32_t j = q * BLOCK + tid;
@@ -420,7 +464,7 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
             if (q * BLOCK >= a.k) continue;
             const int32_t id = j < a.k ? slots.id[j] : -1;
             if (id < 0) continue;
-            const bool first = first_of_class(slots, a.k, j, id, all[q]);
+            const bool first = first_of_class(slots, twice, a.k, j, id, all[q]);
             if (REST && first) {
                 ++named;
                 l.leave_out(slots.x[j], base_of(m), a.c);
@@ -492,9 +536,10 @@ __global__ __launch_bounds__(kPartBlock) void distill_part_kernel(DistillArgs a)
         __syncthreads();
         int32_t named = 0;
         if (REST) {
+            const bool twice = find_twice<kPartBlock>(slots, a.k);
             for (int32_t j = tid; j < a.k; j += kPartBlock) {
                 float all;
-                if (slots.id[j] >= 0) named += first_of_class(slots, a.k, j, slots.id[j], all);
+                if (slots.id[j] >= 0) named += first_of_class(slots, twice, a.k, j, slots.id[j], all);
             }
             named = block_sum<kPartBlock>(named, parti);
         }
@@ -587,6 +632,7 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
         out = mass == 0.0f;
     }
     const Gradient f(m, s, mass, floor, w, a.T, a.c);
+    bool twice = true;
     if (!out) {
         for (int32_t j = tid; j < (a.k + 3) / 4 * 4; j += kPartBlock) {
             int32_t id = -1;
@@ -601,6 +647,7 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
             slots.p[j] = id >= 0 ? (float)exp((double)tl * inv_t - z) : 0.0f;
         }
         __syncthreads();
+        if (REST || a.grad) twice = find_twice<kPartBlock>(slots, a.k);
     }
     if (a.loss && blockIdx.y == 0) {
         LossSums l{0.0, 0.0, 0};
@@ -617,7 +664,7 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
                 const float x = Row<T>::one(r.p + id);
                 l.add_slot(slots.p[j], slots.t[j], x, z, base, inv_t, log_s);
                 float all;
-                if (REST && first_of_class(slots, a.k, j, id, all)) l.leave_out(x, base_of(m), a.c);
+                if (REST && first_of_class(slots, twice, a.k, j, id, all)) l.leave_out(x, base_of(m), a.c);
             }
         }
         l.sum<REST, kPartBlock>(parts);
@@ -659,7 +706,7 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
                 const int32_t id = slots.id[j];
                 if (id < 0 || !((id >= v0 && id < v1) || (slice == 0 && (id < r.head || id >= r.chunk(r.whole))))) continue;
                 float all;
-                first_of_class(slots, a.k, j, id, all);
+                first_of_class(slots, twice, a.k, j, id, all);
                 g[id] = Row<T>::from(f.slot(Row<T>::one(r.p + id), all));
             }
         }

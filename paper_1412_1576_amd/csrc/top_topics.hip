@@ -254,10 +254,10 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
     return counted;
 }
 
-// Bound by the number of instructions: 300 000 documents of 330 tokens in 1000 topics, 32 slots, take 400 us (1.2 TB/s of
-// z and outputs), some 280 vector and 550 scalar instructions a document, more than one in every issue
-// slot of the SIMDs.  (Ranking all keys instead of finding a border first, 530 vector and 440 scalar: 407 us.)
-// 100 000 documents of 100 tokens in 10 000 topics: 105 us.
+// Bound by the number of instructions: 300 000 documents of 330 tokens in 1000 topics, 32 slots, take 360 us (1.3 TB/s of
+// z and outputs), some 320 vector and 500 scalar instructions a document, more than one in every issue
+// slot of the SIMDs.  (Ranking all keys instead of finding a border first, 530 vector and 440 scalar, was 3 % slower.)
+// 100 000 documents of 100 tokens in 10 000 topics: 98 us.
 __global__ __launch_bounds__(kWaveBlock, 6) void wave_topics_kernel(TopicArgs a)
 {
     constexpr int kWaves = kWaveBlock / kWave;
@@ -790,7 +790,8 @@ __device__ __forceinline__ void topics_by_counters(const TopicArgs& a, int64_t r
 
 // The ranges of the documents that are split, a workgroup each.  A document of 440 000 tokens in 100 000 topics: 100 us
 // for all that it takes (340 with its four ranges one after the other); counting takes 75 us of them, some
-// 25 instructions a round of 64 tokens on the four SIMDs of one CU.
+// 25 instructions a round of 64 tokens on the four SIMDs of one CU.  (A range of 63 488 topics is looked through twice, 31
+// words a thread: 4 us each.)
 __global__ __launch_bounds__(kLongBlock) void range_topics_kernel(TopicArgs a)
 {
     extern __shared__ __align__(16) unsigned char raw[];
