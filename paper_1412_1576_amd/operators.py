@@ -5,8 +5,9 @@
   distill_loss_and_grad        the same and its gradient in one call, for weights known beforehand
   verify_drafts                drafted tokens accepted or redrawn from given random numbers
 
-Work goes to torch's current stream of the tensors' device; outputs and workspaces come from
-torch's allocator; no call waits for the GPU.  Wrong shapes, types or devices raise ValueError,
+Work goes to torch's current stream of the tensors' device (inputs made on another stream have to
+be ready on it); outputs and workspaces come from torch's allocator; no call waits for the GPU, and
+all can be captured into a graph.  Wrong shapes, types or devices raise ValueError,
 refusals of the library LdaError.
 """
 from __future__ import annotations
@@ -158,6 +159,8 @@ def distill_loss(logits, ids, teacher, *, temperature=1.0, log_norm=None):
     [rows], they are exp(teacher / temperature - log_norm) and what they leave of 1 is spread evenly over
     the classes without a slot.  The loss is temperature^2 KL(teacher || softmax(logits / temperature)).
     Rows of a tensor may lie any distance apart; within a row elements are adjacent.
+    A backward pass captured into a graph must find no eager graph of the same leaves alive (delete losses
+    that were computed from them before).
     """
     _check_distill(logits, ids, teacher, log_norm)
     return _Distill.apply(logits, ids, teacher, log_norm, float(temperature))
