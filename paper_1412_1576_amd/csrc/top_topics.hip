@@ -268,7 +268,9 @@ __global__ __launch_bounds__(kWaveBlock, 6) void wave_topics_kernel(TopicArgs a)
     const int32_t wave = __builtin_amdgcn_readfirstlane(tid / kWave);  // what is a wave's is scalar
     for (int32_t i = tid; i < kWaves * 2 * kWaveTopics; i += kWaveBlock) (&table[0][0])[i] = 0;
     const double k_alpha = (double)a.K * a.alpha;
-    for (int32_t i = tid; i <= kWaveTopics; i += kWaveBlock) {
+    // worth it from some documents a wave on (2048 documents: 11.4 us without, 12.4 with them; 300 000: 367 with)
+    const bool logs = a.rows > 2 * (int64_t)gridDim.x * kWaves;
+    for (int32_t i = tid; logs && i <= kWaveTopics; i += kWaveBlock) {
         log_of[i] = (float)log((double)i + a.alpha);
         norm_of[i] = (float)log((double)i + k_alpha);
     }
@@ -304,11 +306,11 @@ __global__ __launch_bounds__(kWaveBlock, 6) void wave_topics_kernel(TopicArgs a)
             continue;
         }
         const int32_t counted = topics_by_wave(a, row, z, L, next, table[wave], used[wave], read_next, [&](int32_t n) {
-            return n <= kWaveTopics ? log_of[n] : (float)log((double)n + a.alpha);
+            return logs && n <= kWaveTopics ? log_of[n] : (float)log((double)n + a.alpha);
         });
         if (lane != 0) continue;
         if (counted < 0) a.ids[row * a.k] = kUnfinished;
-        else if (a.log_norm) a.log_norm[row] = counted <= kWaveTopics ? norm_of[counted] : (float)log((double)counted + k_alpha);
+        else if (a.log_norm) a.log_norm[row] = logs && counted <= kWaveTopics ? norm_of[counted] : (float)log((double)counted + k_alpha);
     }
 }
 
