@@ -268,7 +268,9 @@ __global__ __launch_bounds__(kWaveBlock, 6) void wave_topics_kernel(TopicArgs a)
     const int32_t wave = __builtin_amdgcn_readfirstlane(tid / kWave);  // what is a wave's is scalar
     for (int32_t i = tid; i < kWaves * 2 * kWaveTopics; i += kWaveBlock) (&table[0][0])[i] = 0;
     const double k_alpha = (double)a.K * a.alpha;
-    // worth it from some documents a wave on (2048 documents: 11.4 us without, 12.4 with them; 300 000: 367 with)
+    // the logarithms are tabled only where a wave has more than two documents, where both meet. Documents of 90
+    // tokens, with the tables and without: 6 000 16.1 and 13.8 us, 12 000 20.0 and 19.8, 16 000 21.4 and 22.4,
+    // 300 000 205 and 276; of 330 tokens, 300 000: 367 and 426
     const bool logs = a.rows > 2 * (int64_t)gridDim.x * kWaves;
     for (int32_t i = tid; logs && i <= kWaveTopics; i += kWaveBlock) {
         log_of[i] = (float)log((double)i + a.alpha);
