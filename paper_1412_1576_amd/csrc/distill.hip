@@ -20,6 +20,7 @@ constexpr int kSliceLoads = 8;                                // 16-byte loads o
 constexpr int32_t kSliceChunks = kPartBlock * kSliceLoads;    // 32 KB
 constexpr int32_t kStatFloats = 8;
 constexpr float kFar = 16.0f;  // a base is left where it is until a logit exceeds it by this, in powers of 2
+constexpr float kDeep = -0x1p100f;  // sums of 8 numbers above this are far from the end of 32 bits
 
 // What a slice of a row tells about its softmax.  scaled_sum (of c (S - m) over the logits above -infinity) and
 // n (their number) are only there where the teacher has a floor.
@@ -162,7 +163,7 @@ struct Running {
                 least = fminf(least, y[e]);
                 ysum += y[e];
             }
-            if (least > -INFINITY) {
+            if (least > kDeep) {
                 scaled_sum += (double)ysum;
                 n += N;
             } else {
