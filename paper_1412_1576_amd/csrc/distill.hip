@@ -20,10 +20,10 @@ constexpr int kSliceLoads = 8;                                // 16-byte loads o
 constexpr int32_t kSliceChunks = kPartBlock * kSliceLoads;    // 32 KB
 constexpr int32_t kStatFloats = 8;
 constexpr float kFar = 16.0f;  // a base is left where it is until a logit exceeds it by this, in powers of 2
-constexpr float kDeep = -0x1p100f;  // sums of 8 numbers above this are far from the end of 32 bits
+constexpr float kLeastSum = -0x1p100f;  // sums of 8 differences from the base above this have none near the end of 32 bits
 
-// What a slice of a row tells about its softmax.  scaled_sum (of c (S - m) over the logits above -infinity) and
-// n (their number) are only there where the teacher has a floor.
+// What a slice of a row tells about its softmax.  scaled_sum (of c (S - m) over the logits above -infinity but for
+// deep ones that have a slot) and n (their number) are only there where the teacher has a floor.
 struct RowPart {
     float m, s;
     double scaled_sum;
@@ -109,6 +109,21 @@ __device__ __forceinline__ double rebased(double scaled_sum, int32_t n, float fr
     return n > 0 ? scaled_sum + (double)n * (((double)from - (double)to) * (double)c) : scaled_sum;
 }
 
+// Whether any thread of the workgroup has something, in two steps with the barriers of a block_join between
+// them (__syncthreads_or takes 1 us)
+template <int BLOCK>
+__device__ __forceinline__ void put_any(int has, uint32_t* part)
+{
+    const uint64_t some = __ballot(has);
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = some != 0;
+    if (BLOCK == kWave) wave_lds_order();
+}
+template <int BLOCK>
+__device__ __forceinline__ bool get_any(const uint32_t* part)
+{
+    return __ballot(part[threadIdx.x % (BLOCK / kWave)] != 0) != 0;
+}
+
 // A row as the whole 16-byte chunks of memory inside it, and the elements before and behind
 // those (fewer than two chunks), which a thread each takes.
 template <class T>
@@ -129,23 +144,81 @@ struct SplitRow {
     __device__ __forceinline__ uint4 load(int32_t i) const { return *reinterpret_cast<const uint4*>(p + chunk(i)); }
 };
 
-// The running form of one thread's share
-template <class T, bool REST>
+// c (S - base) over classes without a slot whose logit lies above -infinity, and their number: what the floor's part
+// of the loss needs.  Every class is added while the row is read, and those that have a slot are taken out when
+// the slots are there.  A mask's large number, added and taken out, would leave nothing of the others: logits
+// below `deep` are passed over and looked at again, with the bits of the classes that have a slot, in rows that have any
+// (2048 x 10000 f32: 40 us without, 44 with a fifth of a row masked, 46 with each second class; masks of -infinity 41).
+struct BesideSums {
+    double sum;
+    int32_t n;
+
+    __device__ __forceinline__ void add(float x, float base, float c)
+    {
+        if (x == -INFINITY) return;
+        sum += ((double)x - (double)base) * (double)c;
+        ++n;
+    }
+    __device__ __forceinline__ void take_out(float x, float deep, float base, float c)
+    {
+        if (!(x >= deep)) return;
+        sum -= ((double)x - (double)base) * (double)c;
+        --n;
+    }
+    template <int N>
+    __device__ __forceinline__ void add_deep(const float (&x)[N], float deep, float base, float c, uint32_t named)
+    {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (x[e] < deep && !(named >> e & 1u)) add(x[e], base, c);
+    }
+};
+// What is taken out leaves roundings of its chunk's sum in 32 bits behind, some 2^-24 of 8 times this, times the
+// floor.  In rows of a few thousand classes most may have a slot, in longer ones one of ten.
+constexpr float kDeepOfShort = -64.0f, kDeepOfLong = -1024.0f;
+
+// Which classes of COUNT chunks, from chunk c0 on, and of the extras have a slot: a byte a chunk, a bit an
+// element
+template <int COUNT>
+struct NamedBits {
+    static constexpr int kWords = (COUNT + 3) / 4 + 1;  // the extras' behind the chunks'
+    uint32_t word[kWords];
+
+    __device__ __forceinline__ void clear(int32_t thread, int32_t threads)
+    {
+        for (int32_t i = thread; i < kWords; i += threads) word[i] = 0;
+    }
+    template <class T>
+    __device__ __forceinline__ void mark(const SplitRow<T>& r, int32_t c0, int32_t id)
+    {
+        constexpr int E = SplitRow<T>::E;
+        const int32_t at = id - r.head, chunk = at / E - c0;
+        if (at < 0 || at >= r.whole * E) {
+            atomicOr(&word[kWords - 1], 1u << (at < 0 ? id : id - r.whole * E));
+        } else if (chunk >= 0 && chunk < COUNT) {
+            atomicOr(&word[chunk / 4], 1u << (chunk % 4 * 8 + at % E));
+        }
+    }
+    __device__ __forceinline__ uint32_t of_chunk(int32_t i) const { return reinterpret_cast<const uint8_t*>(word)[i]; }
+    __device__ __forceinline__ uint32_t of_extra(int32_t i) const { return word[kWords - 1] >> i & 1u; }
+};
+
+// The running form of one thread's share; REST: with the sums beside the slots, of the same base
+template <bool REST>
 struct Running {
-    static constexpr int E = Row<T>::kChunk;
     float m = -INFINITY, s = 0.0f;
-    double scaled_sum = 0.0;
-    int32_t n = 0;
+    BesideSums beside{};
+    int any_deep = 0;
 
     template <int N>
-    __device__ __forceinline__ void add(const float (&x)[N], float c)
+    __device__ __forceinline__ void add(const float (&x)[N], float c, float deep)
     {
         float top = x[0];
 #pragma unroll
         for (int e = 1; e < N; ++e) top = fmaxf(top, x[e]);
         if ((top - m) * c > kFar) {
             s *= exp_above(m, top, c);
-            if (REST) scaled_sum = rebased(scaled_sum, n, m, top, c);
+            if (REST) beside.sum = rebased(beside.sum, beside.n, m, top, c);
             m = top;
         }
         const float base = base_of(m);
@@ -157,21 +230,20 @@ struct Running {
         }
         s += sum;
         if (REST) {
-            float least = y[0], ysum = y[0];
+            float least = x[0], some = y[0];
 #pragma unroll
             for (int e = 1; e < N; ++e) {
-                least = fminf(least, y[e]);
-                ysum += y[e];
+                least = fminf(least, x[e]);
+                some += y[e];
             }
-            if (least > kDeep) {
-                scaled_sum += (double)ysum;
-                n += N;
+            if (least >= deep && some > kLeastSum) {
+                beside.sum += (double)some;
+                beside.n += N;
             } else {
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    if (x[e] == -INFINITY) continue;
-                    scaled_sum += ((double)x[e] - (double)base) * (double)c;
-                    ++n;
+                    if (x[e] >= deep) beside.add(x[e], base, c);
+                    else any_deep |= x[e] != -INFINITY;
                 }
             }
         }
@@ -336,10 +408,10 @@ __device__ __forceinline__ void store_chunk(T* g, const float (&x)[Row<T>::kChun
 }
 
 // A thread's share of a row's loss: sum of p (log p - log q) over the slots; and where there is a floor, what
-// lies beside them: c (S - m) over the logits above -infinity, and their number.
+// lies beside them
 struct LossSums {
-    double slots, beside;
-    int32_t n;
+    double slots;
+    BesideSums beside;
 
     __device__ __forceinline__ void add_slot(float p, float t, float x, double z, double base, double inv_t, double log_s)
     {
@@ -347,19 +419,13 @@ struct LossSums {
         const double log_q = x == -INFINITY ? -(double)INFINITY : ((double)x - base) * inv_t - log_s;
         slots += (double)p * ((double)t * inv_t - z - log_q);
     }
-    __device__ __forceinline__ void leave_out(float x, float base, float c)  // a named class
-    {
-        if (x == -INFINITY) return;
-        beside -= ((double)x - (double)base) * (double)c;
-        --n;
-    }
     template <bool REST, int BLOCK>
     __device__ __forceinline__ void sum(LossSums* part)
     {
         slots = wave_sum(slots);
         if (REST) {
-            beside = wave_sum(beside);
-            n = wave_sum(n);
+            beside.sum = wave_sum(beside.sum);
+            beside.n = wave_sum(beside.n);
         }
         if (BLOCK == kWave) return;
         __syncthreads();
@@ -370,8 +436,8 @@ struct LossSums {
         for (int w = 1; w < BLOCK / kWave; ++w) {
             slots += part[w].slots;
             if (REST) {
-                beside += part[w].beside;
-                n += part[w].n;
+                beside.sum += part[w].beside.sum;
+                beside.n += part[w].beside.n;
             }
         }
     }
@@ -383,8 +449,8 @@ __device__ __forceinline__ float loss_of(const DistillArgs& a, const LossSums& l
     const double T = (double)a.T;
     double sum = l.slots;
     if (REST && t.floor > 0.0) {
-        const double beside = l.beside / ((double)a.c * T);
-        sum += l.n < t.others ? (double)INFINITY : t.floor * ((double)t.others * (log(t.floor) + log_s) - beside);
+        const double beside = l.beside.n == 0 ? 0.0 : l.beside.sum / ((double)a.c * T);
+        sum += l.beside.n < t.others ? (double)INFINITY : t.floor * ((double)t.others * (log(t.floor) + log_s) - beside);
     }
     double loss = T * T * sum;
     if (!(s == s) || !(t.mass == t.mass)) loss = (double)NAN;
@@ -406,10 +472,12 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
     constexpr int E = Row<T>::kChunk, kSlotsEach = (kMostSlots + BLOCK - 1) / BLOCK;
     // short rows are read before it is known whether they are left out: the weight's latency is theirs too
     constexpr bool kEager = BLOCK * CHUNKS <= 1024;
+    constexpr float kDeep = BLOCK * CHUNKS <= 1024 ? kDeepOfShort : kDeepOfLong;
     extern __shared__ __align__(16) unsigned char lds[];
     __shared__ float2 part2[BLOCK / kWave];
     __shared__ LossSums parts[BLOCK / kWave];
     __shared__ int32_t parti[BLOCK / kWave];
+    __shared__ uint32_t part_any[BLOCK / kWave];
     const Slots slots(lds, a.k);
     const int32_t tid = (int32_t)threadIdx.x;
     const int64_t row = a.row0 + blockIdx.x;
@@ -429,30 +497,51 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
     if (kEager) load();
     bool out = a.grad && w == 0.0f;  // left out
     float m = -INFINITY, s = 0.0f;
-    LossSums l{0.0, 0.0, 0};
+    LossSums l{};
+    bool any_deep = false;
     if (!out) {
         if (tid < kWave) read_teacher(a, row, r.p, slots);
         if (!kEager) load();
-        Running<T, REST> run;
+        Running<REST> run;
 #pragma unroll
         for (int j = 0; j < CHUNKS; ++j) {
             if (j * BLOCK + tid < r.whole) {
                 float x[E];
                 Row<T>::unpack(raw[j], x);
-                run.add(x, a.c);
+                run.add(x, a.c, kDeep);
             }
             __builtin_amdgcn_sched_barrier(0);  // else all of the row is unpacked before it is used
         }
-        if (tid < r.extras) run.add(extra, a.c);
+        if (tid < r.extras) run.add(extra, a.c, kDeep);
         m = run.m;
         s = run.s;
+        if (REST) put_any<BLOCK>(run.any_deep, part_any);
         block_join<BLOCK>(m, s, a.c, part2);
         if (REST) {
-            l.beside = rebased(run.scaled_sum, run.n, run.m, m, a.c);
-            l.n = run.n;
+            l.beside = run.beside;
+            l.beside.sum = rebased(run.beside.sum, run.beside.n, run.m, m, a.c);
+            any_deep = get_any<BLOCK>(part_any);
         }
     }
     __syncthreads();
+    if (REST && any_deep) {
+        __shared__ NamedBits<BLOCK * CHUNKS> named;
+        named.clear(tid, BLOCK);
+        __syncthreads();
+        for (int32_t j = tid; j < a.k; j += BLOCK)
+            if (slots.id[j] >= 0) named.mark(r, 0, slots.id[j]);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            if (j * BLOCK + tid < r.whole) {
+                float x[E];
+                Row<T>::unpack(raw[j], x);
+                l.beside.add_deep(x, kDeep, base_of(m), a.c, named.of_chunk(j * BLOCK + tid));
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (tid < r.extras) l.beside.add_deep(extra, kDeep, base_of(m), a.c, named.of_extra(tid));
+    }
     TeacherPart t = *slots.head;
     float all[kSlotsEach];
     int32_t named = 0;
@@ -468,7 +557,7 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
             const bool first = first_of_class(slots, twice, a.k, j, id, all[q]);
             if (REST && first) {
                 ++named;
-                l.leave_out(slots.x[j], base_of(m), a.c);
+                l.beside.take_out(slots.x[j], kDeep, base_of(m), a.c);
             }
         }
     }
@@ -527,6 +616,7 @@ __global__ __launch_bounds__(kPartBlock) void distill_part_kernel(DistillArgs a)
     __shared__ float2 part2[kPartBlock / kWave];
     __shared__ double partd[kPartBlock / kWave];
     __shared__ int32_t parti[kPartBlock / kWave];
+    __shared__ uint32_t part_any[kPartBlock / kWave];
     const Slots slots(lds, a.k);
     const int32_t tid = (int32_t)threadIdx.x;
     const int64_t row = a.row0 + blockIdx.x;
@@ -559,26 +649,46 @@ __global__ __launch_bounds__(kPartBlock) void distill_part_kernel(DistillArgs a)
 #pragma unroll
         for (int j = 0; j < kSliceLoads; ++j)
             if (i0 + j * kPartBlock < r.whole) raw[j] = r.load(i0 + j * kPartBlock);
-        Running<T, REST> run;
-        if (slice == 0 && tid < r.extras) {
-            const float extra[1] = {Row<T>::one(r.p + r.extra(tid))};
-            run.add(extra, a.c);
-        }
+        const bool has_extra = slice == 0 && tid < r.extras;
+        const float extra[1] = {has_extra ? Row<T>::one(r.p + r.extra(tid)) : -INFINITY};
+        Running<REST> run;
+        if (has_extra) run.add(extra, a.c, kDeepOfLong);
 #pragma unroll
         for (int j = 0; j < kSliceLoads; ++j) {
             if (i0 + j * kPartBlock < r.whole) {
                 float x[E];
                 Row<T>::unpack(raw[j], x);
-                run.add(x, a.c);
+                run.add(x, a.c, kDeepOfLong);
             }
         }
         const float own = run.m;
+        if (REST) put_any<kPartBlock>(run.any_deep, part_any);
         block_join<kPartBlock>(run.m, run.s, a.c, part2);
         if (REST) {
-            run.scaled_sum = block_sum<kPartBlock>(rebased(run.scaled_sum, run.n, own, run.m, a.c), partd);
-            run.n = block_sum<kPartBlock>(run.n, parti);
+            run.beside.sum = rebased(run.beside.sum, run.beside.n, own, run.m, a.c);
+            if (get_any<kPartBlock>(part_any)) {
+                __shared__ NamedBits<kSliceChunks> named;
+                named.clear(tid, kPartBlock);
+                __syncthreads();
+                for (int32_t j = tid; j < a.k; j += kPartBlock) {
+                    const int64_t id = index_at(a.ids, a.ids_type, row * a.ids_stride + j);
+                    if (id >= 0 && id < a.V) named.mark(r, slice * kSliceChunks, (int32_t)id);
+                }
+                __syncthreads();
+#pragma unroll 1
+                for (int j = 0; j < kSliceLoads; ++j) {
+                    if (i0 + j * kPartBlock < r.whole) {
+                        float x[E];
+                        Row<T>::unpack(r.load(i0 + j * kPartBlock), x);  // again: to keep them costs every slice registers
+                        run.beside.add_deep(x, kDeepOfLong, base_of(run.m), a.c, named.of_chunk(j * kPartBlock + tid));
+                    }
+                }
+                if (has_extra) run.beside.add_deep(extra, kDeepOfLong, base_of(run.m), a.c, named.of_extra(tid));
+            }
+            run.beside.sum = block_sum<kPartBlock>(run.beside.sum, partd);
+            run.beside.n = block_sum<kPartBlock>(run.beside.n, parti);
         }
-        if (tid == 0) a.parts[row * a.slices + slice] = RowPart{run.m, run.s, run.scaled_sum, run.n, 0};
+        if (tid == 0) a.parts[row * a.slices + slice] = RowPart{run.m, run.s, run.beside.sum, run.beside.n, 0};
     }
 }
 
@@ -651,13 +761,13 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
         if (REST || a.grad) twice = find_twice<kPartBlock>(slots, a.k);
     }
     if (a.loss && blockIdx.y == 0) {
-        LossSums l{0.0, 0.0, 0};
+        LossSums l{};
         const double log_s = log((double)s);
         if (!out) {
             const double base = (double)base_of(m);
             if (REST && tid == 0) {
-                l.beside = scaled_sum;
-                l.n = n;
+                l.beside.sum = scaled_sum;
+                l.beside.n = n;
             }
             for (int32_t j = tid; j < a.k; j += kPartBlock) {
                 const int32_t id = slots.id[j];
@@ -665,7 +775,7 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
                 const float x = Row<T>::one(r.p + id);
                 l.add_slot(slots.p[j], slots.t[j], x, z, base, inv_t, log_s);
                 float all;
-                if (REST && first_of_class(slots, twice, a.k, j, id, all)) l.leave_out(x, base_of(m), a.c);
+                if (REST && first_of_class(slots, twice, a.k, j, id, all)) l.beside.take_out(x, kDeepOfLong, base_of(m), a.c);
             }
         }
         l.sum<REST, kPartBlock>(parts);

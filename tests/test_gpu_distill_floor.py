@@ -18,6 +18,20 @@ def sizes(shape, dtype):
     return n, v if dtype == "f32" else 2 * v
 
 
+def taken_out(x, ids, P, tau):
+    """What classes with a slot may leave behind that are summed with the others and taken out again (logits above
+    -64, or -1024 in long rows): each 7 roundings, of a sum of 8 differences from the base, which is at most 12 / T
+    below the largest logit."""
+    off = np.zeros(len(x))
+    for i in range(len(x)):
+        at = np.unique(ids[i][(ids[i] >= 0) & (ids[i] < x.shape[1])])
+        others = np.setdiff1d(np.arange(x.shape[1]), at)
+        near = x[i][(x[i] > -1100) & (x[i] < 1100)]
+        if len(others) and len(near):
+            off[i] = tau * P[i][others[0]] * len(at) * 7 * 8 * (near.max() - near.min() + 12) * 2.0 ** -24
+    return off
+
+
 def compare_rows(ops, x, ids, t, rows, tau=1.0, log_norm=None, held=None):
     """The step, and loss and gradient through autograd, of all rows; `rows` of them against the definition.
     held: the norms for the definition, where they differ."""
@@ -32,6 +46,10 @@ def compare_rows(ops, x, ids, t, rows, tau=1.0, log_norm=None, held=None):
     xr = host(x[rows])
     want, grad, q, P, size = reference(xr, ids[rows].cpu().numpy(), host(t[rows]), tau, host(None if norm is None else norm[rows]))
     lb, gb = bounds(xr, tau, size, q, P, None, x.dtype, grad)
+    if norm is not None:
+        lb = lb + np.nan_to_num(taken_out(xr, ids[rows].cpu().numpy(), P, tau))
+    # (a loss above the largest number of 32 bits is rounded to infinity: T times a mask of the lowest value may be)
+    want = np.where(want > np.finfo(np.float32).max, np.inf, want)
     for what, (loss, g) in zip(("step", "autograd"), got):
         compare(loss[rows].cpu().numpy(), want, lb, "loss, " + what)
         compare(host(g[rows]), grad, gb, "gradient, " + what)
@@ -50,3 +68,38 @@ def test_masks_of_the_lowest_value_beside_the_slots(ops, shape, tau, dtype):
     norm = (torch.logsumexp(t.double() / tau, 1) + 0.05).float()
     got = compare_rows(ops, x, ids, t, list(range(n)), tau, norm)
     assert all(torch.isfinite(loss).all() and (loss > 1e35).all() for loss, _ in got)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("mask", [-1e9, -1e30, None])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_masked_classes_with_a_slot(ops, shape, mask, dtype):
+    """A teacher's largest logits where it has fewer classes than slots: what it and the student mask has a slot, and
+    no mass.  Only the classes without a slot count beside the slots."""
+    n, v = sizes(shape, dtype)
+    low = torch.finfo(TYPES[dtype]).min
+    mask = low if mask is None else mask
+    x, ids, t = make(n, v, 16, TYPES[dtype], seed=2)
+    x.scatter_(1, ids[:, 8:], mask)
+    t[:, 8:] = -float("inf")
+    x[1].scatter_(0, ids[1, 12:], low)             # two kinds of masks
+    x[2, (ids[2, 0] + 1) % v] = -float("inf")
+    t[2, 15] = 1.0                                 # masked by the student alone
+    x[3, : v // 2] = mask                          # also classes without a slot: a large loss
+    for tau in (1.0, 2.0, 4.0):
+        full = t.double() / tau
+        norm = (torch.logsumexp(full, 1) + 0.3).float()
+        compare_rows(ops, x, ids, t, [0, 1, 2, 3, n - 1], tau, norm)
+
+
+@pytest.mark.parametrize("mask", [-50.0, -80.0, -1000.0, -1050.0, -1e5])
+@pytest.mark.parametrize("n,v,k", [(3, 20, 16), (3, 300, 200), (3, 2_000, 1_000), (3, 15_000, 1_000), (2, 90_001, 1_000)])
+def test_most_classes_have_a_slot_and_a_mask(ops, n, v, k, mask):
+    """Masks around the borders, in every place of a chunk; and rows of logits that all lie below the borders."""
+    x, ids, t = make(n, v, k, torch.float32, seed=3)
+    x.scatter_(1, ids[:, k // 8:], mask)
+    t[:, k // 8:] = -float("inf")
+    norm = (torch.logsumexp(t.double(), 1) + 0.5).float()
+    compare_rows(ops, x, ids, t, list(range(n)), 1.0, norm)
+    compare_rows(ops, x - 70.0, ids, t, list(range(n)), 1.0, norm)
+    compare_rows(ops, x - 1500.0, ids, t, list(range(n)), 1.0, norm)
