@@ -280,6 +280,12 @@ inline size_t slots_lds(int32_t k)
     return sizeof(TeacherPart) + 16 * ((size_t)(k + 3) / 4 * 4) + (k > kPairs ? 4 + ((size_t)4 << table_bits(k)) : 0);
 }
 
+// exp(t / T - z): none for t = -infinity, which empty slots have, also where the norm is -infinity
+__device__ __forceinline__ double slot_mass(float t, double inv_t, double z)
+{
+    return t == -INFINITY ? 0.0 : exp((double)t * inv_t - z);
+}
+
 // One wave's work: ids, logits of both sides and masses of a row's slots.
 template <class T>
 __device__ __forceinline__ void read_teacher(const DistillArgs& a, int64_t row, const T* logits, const Slots& slots)
@@ -306,7 +312,7 @@ __device__ __forceinline__ void read_teacher(const DistillArgs& a, int64_t row, 
     if (a.log_norm) {
         mass = 0.0;
         for (int32_t j = lane; j < (a.k + 3) / 4 * 4; j += kWave) {
-            const double p = exp((double)slots.t[j] * inv_t - z);
+            const double p = slot_mass(slots.t[j], inv_t, z);
             slots.p[j] = (float)p;
             mass += p;
         }
@@ -317,7 +323,7 @@ __device__ __forceinline__ void read_teacher(const DistillArgs& a, int64_t row, 
         for (int32_t j = lane; j < a.k; j += kWave) sum += exp(((double)slots.t[j] - (double)top) * inv_t);
         sum = wave_sum(sum);
         z = (double)top * inv_t + (sum == 0.0 ? 0.0 : log(sum));
-        for (int32_t j = lane; j < (a.k + 3) / 4 * 4; j += kWave) slots.p[j] = (float)exp((double)slots.t[j] * inv_t - z);
+        for (int32_t j = lane; j < (a.k + 3) / 4 * 4; j += kWave) slots.p[j] = (float)slot_mass(slots.t[j], inv_t, z);
         mass = sum == 0.0 ? 0.0 : sum / sum;  // 1, or what is not a number
     }
     if (lane == 0) {
@@ -755,7 +761,7 @@ __global__ __launch_bounds__(kPartBlock) void distill_join_kernel(DistillArgs a)
             }
             slots.id[j] = id;
             slots.t[j] = tl;
-            slots.p[j] = id >= 0 ? (float)exp((double)tl * inv_t - z) : 0.0f;
+            slots.p[j] = id >= 0 ? (float)slot_mass(tl, inv_t, z) : 0.0f;
         }
         __syncthreads();
         if (REST || a.grad) twice = find_twice<kPartBlock>(slots, a.k);

@@ -103,3 +103,23 @@ def test_most_classes_have_a_slot_and_a_mask(ops, n, v, k, mask):
     compare_rows(ops, x, ids, t, list(range(n)), 1.0, norm)
     compare_rows(ops, x - 70.0, ids, t, list(range(n)), 1.0, norm)
     compare_rows(ops, x - 1500.0, ids, t, list(range(n)), 1.0, norm)
+
+
+@pytest.mark.parametrize("k", [1, 3, 4, 70])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_a_norm_of_no_mass(ops, shape, k):
+    """The log-sum of a row of empty slots, or of logits of -infinity, is -infinity: no slot has mass, and the
+    floor is 1 / (classes without a slot)."""
+    n, v = shape
+    x, ids, t = make(n, v, k, torch.float32, seed=4)
+    norm = (torch.logsumexp(t.double(), 1) + 0.3).float()
+    ids[0] = -1
+    ids[1, 0] = v                      # one slot and its like outside the classes
+    ids[1, 1:] = -5
+    t[1] = float("nan")                # not looked at
+    t[2] = -float("inf")               # slots that name their classes, without mass
+    norm[:3] = -float("inf")
+    held = norm.clone()
+    held[:3] = 0.0                     # (any norm gives the same)
+    got = compare_rows(ops, x, ids, t, [0, 1, 2, 3, n - 1], 1.0, norm, held)
+    assert all(torch.isfinite(g).all() for g in sum(got, ()))
