@@ -283,7 +283,7 @@ int lda_get_beta_table(lda_ctx* ctx, uint32_t* split, uint32_t* alias, uint32_t*
  *   d loss / d S_v = T (M q_v - P_v),  P_v = the p_j of v's slots, or r;  M = sum P_v.
  * A term of mass 0 is 0, and a slot of logit -infinity has no mass, whatever the norm.  A row without any
  * mass has loss 0 and gradient 0, whatever S holds.  Mass on a class of q_v = 0 makes the loss +infinity; the gradient is the formula's.  NaN or +infinity in S, or in the
- * logit of a slot that is not empty, makes the row's loss and gradient NaN.
+ * logit of a slot that is not empty, or masses whose sum 64 bits do not hold, make the row's loss and gradient NaN.
  * The softmax is summed in 32 bits, the teacher's masses and the loss in 64.
  */
 typedef struct lda_distill_rows {

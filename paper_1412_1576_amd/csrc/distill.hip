@@ -326,6 +326,7 @@ __device__ __forceinline__ void read_teacher(const DistillArgs& a, int64_t row, 
         for (int32_t j = lane; j < (a.k + 3) / 4 * 4; j += kWave) slots.p[j] = (float)slot_mass(slots.t[j], inv_t, z);
         mass = sum == 0.0 ? 0.0 : sum / sum;  // 1, or what is not a number
     }
+    if (mass == (double)INFINITY) mass = (double)NAN;  // so that all of loss and gradient is
     if (lane == 0) {
         slots.head->mass = mass;
         slots.head->z = z;

@@ -123,3 +123,28 @@ def test_a_norm_of_no_mass(ops, shape, k):
     held[:3] = 0.0                     # (any norm gives the same)
     got = compare_rows(ops, x, ids, t, [0, 1, 2, 3, n - 1], 1.0, norm, held)
     assert all(torch.isfinite(g).all() for g in sum(got, ()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_infinite_mass(ops, shape, dtype):
+    """A teacher's logit of +infinity, with a norm as without one, or a norm of -infinity beside a logit: the row is not a
+    number; and with weight 0 it is left out like any other."""
+    n, v = sizes(shape, dtype)
+    x, ids, t = make(n, v, 8, TYPES[dtype], seed=5)
+    norm = (torch.logsumexp(t.double(), 1) + 0.3).float()
+    t[0, 3] = float("inf")
+    t[1, 3], norm[1] = float("inf"), float("inf")
+    norm[2] = -float("inf")
+    odd = torch.zeros(n, dtype=torch.bool, device="cuda")
+    for z in (norm, None):
+        odd[:3] = True
+        odd[2] = z is not None
+        leaf = x.detach().requires_grad_(True)
+        loss = ops.distill_loss(leaf, ids, t, log_norm=z)
+        grad, = torch.autograd.grad(loss, leaf, torch.ones_like(loss))
+        for l, g in ((loss, grad), ops.distill_loss_and_grad(x, ids, t, log_norm=z)):
+            assert torch.equal(l.isnan(), odd) and torch.isfinite(l[~odd]).all()
+            assert torch.equal(g.isnan().any(1), odd) and torch.equal(g.isnan().all(1), odd)
+        left = ops.distill_loss_and_grad(x, ids, t, log_norm=z, weight=(~odd).float())
+        assert torch.isfinite(left[0]).all() and (left[0][odd] == 0).all() and (left[1][odd] == 0).all()
