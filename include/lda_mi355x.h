@@ -273,7 +273,8 @@ int lda_get_beta_table(lda_ctx* ctx, uint32_t* split, uint32_t* alias, uint32_t*
  * Distillation from a teacher's top logits.  Row i of the student has one logit S_v for each of
  * `classes` classes (topics, words); row i of the teacher has `slots` slots, an id and a logit t_j each.
  * A slot whose id lies outside [0, classes) is empty; ids may come in any order and more than once
- * (their masses add up).  With T = temperature:
+ * (their masses add up in P_v; the loss has the term p_j log p_j of each, which the student does not change, so
+ * that it is less than that of one slot of their mass by T^2 sum p_j log(P_v / p_j)).  With T = temperature:
  *   q = softmax(S / T), where q_v = 0 for S_v = -infinity;
  *   log_norm == NULL: p_j = softmax over the row's slots of t_j / T, r = 0;
  *   otherwise:        p_j = exp(t_j / T - log_norm), and the mass that is left, if any, is spread
@@ -282,8 +283,9 @@ int lda_get_beta_table(lda_ctx* ctx, uint32_t* split, uint32_t* alias, uint32_t*
  *   loss = T^2 ( sum_j p_j (log p_j - log q_id_j) + sum over classes without a slot of r (log r - log q_v) )
  *   d loss / d S_v = T (M q_v - P_v),  P_v = the p_j of v's slots, or r;  M = sum P_v.
  * A term of mass 0 is 0, and a slot of logit -infinity has no mass, whatever the norm.  A row without any
- * mass has loss 0 and gradient 0, whatever S holds.  Mass on a class of q_v = 0 makes the loss +infinity; the gradient is the formula's.  NaN or +infinity in S, or in the
- * logit of a slot that is not empty, or masses whose sum 64 bits do not hold, make the row's loss and gradient NaN.
+ * mass has loss 0 and gradient 0, whatever S holds.  Mass on a class of q_v = 0 makes the loss +infinity; the
+ * gradient is the formula's.  NaN or +infinity in S, or in the logit of a slot that is not empty, or masses
+ * whose sum 64 bits do not hold, make the row's loss and gradient NaN.
  * The softmax is summed in 32 bits, the teacher's masses and the loss in 64.
  */
 typedef struct lda_distill_rows {

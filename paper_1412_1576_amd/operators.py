@@ -157,7 +157,9 @@ def distill_loss(logits, ids, teacher, *, temperature=1.0, log_norm=None):
     whose id is outside [0, classes) is empty; teacher [rows, slots], its logits there.
     Without log_norm the teacher's masses are a softmax over a row's slots; with log_norm, float32
     [rows], they are exp(teacher / temperature - log_norm) and what they leave of 1 is spread evenly over
-    the classes without a slot.  The loss is temperature^2 KL(teacher || softmax(logits / temperature)).
+    the classes without a slot.  The loss is temperature^2 KL(teacher || softmax(logits / temperature)) where the
+    ids of a row differ; a class with several slots has their masses' sum, and the gradient of that, but each slot's
+    own p log p in the loss (the term that the student does not change).
     Rows of a tensor may lie any distance apart; within a row elements are adjacent.
     A backward pass captured into a graph must find no eager graph of the same leaves alive (delete losses
     that were computed from them before).
