@@ -398,7 +398,8 @@ int64_t lda_topics_workspace(const lda_topic_rows* rows);
 /* ids [rows][slots], logits [rows][slots], log_norm [rows] or NULL */
 int lda_top_topics(const lda_topic_rows* rows, int32_t* ids, float* logits, float* log_norm);
 /* The same from the context's current assignment, its K and alpha, on its stream; docs and the outputs are
- * device pointers.  Any state.  With stream_block_tokens: LDA_ERR_UNSUPPORTED (z is in host memory). */
+ * device pointers.  Any state.  A captured call reads, when it is replayed, what the last sweep or lda_set_z before
+ * it on the stream has left.  With stream_block_tokens: LDA_ERR_UNSUPPORTED (z is in host memory). */
 int lda_doc_topics(lda_ctx* ctx, int64_t rows, const int32_t* docs, int32_t slots, int32_t* ids,
                    float* logits, float* log_norm);
 

@@ -75,6 +75,8 @@ void device_release(lda_ctx* c, void* p)
 
 namespace {
 
+__global__ void z_is_in_kernel(const int32_t** z_now, const int32_t* z) { *z_now = z; }
+
 int setup_hybrid(lda_ctx* c, const std::vector<int32_t>& woff);
 
 template <class T>
@@ -586,8 +588,8 @@ int lda_init(lda_ctx** out, int64_t D, int32_t V, int32_t K, const int64_t* doc_
     TRY(dev_alloc(c, &c->d_partial, (size_t)c->n_partial, "partial sums"));
     TRY(setup_loglik(c));
     TRY(dev_alloc(c, &c->d_row, (size_t)K, "row staging"));
-    TRY(dev_alloc(c, &c->d_flag, 4, "flags"));
-    TRY_HIP(hipMemsetAsync(c->d_flag, 0, sizeof(int32_t) * 4, c->stream));
+    TRY(dev_alloc(c, &c->d_flag, 6, "flags"));
+    TRY_HIP(hipMemsetAsync(c->d_flag, 0, sizeof(int32_t) * 6, c->stream));
 
     TRY_HIP(hipMemcpyAsync(c->d_word, word_ids, sizeof(int32_t) * (size_t)N, hipMemcpyHostToDevice,
                            c->stream));
@@ -702,6 +704,16 @@ static void note_capture(lda_ctx* c)
     if (c->n_implied > 0 && !c->implied_in_graph) c->implied_in_graph = stream_is_captured(c);
 }
 
+// After the buffers have changed places (2 us on the stream, where a graph may look at it)
+static int note_z(lda_ctx* c)
+{
+    if (!c->z_in_graph) c->z_in_graph = stream_is_captured(c);
+    if (!c->z_in_graph) return LDA_OK;
+    hipLaunchKernelGGL(z_is_in_kernel, dim3(1), dim3(1), 0, c->stream, c->z_now(), c->d_z);
+    LDA_HIP(c, hipGetLastError());
+    return LDA_OK;
+}
+
 int lda_build_alias(lda_ctx* c)
 {
     if (!c) return LDA_ERR_ARG;
@@ -767,7 +779,7 @@ int lda_sweep(lda_ctx* c, int32_t mh_steps)
     c->sweep_index += 1;
     c->state = SWEPT;
     c->prev_valid = true;
-    return LDA_OK;
+    return note_z(c);
 }
 
 int lda_sweep_pass_ms(lda_ctx* c, float* word_pass_ms, float* doc_pass_ms)
@@ -867,7 +879,7 @@ int lda_set_z(lda_ctx* c, const int32_t* z, int64_t next_sweep_index)
     c->prev_valid = false;
     c->sweep_index = (uint32_t)next_sweep_index;
     c->state = SWEPT;
-    return LDA_OK;
+    return note_z(c);
 }
 
 int lda_get_nk(lda_ctx* c, int32_t* nk)

@@ -314,7 +314,11 @@ struct lda_ctx {
     int32_t n_partial = 0;
     double* d_lg_terms = nullptr;      // log-likelihood terms by count: of alpha, then of beta
     int32_t* d_row = nullptr;          // [max(K,1)] row staging for accessors
-    int32_t* d_flag = nullptr;         // [4] validation; recount wanted; sum of a sample (zero between uses)
+    int32_t* d_flag = nullptr;         // [6] validation; recount wanted; sum of a sample (zero between uses); z_now
+    // What captured work reads the assignment through, as the two buffers change places: the buffer that the last
+    // sweep or lda_set_z has written, 0 before one that says so; they do from the first on that a graph may replay
+    bool z_in_graph = false;
+    const int32_t** z_now() const { return reinterpret_cast<const int32_t**>(d_flag + 4); }
     std::vector<void*> kept;           // replaced while the stream was being captured; freed at the end
     // host copies of small layouts
     std::vector<int32_t> h_doff;

@@ -47,6 +47,7 @@ struct TopicArgs {
     int32_t offsets_type;
     int32_t K;
     const int32_t* z;
+    const int32_t* const* z_now;  // NULL, or where z is instead, if anywhere: work that a graph replays
     int64_t tokens;
     int32_t k;
     double alpha;
@@ -66,6 +67,12 @@ __host__ __device__ __forceinline__ int32_t ranges_of(int32_t K, int64_t L)
     const int32_t range = L < kWideTokens ? kNarrowRange : kWideRange;
     return (K + range - 1) / range;
 }
+__device__ __forceinline__ const int32_t* assignment(const TopicArgs& a)
+{
+    const int32_t* const z = a.z_now ? *a.z_now : nullptr;
+    return z ? z : a.z;
+}
+
 // Split where a workgroup would take long: where 32-bit counters are needed, or a few ranges (where there
 // are more, a table is the better one).
 __device__ __forceinline__ bool split_document(const TopicArgs& a, int64_t L)
@@ -261,6 +268,7 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
 __global__ __launch_bounds__(kWaveBlock, 6) void wave_topics_kernel(TopicArgs a)
 {
     constexpr int kWaves = kWaveBlock / kWave;
+    a.z = assignment(a);
     __shared__ __align__(16) uint32_t table[kWaves][2 * kWaveTopics];
     __shared__ uint16_t used[kWaves][kWaveTopics];
     __shared__ float log_of[kWaveTopics + 1], norm_of[kWaveTopics + 1];  // of count + alpha, of tokens + K alpha
@@ -850,6 +858,7 @@ __global__ __launch_bounds__(kLongBlock) void long_topics_kernel(TopicArgs a)
 {
     extern __shared__ __align__(16) unsigned char raw[];
     LongLds& lds = *reinterpret_cast<LongLds*>(raw);
+    a.z = assignment(a);
     for_rows_left<kLongBlock>(a, lds.mine, &lds.n_mine, [&](int64_t row, int64_t g0, int32_t L) {
         const int32_t mark = a.ids[row * a.k], ranges = ranges_of(a.K, L);
         if (mark <= kSplit) {
@@ -1019,6 +1028,10 @@ try {
     a.offsets_type = LDA_I32;
     a.K = c->K;
     a.z = c->d_z;
+    if (stream_is_captured(c)) {  // replays come after sweeps that the host calls then
+        c->z_in_graph = true;
+        a.z_now = c->z_now();
+    }
     a.tokens = c->N;
     a.k = slots;
     a.alpha = c->alpha;

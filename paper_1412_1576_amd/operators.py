@@ -265,7 +265,8 @@ def top_topics(z, doc_offsets, K, slots, alpha, *, docs=None):
 
 
 def doc_topics(sampler, slots, docs=None):
-    """Lda.doc_topics: top_topics of a sampler's current assignment."""
+    """Lda.doc_topics: top_topics of a sampler's current assignment; captured on the sampler's own stream, of the
+    assignment that there is when the graph is replayed."""
     device = torch.cuda.current_device()
     slots = _int32(slots, "slots")
     if docs is not None:

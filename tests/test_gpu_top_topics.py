@@ -290,3 +290,95 @@ def test_a_sampler_captured(ops):
     torch.cuda.synchronize()
     same(m.doc_topics(10, docs), reference(m.get_z(), doff, cfg.K, 10, cfg.alpha, [100, -1, 150]))
     m.close()
+
+
+def test_a_sampler_captured_and_swept(ops):
+    """A captured call replayed after sweeps and new assignments reads the assignment that there is then, whichever of
+    the sampler's two buffers has it."""
+    from paper_1412_1576_amd import corpus, lda
+    cfg = corpus.scaled(corpus.CONFIGS["c1"], D=150)
+    doff, words = corpus.make_corpus(cfg)
+    stream = torch.cuda.Stream()
+    m = lda.Lda(doff, words, cfg.V, cfg.K, cfg.alpha, cfg.beta, seed=4, stream=stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        m.doc_topics(10)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        got = m.doc_topics(10)
+
+    def replayed():
+        with torch.cuda.stream(stream):
+            graph.replay()
+        torch.cuda.synchronize()
+        same(got, reference(m.get_z(), doff, cfg.K, 10, cfg.alpha, range(cfg.D)))
+
+    replayed()
+    for _ in range(3):
+        m.build_alias()
+        m.sweep(2)
+        replayed()
+        m.rebuild_counts()
+    rng = np.random.default_rng(3)
+    for _ in range(2):
+        m.set_z(rng.integers(0, cfg.K, len(words)).astype(np.int32), m.sweep_index)
+        replayed()
+    m.close()
+
+
+def test_a_sweep_captured_with_its_topics(ops):
+    """An iteration and its topics in one graph, with sweeps by the host between the replays; and the topics in a
+    graph of their own."""
+    from paper_1412_1576_amd import corpus, lda
+    cfg = corpus.scaled(corpus.CONFIGS["c1"], D=150)
+    doff, words = corpus.make_corpus(cfg)
+    stream = torch.cuda.Stream()
+
+    def iterate(m):
+        m.build_alias()
+        m.sweep(2)
+        m.rebuild_counts()
+
+    m = lda.Lda(doff, words, cfg.V, cfg.K, cfg.alpha, cfg.beta, seed=5, stream=stream.cuda_stream)
+    other = lda.Lda(doff, words, cfg.V, cfg.K, cfg.alpha, cfg.beta, seed=5, stream=stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        for _ in range(2):
+            iterate(m)
+        m.doc_topics(10)
+    torch.cuda.synchronize()
+    before, index = m.get_z(), m.sweep_index
+    m.set_z(before, index)  # a sweep captured after another one goes on from what that one has drawn ahead
+    m.rebuild_counts()
+    graph, alone = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        iterate(m)
+        got = m.doc_topics(10)
+    with torch.cuda.graph(alone, stream=stream):
+        after = m.doc_topics(10)
+
+    def one_sweep_from(z):
+        other.set_z(z, index)
+        other.rebuild_counts()
+        iterate(other)
+        return other.get_z()
+
+    # the graph sweeps from one of the two buffers into the other; the host's sweeps take the assignment back into
+    # the first, from the second after the capture and from the first itself later
+    for sweeps in (1, 2, 2):
+        with torch.cuda.stream(stream):
+            graph.replay()
+            alone.replay()
+        torch.cuda.synchronize()
+        z = one_sweep_from(before)
+        for rows in (got, after):
+            same(rows, reference(z, doff, cfg.K, 10, cfg.alpha, range(cfg.D)))
+        m.rebuild_counts()
+        for _ in range(sweeps):
+            iterate(m)
+            before = m.get_z()
+            with torch.cuda.stream(stream):
+                alone.replay()
+            torch.cuda.synchronize()
+            same(after, reference(before, doff, cfg.K, 10, cfg.alpha, range(cfg.D)))
+    m.close()
+    other.close()
