@@ -227,6 +227,8 @@ int lda_loglik_noalloc(lda_ctx* ctx, double* total, double* doc_part, double* wo
 
 /* ---- accessors (parity checks, checkpoint / warm start of Sec. 6); all synchronise ---- */
 int64_t lda_num_tokens(const lda_ctx* ctx);
+/* The device of the context: the current one at lda_init.  -1 for NULL.  (Does not synchronise.) */
+int lda_device(const lda_ctx* ctx);
 int64_t lda_sweep_index(const lda_ctx* ctx);
 /* z [N] in CSR token order. */
 int lda_get_z(lda_ctx* ctx, int32_t* z);
@@ -398,8 +400,9 @@ int64_t lda_topics_workspace(const lda_topic_rows* rows);
 /* ids [rows][slots], logits [rows][slots], log_norm [rows] or NULL */
 int lda_top_topics(const lda_topic_rows* rows, int32_t* ids, float* logits, float* log_norm);
 /* The same from the context's current assignment, its K and alpha, on its stream; docs and the outputs are
- * device pointers.  Any state.  A captured call reads, when it is replayed, what the last sweep or lda_set_z before
- * it on the stream has left.  With stream_block_tokens: LDA_ERR_UNSUPPORTED (z is in host memory). */
+ * device pointers, and the context's device has to be the current one.  Any state.  A captured call reads, when it
+ * is replayed, what the last sweep or lda_set_z before it on the stream has left.  With stream_block_tokens:
+ * LDA_ERR_UNSUPPORTED (z is in host memory). */
 int lda_doc_topics(lda_ctx* ctx, int64_t rows, const int32_t* docs, int32_t slots, int32_t* ids,
                    float* logits, float* log_norm);
 

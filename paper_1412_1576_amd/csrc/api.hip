@@ -475,6 +475,7 @@ int lda_init(lda_ctx** out, int64_t D, int32_t V, int32_t K, const int64_t* doc_
         c->bucket_below = (int32_t)std::max<int64_t>(256, N >> 16);
     }
     c->stream = reinterpret_cast<hipStream_t>(o.hip_stream);
+    if (hipGetDevice(&c->device) != hipSuccess) (void)hipGetLastError();  // (what follows says why)
 
     // sweep tiling parameters (LDS: 12 bytes per token + 4 per document).  A packed n_kd
     // slot holds counts up to 4095, a token's slot index takes 12 bits and its document index
@@ -838,6 +839,7 @@ int lda_loglik(lda_ctx* c, double* total, double* doc_part, double* word_part)
 }
 
 int64_t lda_num_tokens(const lda_ctx* c) { return c ? c->N : -1; }
+int lda_device(const lda_ctx* c) { return c ? c->device : -1; }
 int64_t lda_sweep_index(const lda_ctx* c) { return c ? (int64_t)c->sweep_index : -1; }
 
 int lda_get_z(lda_ctx* c, int32_t* z)

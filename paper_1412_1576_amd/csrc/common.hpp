@@ -91,6 +91,7 @@ struct lda_ctx {
     uint64_t seed = 0;
     lda_options opt{};
     hipStream_t stream = nullptr;
+    int device = -1;          // the current one at lda_init
     int state = 0;
     uint32_t sweep_index = 0;
     bool prev_valid = false;  // d_znew holds the assignment before the last sweep

@@ -1020,6 +1020,10 @@ try {
     if (rc != LDA_OK) return rc;
     if (!docs && rows > c->D) return fail(c, LDA_ERR_ARG, "%s: more rows than documents", call);
     if (!aligned_to(docs, 4)) return fail(c, LDA_ERR_ARG, "%s: a pointer is not aligned to its type", call);
+    int device = -1;
+    LDA_HIP(c, hipGetDevice(&device));
+    if (device != c->device)
+        return fail(c, LDA_ERR_ARG, "%s: device %d has to be the current one, not %d", call, c->device, device);
     TopicArgs a{};
     a.rows = rows;
     a.docs = docs;

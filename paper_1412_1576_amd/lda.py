@@ -24,7 +24,7 @@ LDA_ERR_UNSUPPORTED = -5
 EXPORTS = [
     "lda_init", "lda_build_alias", "lda_sweep", "lda_sweep_pass_ms", "lda_rebuild_counts",
     "lda_update_counts", "lda_loglik", "lda_loglik_noalloc",
-    "lda_num_tokens", "lda_sweep_index", "lda_get_z", "lda_set_z", "lda_get_nk",
+    "lda_num_tokens", "lda_device", "lda_sweep_index", "lda_get_z", "lda_set_z", "lda_get_nk",
     "lda_get_nkw_row", "lda_get_ndk_row", "lda_get_alias_row", "lda_get_sparse_table",
     "lda_get_beta_table",
     "lda_distill_workspace", "lda_distill_loss", "lda_distill_grad", "lda_distill_step",
@@ -134,6 +134,7 @@ def load_library():
         "lda_loglik": (C.c_int, [vp, dp, dp, dp]),
         "lda_loglik_noalloc": (C.c_int, [vp, dp, dp, dp]),
         "lda_num_tokens": (C.c_int64, [vp]),
+        "lda_device": (C.c_int, [vp]),
         "lda_sweep_index": (C.c_int64, [vp]),
         "lda_get_z": (C.c_int, [vp, _i32p]),
         "lda_set_z": (C.c_int, [vp, _i32p, C.c_int64]),
@@ -209,6 +210,7 @@ class Lda:
         if rc != LDA_OK:
             raise LdaError(rc, (L.lda_last_error(None) or b"").decode())
         self.N = int(L.lda_num_tokens(self._h))
+        self.device = int(L.lda_device(self._h))
 
     def _ck(self, rc):
         if rc != LDA_OK:
@@ -289,7 +291,7 @@ class Lda:
         """(ids int32, logits float32, log_norm float32) of documents as torch tensors on the GPU:
         their `slots` most frequent topics with log(n_dk + alpha), and log(L + K alpha) -- teacher
         rows for operators.distill_loss.  docs: int32 GPU tensor (None: every document).  The work is
-        on the context's stream; torch's current stream waits for it."""
+        on the context's stream and device; torch's current stream of that device waits for it."""
         from . import operators
         return operators.doc_topics(self, slots, docs)
 

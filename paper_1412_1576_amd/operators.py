@@ -267,24 +267,25 @@ def top_topics(z, doc_offsets, K, slots, alpha, *, docs=None):
 def doc_topics(sampler, slots, docs=None):
     """Lda.doc_topics: top_topics of a sampler's current assignment; captured on the sampler's own stream, of the
     assignment that there is when the graph is replayed."""
-    device = torch.cuda.current_device()
+    device = sampler.device
     slots = _int32(slots, "slots")
     if docs is not None:
         _tensor(docs, "docs", 1, (torch.int32,), device)
     n = sampler.D if docs is None else docs.numel()
-    apart = _raw_stream(device) != sampler.stream
-    if apart and torch.cuda.is_current_stream_capturing():
-        raise ValueError("doc_topics in a captured stream: only where it is the sampler's own stream")
-    if apart:
-        current = torch.cuda.current_stream(device)
-        own = torch.cuda.ExternalStream(sampler.stream, device=device) if sampler.stream else \
-            torch.cuda.default_stream(device)
-    ids, logits, log_norm = _teacher_rows(n, max(slots, 0), device)
-    if apart:  # docs may still be on their way, and the outputs' memory in use
-        own.wait_stream(current)
-    sampler._ck(lda.load_library().lda_doc_topics(
-        sampler._h, n, None if docs is None else docs.data_ptr(), slots, ids.data_ptr(),
-        logits.data_ptr(), log_norm.data_ptr()))
-    if apart:
-        current.wait_stream(own)
+    with _On(device):
+        apart = _raw_stream(device) != sampler.stream
+        if apart and torch.cuda.is_current_stream_capturing():
+            raise ValueError("doc_topics in a captured stream: only where it is the sampler's own stream")
+        if apart:
+            current = torch.cuda.current_stream(device)
+            own = torch.cuda.ExternalStream(sampler.stream, device=device) if sampler.stream else \
+                torch.cuda.default_stream(device)
+        ids, logits, log_norm = _teacher_rows(n, max(slots, 0), device)
+        if apart:  # docs may still be on their way, and the outputs' memory in use
+            own.wait_stream(current)
+        sampler._ck(lda.load_library().lda_doc_topics(
+            sampler._h, n, None if docs is None else docs.data_ptr(), slots, ids.data_ptr(),
+            logits.data_ptr(), log_norm.data_ptr()))
+        if apart:
+            current.wait_stream(own)
     return ids, logits, log_norm

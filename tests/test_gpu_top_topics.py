@@ -382,3 +382,30 @@ def test_a_sweep_captured_with_its_topics(ops):
             same(after, reference(before, doff, cfg.K, 10, cfg.alpha, range(cfg.D)))
     m.close()
     other.close()
+
+
+def test_a_sampler_on_another_device(ops, monkeypatch):
+    """The call goes to the sampler's device, whichever is the current one, and leaves that as it was."""
+    from paper_1412_1576_amd import corpus, lda
+    cfg = corpus.scaled(corpus.CONFIGS["c1"], D=50)
+    doff, words = corpus.make_corpus(cfg)
+    m = lda.Lda(doff, words, cfg.V, cfg.K, cfg.alpha, cfg.beta, seed=6)
+    want = reference(m.get_z(), doff, cfg.K, 10, cfg.alpha, range(cfg.D))
+    device = torch.cuda.current_device()
+    docs = torch.arange(cfg.D, dtype=torch.int32, device="cuda")
+    made = []
+    with monkeypatch.context() as other:  # the program's device is the next one
+        other.setattr(torch.cuda, "current_device", lambda: device + 1)
+        other.setattr(torch.cuda, "set_device", made.append)
+        got = [m.doc_topics(10), m.doc_topics(10, docs)]
+    assert made == [device, device + 1] * 2
+    for rows in got:
+        assert all(x.get_device() == device for x in rows)
+        same(rows, want)
+    if torch.cuda.device_count() > 1:
+        with torch.cuda.device((device + 1) % torch.cuda.device_count()):
+            same(m.doc_topics(10), want)
+            ids = torch.empty(cfg.D, 10, dtype=torch.int32, device=device)
+            rc = lda.load_library().lda_doc_topics(m._h, cfg.D, None, 10, ids.data_ptr(), ids.data_ptr(), None)
+            assert rc == lda.LDA_ERR_ARG
+    m.close()
