@@ -20,7 +20,14 @@ from .lda import LDA_OK, LdaError
 _FLOATS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 _INDEXES = {torch.int32: 0, torch.int64: 1}
 _INT32 = 2 ** 31 - 1
-_raw_stream = torch._C._cuda_getCurrentRawStream  # of a device's number; what current_stream() wraps
+
+
+def _stream_of(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+# What current_stream() wraps, where torch has it: some 1 us less of a call
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream_of)
 
 
 def _tensor(x, name, dims, types, device=None, shape=None, spread=False):

@@ -229,3 +229,10 @@ def test_streams_and_graphs(ops, B, V):
         for _, got in graphs:
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     check(ops, target, draft, tokens, u, v)
+
+
+def test_streams_by_the_public_way(ops):
+    for stream in (torch.cuda.default_stream(), torch.cuda.Stream()):
+        with torch.cuda.stream(stream):
+            device = torch.cuda.current_device()
+            assert ops._stream_of(device) == ops._raw_stream(device) == stream.cuda_stream

@@ -175,3 +175,13 @@ def test_the_binding_refuses_host_tensors():
         operators.top_topics(torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int64), 4, 2, 0.1)
     with pytest.raises(ValueError, match="on the GPU"):
         operators.distill_loss(None, i, x)
+
+
+def test_the_import_needs_nothing_private_of_torch(monkeypatch):
+    import importlib
+    from paper_1412_1576_amd import operators
+    with monkeypatch.context() as without:
+        without.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+        importlib.reload(operators)
+        assert operators._raw_stream is operators._stream_of
+    importlib.reload(operators)
