@@ -1,5 +1,5 @@
-// What the row operators (distill.hip, verify.hip, top_topics.hip) share: element types, 16-byte
-// loads of rows that start anywhere, reductions over a wave and over a workgroup.
+// What the row operators (distill.hip, verify.hip, top_topics.hip) share: element types, reductions
+// over a wave and over a workgroup.
 #pragma once
 
 #include <hip/hip_bf16.h>
@@ -95,34 +95,6 @@ struct Row<__hip_bfloat16> {
     }
 };
 
-// A row of V elements seen as 16-byte chunks of memory: chunk i holds the elements
-// [i * kChunk - lead, (i + 1) * kChunk - lead) of the row, those outside [0, V) not the row's.
-template <class T>
-struct ChunkedRow {
-    const T* p;
-    int32_t V, lead;
-
-    __device__ __forceinline__ ChunkedRow(const T* row, int32_t V) : p(row), V(V)
-    {
-        lead = (int32_t)(((uintptr_t)row & 15u) / sizeof(T));
-    }
-    __device__ __forceinline__ int32_t chunks() const { return (int32_t)(((int64_t)lead + V + Row<T>::kChunk - 1) / Row<T>::kChunk); }
-    __device__ __forceinline__ int64_t first(int32_t i) const { return (int64_t)i * Row<T>::kChunk - lead; }
-    __device__ __forceinline__ bool whole(int64_t v) const { return v >= 0 && v + Row<T>::kChunk <= V; }
-    // chunk i as floats, `fill` in the places that are not the row's
-    __device__ __forceinline__ void load(int32_t i, float (&x)[Row<T>::kChunk], float fill) const
-    {
-        const int64_t v = first(i);
-        if (whole(v)) {
-            Row<T>::unpack(*reinterpret_cast<const uint4*>(p + v), x);
-        } else {
-#pragma unroll
-            for (int e = 0; e < Row<T>::kChunk; ++e)
-                x[e] = v + e >= 0 && v + e < V ? Row<T>::one(p + v + e) : fill;
-        }
-    }
-};
-
 __device__ __forceinline__ int64_t index_at(const void* p, int32_t type, int64_t i)
 {
     return type == LDA_I32 ? (int64_t) static_cast<const int32_t*>(p)[i] : static_cast<const int64_t*>(p)[i];
@@ -133,14 +105,6 @@ __device__ __forceinline__ float element_at(const void* p, int32_t type, int64_t
     if (type == LDA_F32) return static_cast<const float*>(p)[i];
     if (type == LDA_F16) return Row<__half>::one(static_cast<const __half*>(p) + i);
     return Row<__hip_bfloat16>::one(static_cast<const __hip_bfloat16*>(p) + i);
-}
-
-template <class V, class F>
-__device__ __forceinline__ V wave_reduce(V v, F f)
-{
-#pragma unroll
-    for (int d = kWave / 2; d > 0; d >>= 1) v = f(v, __shfl_xor(v, d, kWave));
-    return v;
 }
 
 // Sums and scans over a whole wave by lane shifts inside the vector ALU (row_shr 1, 2, 4, 8 inside rows of
