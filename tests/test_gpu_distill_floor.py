@@ -169,3 +169,52 @@ def test_what_several_slots_of_a_class_change(ops, tau, rest):
     assert less.min() > 0.01   # (much more than the sides may be off)
     assert ((want.double() - loss.double()) - less).abs().max() < 4e-5
     assert (grad - same).abs().max() < 4e-6
+
+
+def test_the_shapes_are_all_there_are():
+    """SHAPES against the table of the source: each of its rows is chosen by one, and slices by one."""
+    import os
+    import re
+    from paper_1412_1576_amd import build
+    text = open(os.path.join(build.CSRC, "distill.hip")).read()
+    table = re.search(r"kShapes\[\] = \{(.*)\};", text).group(1)
+    table = [tuple(map(int, row.split(","))) for row in re.findall(r"\{([^{}]*)\}", table)]
+    chosen = []
+    for n, v in SHAPES:
+        fits = [s for s in table if v // 4 <= s[0] * s[1]]
+        chosen.append(fits[0] if fits and (fits[0][0] < 1024 or n >= fits[0][2]) else None)
+    assert chosen == table + [None]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_odd_logits_in_every_shape(ops, shape, rest, dtype):
+    """The rows of a batch that takes the shape, each against the definition: masks that leave a thread, or all but one,
+    nothing, numbers that are none, a row without a teacher."""
+    inf = float("inf")
+    n, v = sizes(shape, dtype)
+    n = max(n, 13)
+    x, ids, t = make(n, v, 6, TYPES[dtype], seed=7)
+    low = torch.finfo(x.dtype).min
+    ids[:] = torch.tensor([0, 1, 2, v // 2, v - 2, v - 1], device="cuda")
+    x[0, : v // 2] = low
+    x[1, 10:] = low
+    x[2, :] = low
+    x[3, :] = -inf
+    x[4, 2] = -inf
+    x[5, v // 3] = float("nan")
+    x[6, v - 7] = inf
+    x[7, 20: v - 20] = -inf
+    x[8, :] = -inf
+    x[8, v // 2] = 1.0
+    x[9, v // 5] = float("nan")
+    ids[9] = -1
+    x[10, 2], t[10, 2] = -inf, -inf
+    t.clamp_(max=2.0)
+    norm = torch.full((n,), 4.0, device="cuda") if rest else None
+    if rest:
+        ids[9] = torch.arange(6, device="cuda")
+        t[9], norm[9] = -inf, inf       # a floor alone
+        x[9] = x[11]
+    compare_rows(ops, x, ids, t, list(range(12)) + [n - 1], 1.0, norm)
