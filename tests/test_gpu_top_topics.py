@@ -409,3 +409,26 @@ def test_a_sampler_on_another_device(ops, monkeypatch):
             rc = lda.load_library().lda_doc_topics(m._h, cfg.D, None, 10, ids.data_ptr(), ids.data_ptr(), None)
             assert rc == lda.LDA_ERR_ARG
     m.close()
+
+
+@pytest.mark.parametrize("K", [1000, 1024, 1025, 5000])
+@pytest.mark.parametrize("rows", [7_000, 14_000])
+def test_waves_with_several_documents(ops, rows, K):
+    """More documents than the GPU has waves (6144), then more than two each (from there on the logarithms come from
+    tables): a wave gets empty, short and middle ones, some with too many topics for it and some too long for it, in
+    every order, and what it leaves goes to workgroups with several rows each."""
+    rng = np.random.default_rng(rows + K)
+    kind = rng.choice(5, rows, p=[0.1, 0.5, 0.2, 0.17, 0.03])
+    lengths = np.select([kind == 0, kind == 1, kind == 2, kind == 3],
+                        [0, rng.integers(1, 91, rows), rng.integers(300, 700, rows), rng.integers(700, 1_500, rows)],
+                        rng.integers(4_096, 4_300, rows))
+    after = {(a, b) for a, b in zip(kind[:-6144], kind[6144:])}
+    assert len(after) >= (25 if rows > 12_288 else 20)  # each kind after each in the same wave
+    owner = np.repeat(np.arange(rows), lengths)
+    z = np.where((kind[owner] == 3) | (rng.random(len(owner)) < 0.4), rng.integers(0, K, len(owner)),
+                 (rng.integers(0, 9, len(owner)) * 7919 + owner * 31) % K)
+    offsets = np.concatenate([[0], np.cumsum(lengths)])
+    many = [d for d in np.flatnonzero(kind == 3)[:200] if len(np.unique(z[offsets[d]:offsets[d + 1]])) > 512]
+    assert len(many) > 20
+    check(ops, z, lengths, K, 24)
+    check(ops, z, lengths, K, 24, docs=rng.integers(-1, rows + 1, rows), dtype=np.int32)
