@@ -371,7 +371,10 @@ int lda_verify_drafts(const lda_draft_rows* rows, int32_t* accepted, void* out, 
  * frequent first, ties to the lower topic, with logits log(n + alpha), n the number of
  * tokens; slots without a topic get id -1 and logit -infinity.  log_norm = log(L + K alpha), L the
  * tokens counted: with these three lda_distill_loss learns the document's whole
- * theta_dk = (n_dk + alpha) / (L + K alpha), at temperature 1, when slots holds all of its topics.
+ * theta_dk = (n_dk + alpha) / (L + K alpha), at temperature 1, when slots holds all of its topics.  Logits and log_norm have
+ * 32 bits, so that a slot's mass is off by up to 2^-23 log_norm of itself, and the mass of all classes without a slot,
+ * which is what the slots leave of 1, by as much of 1: of documents whose rest, about K alpha / L, is not far
+ * above 10^-6 (10^5 tokens and more with a small alpha) the loss learns the slots, and the floor's size at most.
  */
 typedef struct lda_topic_rows {
     int64_t rows;            /* rows of output, >= 0 */

@@ -432,3 +432,25 @@ def test_waves_with_several_documents(ops, rows, K):
     assert len(many) > 20
     check(ops, z, lengths, K, 24)
     check(ops, z, lengths, K, 24, docs=rng.integers(-1, rows + 1, rows), dtype=np.int32)
+
+
+@pytest.mark.parametrize("length,K,alpha", [(300, 100, 0.01), (20_000, 1000, 0.05), (440_000, 100, 0.01), (2_000_000, 1000, 0.01)])
+def test_the_floor_that_the_rows_stand_for(ops, length, K, alpha):
+    """What a document's rows leave for the classes without a slot, from the gradient at one of them: T (M q - r) with
+    equal logits, q = 1 / K.  Each mass is off by half a step of its logit and of the norm, 2^-24 of their size, the rest
+    by as much of 1; the gradient by some roundings of q."""
+    rng = np.random.default_rng(length)
+    few = rng.permutation(K)[:K * 6 // 10]
+    z = torch.from_numpy(few[rng.integers(0, len(few), length)].astype(np.int32)).cuda()
+    ids, logits, norm = ops.top_topics(z, torch.tensor([0, length], device="cuda"), K, min(K, 1024), alpha)
+    _, grad = ops.distill_loss_and_grad(torch.zeros(1, K, device="cuda"), ids, logits, log_norm=norm)
+    named = np.unique(z.cpu().numpy())
+    others = np.setdiff1d(np.arange(K), named)
+    r = 1.0 / K - grad[0, others].double().cpu().numpy()
+    size = float(norm[0])
+    off = 2.0 ** -24 * (np.log(length) + size + 2) + len(others) * 8 * 2.0 ** -24 / K
+    assert np.abs(r * len(others) - len(others) * alpha / (length + K * alpha)).max() <= off
+    got = torch.exp(logits[0].double() - norm[0].double()).cpu().numpy()[:len(named)]
+    counts = np.bincount(z.cpu().numpy(), minlength=K)[ids[0].cpu().numpy()[:len(named)]]
+    want = (counts + alpha) / (length + K * alpha)
+    assert (np.abs(got - want) <= want * 2.0 ** -23 * size).all()
