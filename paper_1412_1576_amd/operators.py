@@ -49,6 +49,8 @@ def _tensor(x, name, dims, types, device=None, shape=None, spread=False):
         raise ValueError("%s: elements of a row must be adjacent (call .contiguous())" % name)
     if last > _INT32 and dims > 1:
         raise ValueError("%s: a row has at most 2^31 - 1 elements" % name)
+    if x.is_neg():
+        raise ValueError("%s: a view that negates its memory (call .resolve_neg())" % name)
     return stride
 
 

@@ -467,3 +467,14 @@ def test_many_slots_of_few_classes(ops, V, k, rest):
     full = torch.where((ids >= 0) & (ids < V), t.double(), -torch.inf)
     norm = (torch.logsumexp(full, 1) + 0.3).float() if rest else None
     check(ops, x, ids, t, log_norm=norm)
+
+
+def test_lazily_negated_tensors_are_refused(ops):
+    """The imaginary part of a conjugated tensor is a view whose memory holds the opposite numbers."""
+    x, ids, t = make(4, 100, 5, torch.float32, seed=17)
+    weight = torch.ones(4, dtype=torch.complex64, device="cuda").conj().imag
+    assert weight.is_neg()
+    with pytest.raises(ValueError, match="resolve_neg"):
+        ops.distill_loss_and_grad(x, ids, t, weight=weight)
+    loss, grad = ops.distill_loss_and_grad(x, ids, t, weight=weight.resolve_neg())
+    assert (loss == 0).all() and (grad == 0).all()
