@@ -288,7 +288,8 @@ int lda_get_beta_table(lda_ctx* ctx, uint32_t* split, uint32_t* alias, uint32_t*
  * mass has loss 0 and gradient 0, whatever S holds.  Mass on a class of q_v = 0 makes the loss +infinity; the
  * gradient is the formula's.  NaN or +infinity in S, or in the logit of a slot that is not empty, or masses
  * whose sum 64 bits do not hold, make the row's loss and gradient NaN.
- * The softmax is summed in 32 bits, the teacher's masses and the loss in 64.
+ * The softmax is summed in 32 bits; the teacher's masses are summed in 64 and rounded to 32 each, and the loss is
+ * put together in 64.
  */
 typedef struct lda_distill_rows {
     int64_t rows;            /* >= 0 */

@@ -261,7 +261,7 @@ __device__ __forceinline__ int32_t topics_by_wave(const TopicArgs& a, int64_t ro
     return counted;
 }
 
-// Bound by the number of instructions: 300 000 documents of 330 tokens in 1000 topics, 32 slots, take 360 us (1.3 TB/s of
+// Bound by the number of instructions: 300 000 documents of 330 tokens in 1000 topics, 32 slots, take 370 us (1.3 TB/s of
 // z and outputs), some 320 vector and 500 scalar instructions a document, more than one in every issue
 // slot of the SIMDs.  (Ranking all keys instead of finding a border first, 530 vector and 440 scalar, was 3 % slower.)
 // 100 000 documents of 100 tokens in 10 000 topics: 98 us.
