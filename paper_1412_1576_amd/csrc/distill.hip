@@ -479,7 +479,7 @@ __global__ __launch_bounds__(BLOCK, 4) void distill_rows_kernel(DistillArgs a)
     constexpr int E = Row<T>::kChunk, kSlotsEach = (kMostSlots + BLOCK - 1) / BLOCK;
     // short rows are read before it is known whether they are left out: the weight's latency is theirs too
     constexpr bool kEager = BLOCK * CHUNKS <= 1024;
-    constexpr float kDeep = BLOCK * CHUNKS <= 1024 ? kDeepOfShort : kDeepOfLong;
+    constexpr float kDeep = kEager ? kDeepOfShort : kDeepOfLong;
     extern __shared__ __align__(16) unsigned char lds[];
     __shared__ float2 part2[BLOCK / kWave];
     __shared__ LossSums parts[BLOCK / kWave];
