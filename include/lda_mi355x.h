@@ -256,8 +256,9 @@ int lda_get_beta_table(lda_ctx* ctx, uint32_t* split, uint32_t* alias, uint32_t*
                        uint64_t* mass);
 
 /* ---- operators on rows (beside the sampler; no context) ------------------------------------
- * Teacher rows out of topic counts, the distillation loss that trains a student on them, and the
- * verification of tokens that a draft proposed.  All pointers inside the structs and all outputs
+ * Teacher rows out of topic counts, the distillation loss that trains a student on them, the
+ * verification of tokens that a draft proposed; a classifying head (norm of hidden rows, product with the classes'
+ * weights in 8 bits) and the log probabilities that are read off its logits.  All pointers inside the structs and all outputs
  * are DEVICE pointers; the structs themselves are read on the host during the call.  The calls
  * enqueue on hip_stream (NULL: the null stream) and return; they allocate nothing, wait for
  * nothing and can be captured into a graph.  The current device must be the one that holds the
@@ -409,6 +410,65 @@ int lda_top_topics(const lda_topic_rows* rows, int32_t* ids, float* logits, floa
  * LDA_ERR_UNSUPPORTED (z is in host memory). */
 int lda_doc_topics(lda_ctx* ctx, int64_t rows, const int32_t* docs, int32_t slots, int32_t* ids,
                    float* logits, float* log_norm);
+
+/*
+ * Root-mean-square norm of rows with the residual's addition.  With x [rows][width], r the residual of the
+ * same shape (none: 0) and w the weight [width] (none: 1):
+ *   h = x + r, rounded to the sum's type;  n = h / sqrt(mean over the row of h^2 + eps);  y = n w
+ * y is the norm of the sum as it is written.  A row of zeros with eps = 0 has n = 0.
+ * To 8 bits: scale = max |y| / Q of the row, Q = 127 (LDA_INT8) or 448 (LDA_E4M3, the largest such number), and
+ * out = y / scale, rounded to the nearest number of the type, ties to even, so that out * scale stands for y.  A row
+ * whose max |y| is below 2^-100 has scale 0 and out 0, one with a NaN or an infinity in y has scale NaN and out 0.
+ * Gradient, from y' of y and h' of the sum (NULL: 0), with u = y' w:
+ *   x' = r' = h' + (u - n mean over the row of u n) / sqrt(mean of h^2 + eps);  w' = sum over the rows of y' n
+ * Sums are 32-bit; squares that leave 32 bits are scaled.
+ */
+#define LDA_INT8 0
+#define LDA_E4M3 1
+typedef struct lda_norm_rows {
+    int64_t rows;            /* >= 0 */
+    int32_t width;           /* >= 1 */
+    int32_t x_type;          /* of x, y and their gradients: LDA_F32, LDA_F16, LDA_BF16 */
+    const void* x;           /* [rows][width], rows x_stride apart */
+    int64_t x_stride;
+    const void* residual;    /* [rows][width] or NULL */
+    int64_t residual_stride;
+    const void* weight;      /* [width] or NULL */
+    int32_t weight_type;     /* of the weight and its gradient: x_type or LDA_F32 */
+    int32_t sum_type;        /* of the residual, the sum and their gradients: x_type or LDA_F32 */
+    float eps;               /* >= 0 */
+    int32_t reserved_word;   /* must be zero */
+    void* hip_stream;
+    int32_t reserved[4];     /* must be zero */
+} lda_norm_rows;
+
+typedef struct lda_norm_gradients {
+    const void* y_grad;      /* [rows][width] */
+    int64_t y_grad_stride;
+    const void* sum_grad;    /* [rows][width] or NULL */
+    int64_t sum_grad_stride;
+    const void* sum;         /* lda_norm's; not used without a residual */
+    int64_t sum_stride;
+    const float* stats;      /* lda_norm's */
+    void* x_grad;            /* [rows][width] or NULL */
+    int64_t x_grad_stride;
+    void* residual_grad;     /* [rows][width] or NULL; with x_type = sum_type it is x_grad once more */
+    int64_t residual_grad_stride;
+    void* weight_grad;       /* [width] or NULL */
+    void* workspace;         /* with weight_grad: at least lda_norm_grad_workspace() bytes, aligned to 16 */
+    int64_t workspace_bytes;
+    int32_t reserved[4];     /* must be zero */
+} lda_norm_gradients;
+
+/* y [rows][width]; with a residual sum [rows][width] (otherwise it is not looked at); stats, aligned to 8 bytes:
+ * 2 floats a row for lda_norm_grad, or NULL. */
+int lda_norm(const lda_norm_rows* rows, void* y, int64_t y_stride, void* sum, int64_t sum_stride, float* stats);
+/* out [rows][width], a byte an element, scale [rows]; sum as above */
+int lda_norm_bytes(const lda_norm_rows* rows, int32_t levels, void* out, int64_t out_stride, float* scale, void* sum,
+                   int64_t sum_stride);
+int64_t lda_norm_grad_workspace(const lda_norm_rows* rows);
+/* Of the residual only that there is one is looked at. */
+int lda_norm_grad(const lda_norm_rows* rows, const lda_norm_gradients* gradients);
 
 /* Wait for all work enqueued by this context. */
 int lda_sync(lda_ctx* ctx);

@@ -1,0 +1,628 @@
+// Root-mean-square norm of rows with the residual's addition, to the rows' type or to 8 bits with a scale a
+// row, and its gradient (the formulas stand at lda_norm_rows in lda_mi355x.h).
+//
+// A row is a workgroup's, in registers from its load to its store: a thread holds CHUNKS times 8 elements, 8
+// adjacent ones a chunk, and reads nothing twice.  Rows too wide for that are read again from the cache
+// (CHUNKS = 0).
+#include <type_traits>
+
+#include "rows.hpp"
+
+namespace lda {
+
+constexpr int kNormChunk = 8;
+constexpr int kNormStats = 2;
+constexpr int kGradGroups = 512;  // workgroups of the gradient, each with its sum of the weight's
+
+struct NormArgs {
+    int64_t rows, row0;
+    int32_t H;
+    const void* x;
+    int64_t x_stride;
+    const void* residual;
+    int64_t residual_stride;
+    const void* weight;
+    int32_t weight_type;
+    float eps;
+    void* out;  // y, or 8-bit numbers
+    int64_t out_stride;
+    void* sum;
+    int64_t sum_stride;
+    float* scale;
+    float* stats;  // [rows][kNormStats]
+};
+
+struct NormGradArgs {
+    int64_t rows;
+    int32_t H;
+    const void* h;  // the sum, or x where there is no residual
+    int64_t h_stride;
+    const void* weight;
+    int32_t weight_type;
+    const float* stats;
+    const void* y_grad;
+    int64_t y_grad_stride;
+    const void* sum_grad;
+    int64_t sum_grad_stride;
+    void* x_grad;
+    int64_t x_grad_stride;
+    void* residual_grad;
+    int64_t residual_grad_stride;
+    float* partial;  // [kGradGroups or fewer][H], or NULL: no gradient of the weight
+    void* weight_grad;
+    int32_t groups;
+};
+
+// The 8 elements from p on; p is aligned to its type, which is all that the hardware's loads ask for.
+__device__ __forceinline__ void load8(const float* p, float (&v)[8])
+{
+    __builtin_memcpy(v, p, 32);
+}
+template <class T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8])
+{
+    uint4 r;
+    __builtin_memcpy(&r, p, 16);
+    Row<T>::unpack(r, v);
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) { __builtin_memcpy(p, v, 32); }
+template <class T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8])
+{
+    const uint4 r = Row<T>::pack(v);
+    __builtin_memcpy(p, &r, 16);
+}
+// A row's elements from i on: 8, or what is left of the row with 0 behind it
+template <class T>
+__device__ __forceinline__ void load_some(const T* row, int32_t i, int32_t H, float (&v)[8])
+{
+    if (i + 8 <= H) {
+        load8(row + i, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = i + e < H ? Row<T>::one(row + i + e) : 0.0f;
+    }
+}
+template <class T>
+__device__ __forceinline__ void store_some(T* row, int32_t i, int32_t H, const float (&v)[8])
+{
+    if (i + 8 <= H) {
+        store8(row + i, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (i + e < H) row[i + e] = Row<T>::from(v[e]);
+    }
+}
+template <class T>
+__device__ __forceinline__ void load_weight(const void* w, int32_t type, int32_t i, int32_t H, float (&v)[8])
+{
+    if (!w) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 1.0f;
+    } else if (type == LDA_F32) {
+        load_some(static_cast<const float*>(w), i, H, v);
+    } else {
+        load_some(static_cast<const T*>(w), i, H, v);
+    }
+}
+
+template <int BLOCK>
+__device__ __forceinline__ uint32_t block_top(uint32_t v, uint32_t* part)  // largest, the same in every thread
+{
+    v = (uint32_t)lane_value((int32_t)wave_scan(v, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; }), kWave - 1);
+    if (BLOCK == kWave) return v;
+    __syncthreads();
+    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int w = 1; w < BLOCK / kWave; ++w) v = max(v, part[w]);
+    return v;
+}
+
+// n = (h * first) * second.  first is 1 but where squares leave 32 bits.
+struct NormFactor {
+    float first, second;
+    __device__ __forceinline__ float of(float h) const { return (h * first) * second; }
+};
+// Sums of squares within these are good: none overflowed, and what underflowed is nothing beside them.
+constexpr float kLeastSquares = 0x1p-80f, kMostSquares = 0x1p120f;
+
+__device__ __forceinline__ NormFactor factor_of(float squares, float first, int32_t H, float eps)
+{
+    const float mean = squares / (float)H + eps * first * first;
+    return {first, mean == 0.0f ? 0.0f : 1.0f / sqrtf(mean)};
+}
+// The power of two that brings a magnitude near 1
+__device__ __forceinline__ float power_for(uint32_t top)
+{
+    const int e = (int)(top >> 23);
+    if (e == 255 || top == 0) return 1.0f;
+    return __uint_as_float((uint32_t)max(254 - e, 1) << 23);
+}
+
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// 8 bits: a number's place among the levels, y / scale rounded to nearest even
+constexpr uint32_t kLeastTop = (127 - 100) << 23;  // 2^-100: rows of less count as zeros
+struct Levels {
+    float k, scale;
+    bool none;
+    __device__ __forceinline__ Levels(uint32_t top, float most)
+    {
+        const bool odd = top >= 0x7F800000u;
+        none = odd || top < kLeastTop;
+        scale = odd ? NAN : none ? 0.0f : __uint_as_float(top) / most;
+        k = none ? 0.0f : 1.0f / scale;
+    }
+};
+template <class Q>
+__device__ __forceinline__ uint2 levels_of(const float (&y)[8], const Levels& l);
+template <>
+__device__ __forceinline__ uint2 levels_of<int8_t>(const float (&y)[8], const Levels& l)
+{
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int32_t q = (int32_t)rintf(fminf(fmaxf(y[e] * l.k, -127.0f), 127.0f));
+        w[e / 4] |= ((uint32_t)q & 0xFFu) << (e % 4 * 8);
+    }
+    return make_uint2(w[0], w[1]);
+}
+struct E4m3 {
+    uint8_t bits;
+};
+template <>
+__device__ __forceinline__ uint2 levels_of<E4m3>(const float (&y)[8], const Levels& l)
+{
+    int w[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; e += 4) {
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = fminf(fmaxf(y[e + i] * l.k, -448.0f), 448.0f);
+        w[e / 4] = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], w[e / 4], false);
+        w[e / 4] = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w[e / 4], true);
+    }
+    return make_uint2((uint32_t)w[0], (uint32_t)w[1]);
+}
+template <class Q>
+constexpr float most_of() { return std::is_same<Q, E4m3>::value ? 448.0f : 127.0f; }
+
+template <class Q>
+__device__ __forceinline__ void store_levels(Q* row, int32_t i, int32_t H, const float (&y)[8], const Levels& l)
+{
+    uint2 w = levels_of<Q>(y, l);
+    if (l.none) w = make_uint2(0, 0);
+    if (i + 8 <= H) {
+        __builtin_memcpy(row + i, &w, 8);
+    } else {
+        const uint32_t b[2] = {w.x, w.y};
+        uint8_t* const p = reinterpret_cast<uint8_t*>(row);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (i + e < H) p[i + e] = (uint8_t)(b[e / 4] >> (e % 4 * 8));
+    }
+}
+
+// T: of x and y; S: of the residual and the sum; Q: T, or 8 bits.
+template <class T, class S, class Q, int BLOCK, int CHUNKS>
+__global__ __launch_bounds__(BLOCK) void norm_kernel(NormArgs a)
+{
+    constexpr bool k8 = !std::is_same<Q, T>::value, kWide = CHUNKS == 0;
+    constexpr int kHeld = kWide ? 1 : CHUNKS, kStep = BLOCK * kNormChunk;
+    __shared__ float part[BLOCK / kWave];
+    __shared__ uint32_t part_top[BLOCK / kWave];
+    const int32_t tid = (int32_t)threadIdx.x, H = a.H;
+    const int64_t row = a.row0 + blockIdx.x;
+    const T* const x = static_cast<const T*>(a.x) + row * a.x_stride;
+    const S* const r = a.residual ? static_cast<const S*>(a.residual) + row * a.residual_stride : nullptr;
+    S* const sum = static_cast<S*>(a.sum) + row * a.sum_stride;
+    Q* const out = static_cast<Q*>(a.out) + row * a.out_stride;
+    float h[kHeld][8];
+    // the sum as it is written: what is normed, and what the gradient reads
+    const auto load = [&](int32_t i, float (&v)[8]) {
+        load_some(x, i, H, v);
+        if (!r) return;
+        float b[8];
+        load_some(r, i, H, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const S s = Row<S>::from(v[e] + b[e]);
+            v[e] = Row<S>::one(&s);
+        }
+    };
+    const auto each = [&](auto f) {
+        if (kWide) {
+            for (int32_t i = tid * kNormChunk; i < H; i += kStep) {
+                load(i, h[0]);
+                f(i, h[0]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < CHUNKS; ++j) {
+                const int32_t i = j * kStep + tid * kNormChunk;
+                if (i < H) f(i, h[j]);
+            }
+        }
+    };
+    if (!kWide) {
+#pragma unroll
+        for (int j = 0; j < CHUNKS; ++j) {
+            const int32_t i = j * kStep + tid * kNormChunk;
+            if (i < H) load(i, h[j]);
+        }
+    }
+    float squares = 0.0f;
+    each([&](int32_t i, const float (&v)[8]) {
+        if (r) store_some(sum, i, H, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) squares = __builtin_fmaf(v[e], v[e], squares);
+    });
+    squares = block_sum<BLOCK>(squares, part);
+    float first = 1.0f;
+    // rare: squares left 32 bits and eps does not hide it, or the row is 0
+    if (!(squares + (float)H * a.eps >= kLeastSquares && squares <= kMostSquares)) {
+        uint32_t top = 0;
+        each([&](int32_t, const float (&v)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[e]));
+        });
+        first = power_for(max(block_top<BLOCK>(top, part_top), __float_as_uint(sqrtf(a.eps))));
+        squares = 0.0f;
+        each([&](int32_t, const float (&v)[8]) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) squares = __builtin_fmaf(v[e] * first, v[e] * first, squares);
+        });
+        squares = block_sum<BLOCK>(squares, part);
+    }
+    const NormFactor f = factor_of(squares, first, H, a.eps);
+    if (a.stats && tid == 0) *reinterpret_cast<float2*>(a.stats + row * kNormStats) = make_float2(f.first, f.second);
+    const auto normed = [&](int32_t i, const float (&v)[8], float (&y)[8]) {
+        load_weight<T>(a.weight, a.weight_type, i, H, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = f.of(v[e]) * y[e];
+    };
+    if constexpr (!k8) {
+        each([&](int32_t i, const float (&v)[8]) {
+            float y[8];
+            normed(i, v, y);
+            store_some(out, i, H, y);
+        });
+    } else {
+        uint32_t top = 0;
+        each([&](int32_t i, float (&v)[8]) {
+            float y[8];
+            normed(i, v, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = max(top, i + e < H ? magnitude(y[e]) : 0u);
+            if (!kWide) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = y[e];
+            }
+        });
+        const Levels l(block_top<BLOCK>(top, part_top), most_of<Q>());
+        if (tid == 0) a.scale[row] = l.scale;
+        each([&](int32_t i, const float (&v)[8]) {
+            if (!kWide) {
+                store_levels(out, i, H, v, l);
+            } else {
+                float y[8];
+                normed(i, v, y);
+                store_levels(out, i, H, y, l);
+            }
+        });
+    }
+}
+
+// The gradient of rows blockIdx.x, + gridDim.x, ...; what they give the weight is summed in registers and
+// written as one row of `partial`.
+template <class T, class S, int BLOCK, int CHUNKS>
+__global__ __launch_bounds__(BLOCK) void norm_grad_kernel(NormGradArgs a)
+{
+    constexpr bool kWide = CHUNKS == 0;
+    constexpr int kHeld = kWide ? 1 : CHUNKS, kStep = BLOCK * kNormChunk;
+    __shared__ float part[BLOCK / kWave];
+    const int32_t tid = (int32_t)threadIdx.x, H = a.H;
+    float n[kHeld][8], g[kHeld][8], w[kHeld][8], sums[kHeld][8];
+#pragma unroll
+    for (int j = 0; j < kHeld; ++j) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sums[j][e] = 0.0f;
+        if (!kWide) load_weight<T>(a.weight, a.weight_type, j * kStep + tid * kNormChunk, H, w[j]);
+    }
+    float* const partial = a.partial ? a.partial + (int64_t)blockIdx.x * H : nullptr;
+    bool fresh = true;
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const S* const h = static_cast<const S*>(a.h) + row * a.h_stride;
+        const T* const gy = static_cast<const T*>(a.y_grad) + row * a.y_grad_stride;
+        const S* const gh = a.sum_grad ? static_cast<const S*>(a.sum_grad) + row * a.sum_grad_stride : nullptr;
+        T* const gx = a.x_grad ? static_cast<T*>(a.x_grad) + row * a.x_grad_stride : nullptr;
+        S* const gr = a.residual_grad ? static_cast<S*>(a.residual_grad) + row * a.residual_grad_stride : nullptr;
+        const float2 st = *reinterpret_cast<const float2*>(a.stats + row * kNormStats);
+        const NormFactor f{st.x, st.y};
+        const auto each = [&](auto go) {
+            if (kWide) {
+                for (int32_t i = tid * kNormChunk; i < H; i += kStep) go(i, 0);
+            } else {
+#pragma unroll
+                for (int j = 0; j < CHUNKS; ++j) {
+                    const int32_t i = j * kStep + tid * kNormChunk;
+                    if (i < H) go(i, j);
+                }
+            }
+        };
+        const auto load = [&](int32_t i, int j) {
+            load_some(h, i, H, n[j]);
+            load_some(gy, i, H, g[j]);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) n[j][e] = f.of(n[j][e]);
+            if (kWide) load_weight<T>(a.weight, a.weight_type, i, H, w[j]);
+        };
+        if (!kWide) each(load);
+        float along = 0.0f;
+        each([&](int32_t i, int j) {
+            if (kWide) load(i, j);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float gn = g[j][e] * n[j][e];
+                if (kWide) sums[0][e] = gn;
+                else if (i + e < H) sums[j][e] += gn;
+                along = __builtin_fmaf(gn, i + e < H ? w[j][e] : 0.0f, along);
+            }
+            if (kWide && partial) {
+                float before[8];
+                if (!fresh) load_some(partial, i, H, before);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) before[e] = fresh ? sums[0][e] : before[e] + sums[0][e];
+                store_some(partial, i, H, before);
+            }
+        });
+        fresh = false;
+        if (!gx && !gr) continue;
+        along = block_sum<BLOCK>(along, part) / (float)H;
+        each([&](int32_t i, int j) {
+            if (kWide) load(i, j);
+            float b[8];
+            if (gh) load_some(gh, i, H, b);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = ((g[j][e] * w[j][e] - n[j][e] * along) * f.second) * f.first;
+                b[e] = gh ? b[e] + d : d;
+            }
+            if (gx) store_some(gx, i, H, b);
+            if (gr) store_some(gr, i, H, b);
+        });
+    }
+    if (!kWide && partial) {
+#pragma unroll
+        for (int j = 0; j < kHeld; ++j) {
+            const int32_t i = j * kStep + tid * kNormChunk;
+            if (i < H) store_some(partial, i, H, sums[j]);
+        }
+    }
+}
+
+// The weight's gradient: a column's partial sums, in order.
+constexpr int kWeightBlock = 64;
+template <class W>
+__global__ __launch_bounds__(kWeightBlock * 4) void norm_weight_grad_kernel(NormGradArgs a)
+{
+    __shared__ float part[4][kWeightBlock];
+    const int32_t column = (int32_t)(blockIdx.x * kWeightBlock + threadIdx.x % kWeightBlock), q = threadIdx.x / kWeightBlock;
+    float s = 0.0f;
+    if (column < a.H) {
+#pragma unroll 8
+        for (int32_t i = q; i < a.groups; i += 4) s += a.partial[(int64_t)i * a.H + column];
+    }
+    part[q][threadIdx.x % kWeightBlock] = s;
+    __syncthreads();
+    if (q != 0 || column >= a.H) return;
+    s = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+    static_cast<W*>(a.weight_grad)[column] = Row<W>::from(s);
+}
+
+static int check_norm(const lda_norm_rows* d, const char* call)
+{
+    if (!d) return fail(nullptr, LDA_ERR_ARG, "%s: NULL rows", call);
+    for (int32_t r : d->reserved)
+        if (r != 0) return fail(nullptr, LDA_ERR_ARG, "%s: reserved fields must be zero", call);
+    if (d->reserved_word != 0) return fail(nullptr, LDA_ERR_ARG, "%s: reserved fields must be zero", call);
+    if (d->rows < 0 || d->width < 1) return fail(nullptr, LDA_ERR_ARG, "%s: rows >= 0 and width >= 1 needed", call);
+    if (!known_type(d->x_type) || !known_type(d->sum_type) || !known_type(d->weight_type))
+        return fail(nullptr, LDA_ERR_ARG, "%s: unknown type", call);
+    if (d->sum_type != d->x_type && d->sum_type != LDA_F32)
+        return fail(nullptr, LDA_ERR_ARG, "%s: the sum has x's type or 32 bits", call);
+    if (d->weight_type != d->x_type && d->weight_type != LDA_F32)
+        return fail(nullptr, LDA_ERR_ARG, "%s: the weight has x's type or 32 bits", call);
+    if (!(d->eps >= 0.0f) || !(d->eps <= 3.0e38f))
+        return fail(nullptr, LDA_ERR_ARG, "%s: eps must be finite and not negative", call);
+    if (!aligned_to(d->weight, type_bytes(d->weight_type)))
+        return fail(nullptr, LDA_ERR_ARG, "%s: a pointer is not aligned to its type", call);
+    return LDA_OK;
+}
+
+// Threads and chunks of a thread that hold a row; 0 chunks: a row too wide for registers
+struct NormShape {
+    int block, chunks;
+};
+static NormShape norm_shape(int32_t H)
+{
+    static constexpr NormShape kShapes[] = {{64, 1}, {256, 1}, {512, 1}, {512, 2}, {1024, 2}};
+    for (const NormShape& s : kShapes)
+        if (H <= s.block * s.chunks * kNormChunk) return s;
+    return {1024, 0};
+}
+
+template <class F>
+static void with_shape(NormShape s, F f)
+{
+    using std::integral_constant;
+    if (s.block == 64) f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (s.block == 256) f(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+    else if (s.block == 512 && s.chunks == 1) f(integral_constant<int, 512>{}, integral_constant<int, 1>{});
+    else if (s.block == 512) f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+    else if (s.chunks == 2) f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    else f(integral_constant<int, 1024>{}, integral_constant<int, 0>{});
+}
+template <class F>
+static void with_types(int32_t x, int32_t sum, F f)
+{
+    if (x == LDA_F32) f(float{}, float{});
+    else if (x == LDA_F16 && sum == LDA_F32) f(__half{}, float{});
+    else if (x == LDA_F16) f(__half{}, __half{});
+    else if (sum == LDA_F32) f(__hip_bfloat16{}, float{});
+    else f(__hip_bfloat16{}, __hip_bfloat16{});
+}
+
+// levels: -1 for y in x's type, else LDA_INT8 or LDA_E4M3
+static int launch_norm(const lda_norm_rows* d, const char* call, int32_t levels, void* out, int64_t out_stride, float* scale,
+                       void* sum, int64_t sum_stride, float* stats)
+{
+    if (d->rows == 0) return LDA_OK;
+    if (!d->x || !out || (d->residual && !sum)) return fail(nullptr, LDA_ERR_ARG, "%s: NULL pointer", call);
+    const size_t xb = type_bytes(d->x_type), sb = type_bytes(d->sum_type);
+    if (!aligned_to(d->x, xb) || !aligned_to(d->residual, sb) || !aligned_to(sum, sb) || !aligned_to(scale, 4) ||
+        !aligned_to(stats, 8) || !aligned_to(out, levels < 0 ? xb : 1))
+        return fail(nullptr, LDA_ERR_ARG, "%s: a pointer is not aligned to its type", call);
+    if (d->rows > 1 && (out_stride < d->width || (d->residual && sum_stride < d->width)))
+        return fail(nullptr, LDA_ERR_ARG, "%s: rows of an output overlap", call);
+    NormArgs a{};
+    a.rows = d->rows;
+    a.H = d->width;
+    a.x = d->x;
+    a.x_stride = d->x_stride;
+    a.residual = d->residual;
+    a.residual_stride = d->residual_stride;
+    a.weight = d->weight;
+    a.weight_type = d->weight_type;
+    a.eps = d->eps;
+    a.out = out;
+    a.out_stride = out_stride;
+    a.sum = sum;
+    a.sum_stride = sum_stride;
+    a.scale = scale;
+    a.stats = stats;
+    const hipStream_t stream = static_cast<hipStream_t>(d->hip_stream);
+    with_types(d->x_type, d->sum_type, [&](auto t, auto s) {
+        with_shape(norm_shape(a.H), [&](auto block, auto chunks) {
+            using T = decltype(t);
+            using S = decltype(s);
+            for (a.row0 = 0; a.row0 < a.rows; a.row0 += 1 << 20) {
+                const unsigned n = (unsigned)(a.rows - a.row0 < (1 << 20) ? a.rows - a.row0 : 1 << 20);
+                if (levels < 0) norm_kernel<T, S, T, block(), chunks()><<<n, block(), 0, stream>>>(a);
+                else if (levels == LDA_INT8) norm_kernel<T, S, int8_t, block(), chunks()><<<n, block(), 0, stream>>>(a);
+                else norm_kernel<T, S, E4m3, block(), chunks()><<<n, block(), 0, stream>>>(a);
+            }
+        });
+    });
+    LDA_HIP(static_cast<lda_ctx*>(nullptr), hipGetLastError());
+    return LDA_OK;
+}
+
+static int32_t grad_groups(const lda_norm_rows* d) { return (int32_t)(d->rows < kGradGroups ? d->rows : kGradGroups); }
+
+}  // namespace lda
+
+using namespace lda;
+
+extern "C" {
+
+int lda_norm(const lda_norm_rows* d, void* y, int64_t y_stride, void* sum, int64_t sum_stride, float* stats)
+try {
+    const int rc = check_norm(d, "lda_norm");
+    if (rc != LDA_OK) return rc;
+    return launch_norm(d, "lda_norm", -1, y, y_stride, nullptr, sum, sum_stride, stats);
+} catch (...) {
+    return LDA_ERR_OOM;
+}
+
+int lda_norm_bytes(const lda_norm_rows* d, int32_t levels, void* out, int64_t out_stride, float* scale, void* sum,
+                   int64_t sum_stride)
+try {
+    const int rc = check_norm(d, "lda_norm_bytes");
+    if (rc != LDA_OK) return rc;
+    if (levels != LDA_INT8 && levels != LDA_E4M3) return fail(nullptr, LDA_ERR_ARG, "lda_norm_bytes: unknown type");
+    if (d->rows > 0 && !scale) return fail(nullptr, LDA_ERR_ARG, "lda_norm_bytes: NULL scale");
+    return launch_norm(d, "lda_norm_bytes", levels, out, out_stride, scale, sum, sum_stride, nullptr);
+} catch (...) {
+    return LDA_ERR_OOM;
+}
+
+int64_t lda_norm_grad_workspace(const lda_norm_rows* d)
+try {
+    const int rc = check_norm(d, "lda_norm_grad_workspace");
+    if (rc != LDA_OK) return rc;
+    return (int64_t)grad_groups(d) * d->width * (int64_t)sizeof(float);
+} catch (...) {
+    return LDA_ERR_OOM;
+}
+
+int lda_norm_grad(const lda_norm_rows* d, const lda_norm_gradients* g)
+try {
+    const int rc = check_norm(d, "lda_norm_grad");
+    if (rc != LDA_OK) return rc;
+    if (!g) return fail(nullptr, LDA_ERR_ARG, "lda_norm_grad: NULL gradients");
+    for (int32_t r : g->reserved)
+        if (r != 0) return fail(nullptr, LDA_ERR_ARG, "lda_norm_grad: reserved fields must be zero");
+    const size_t xb = type_bytes(d->x_type), sb = type_bytes(d->sum_type);
+    const bool with_weight = g->weight_grad != nullptr;
+    if (!aligned_to(g->weight_grad, type_bytes(d->weight_type)))
+        return fail(nullptr, LDA_ERR_ARG, "lda_norm_grad: a pointer is not aligned to its type");
+    if (d->rows == 0 && !with_weight) return LDA_OK;
+    const void* h = d->residual ? g->sum : d->x;
+    if (d->rows > 0) {
+        if (!h || !g->stats || !g->y_grad) return fail(nullptr, LDA_ERR_ARG, "lda_norm_grad: NULL pointer");
+        if (!aligned_to(h, d->residual ? sb : xb) || !aligned_to(g->y_grad, xb) || !aligned_to(g->sum_grad, sb) ||
+            !aligned_to(g->stats, 8) || !aligned_to(g->x_grad, xb) || !aligned_to(g->residual_grad, sb))
+            return fail(nullptr, LDA_ERR_ARG, "lda_norm_grad: a pointer is not aligned to its type");
+        if (d->rows > 1 && ((g->x_grad && g->x_grad_stride < d->width) || (g->residual_grad && g->residual_grad_stride < d->width)))
+            return fail(nullptr, LDA_ERR_ARG, "lda_norm_grad: rows of an output overlap");
+    }
+    NormGradArgs a{};
+    a.rows = d->rows;
+    a.H = d->width;
+    a.h = h;
+    a.h_stride = d->residual ? g->sum_stride : d->x_stride;
+    a.weight = d->weight;
+    a.weight_type = d->weight_type;
+    a.stats = g->stats;
+    a.y_grad = g->y_grad;
+    a.y_grad_stride = g->y_grad_stride;
+    a.sum_grad = g->sum_grad;
+    a.sum_grad_stride = g->sum_grad_stride;
+    a.x_grad = g->x_grad;
+    a.x_grad_stride = g->x_grad_stride;
+    a.residual_grad = g->residual_grad;
+    a.residual_grad_stride = g->residual_grad_stride;
+    a.weight_grad = g->weight_grad;
+    a.groups = grad_groups(d);
+    if (with_weight && d->rows > 0) {
+        const int64_t need = (int64_t)a.groups * a.H * (int64_t)sizeof(float);
+        if (!g->workspace || g->workspace_bytes < need || !aligned_to(g->workspace, 16))
+            return fail(nullptr, LDA_ERR_ARG, "lda_norm_grad: needs a workspace of %lld bytes, aligned to 16", (long long)need);
+        a.partial = static_cast<float*>(g->workspace);
+    }
+    const hipStream_t stream = static_cast<hipStream_t>(d->hip_stream);
+    // without a residual the sum is x
+    with_types(d->x_type, d->residual ? d->sum_type : d->x_type, [&](auto t, auto s) {
+        using T = decltype(t);
+        using S = decltype(s);
+        if (a.rows > 0 && (a.x_grad || a.residual_grad || a.partial))
+            with_shape(norm_shape(a.H), [&](auto block, auto chunks) {
+                // without sums of the weight's a workgroup a row would do as well
+                norm_grad_kernel<T, S, block(), chunks()><<<a.groups, block(), 0, stream>>>(a);
+            });
+        if (!with_weight) return;
+        const unsigned n = (unsigned)((a.H + kWeightBlock - 1) / kWeightBlock);
+        if (d->weight_type == LDA_F32) norm_weight_grad_kernel<float><<<n, kWeightBlock * 4, 0, stream>>>(a);
+        else norm_weight_grad_kernel<T><<<n, kWeightBlock * 4, 0, stream>>>(a);
+    });
+    LDA_HIP(static_cast<lda_ctx*>(nullptr), hipGetLastError());
+    return LDA_OK;
+} catch (...) {
+    return LDA_ERR_OOM;
+}
+
+}  // extern "C"

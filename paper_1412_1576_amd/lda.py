@@ -29,7 +29,7 @@ EXPORTS = [
     "lda_get_beta_table",
     "lda_distill_workspace", "lda_distill_loss", "lda_distill_grad", "lda_distill_step",
     "lda_verify_workspace", "lda_verify_drafts", "lda_topics_workspace", "lda_top_topics",
-    "lda_doc_topics", "lda_sync", "lda_last_error", "lda_destroy",
+    "lda_doc_topics", "lda_norm", "lda_norm_bytes", "lda_norm_grad_workspace", "lda_norm_grad", "lda_sync", "lda_last_error", "lda_destroy",
 ]
 
 
@@ -95,6 +95,29 @@ class lda_topic_rows(C.Structure):
     ]
 
 
+class lda_norm_rows(C.Structure):
+    _fields_ = [
+        ("rows", C.c_int64), ("width", C.c_int32), ("x_type", C.c_int32),
+        ("x", C.c_void_p), ("x_stride", C.c_int64),
+        ("residual", C.c_void_p), ("residual_stride", C.c_int64),
+        ("weight", C.c_void_p), ("weight_type", C.c_int32), ("sum_type", C.c_int32),
+        ("eps", C.c_float), ("reserved_word", C.c_int32), ("hip_stream", C.c_void_p),
+        ("reserved", C.c_int32 * 4),
+    ]
+
+
+class lda_norm_gradients(C.Structure):
+    _fields_ = [
+        ("y_grad", C.c_void_p), ("y_grad_stride", C.c_int64),
+        ("sum_grad", C.c_void_p), ("sum_grad_stride", C.c_int64),
+        ("sum", C.c_void_p), ("sum_stride", C.c_int64), ("stats", C.c_void_p),
+        ("x_grad", C.c_void_p), ("x_grad_stride", C.c_int64),
+        ("residual_grad", C.c_void_p), ("residual_grad_stride", C.c_int64),
+        ("weight_grad", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64),
+        ("reserved", C.c_int32 * 4),
+    ]
+
+
 class LdaError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__("lda error %d: %s" % (code, msg))
@@ -156,6 +179,10 @@ def load_library():
         "lda_topics_workspace": (C.c_int64, [C.POINTER(lda_topic_rows)]),
         "lda_top_topics": (C.c_int, [C.POINTER(lda_topic_rows), vp, vp, vp]),
         "lda_doc_topics": (C.c_int, [vp, C.c_int64, vp, C.c_int32, vp, vp, vp]),
+        "lda_norm": (C.c_int, [C.POINTER(lda_norm_rows), vp, C.c_int64, vp, C.c_int64, vp]),
+        "lda_norm_bytes": (C.c_int, [C.POINTER(lda_norm_rows), C.c_int32, vp, C.c_int64, vp, vp, C.c_int64]),
+        "lda_norm_grad_workspace": (C.c_int64, [C.POINTER(lda_norm_rows)]),
+        "lda_norm_grad": (C.c_int, [C.POINTER(lda_norm_rows), C.POINTER(lda_norm_gradients)]),
         "lda_sync": (C.c_int, [vp]),
         "lda_last_error": (C.c_char_p, [vp]),
         "lda_destroy": (None, [vp]),

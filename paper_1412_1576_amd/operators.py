@@ -4,6 +4,8 @@
   distill_loss                 distillation from a teacher's top logits, with autograd
   distill_loss_and_grad        the same and its gradient in one call, for weights known beforehand
   verify_drafts                drafted tokens accepted or redrawn from given random numbers
+  rms_norm                     root-mean-square norm with the residual's addition, with autograd
+  rms_norm_8bit                the same to 8 bits with a scale a row
 
 Work goes to torch's current stream of the tensors' device (inputs made on another stream have to
 be ready on it); outputs and workspaces come from torch's allocator; no call waits for the GPU, and
@@ -298,3 +300,141 @@ def doc_topics(sampler, slots, docs=None):
         if apart:
             current.wait_stream(own)
     return ids, logits, log_norm
+
+
+def _wants_gradient(*tensors):
+    return torch.is_grad_enabled() and any(t is not None and getattr(t, "requires_grad", False) for t in tensors)
+
+
+def _check_norm(x, weight, residual):
+    in_x = _tensor(x, "x", 2, _FLOATS)
+    device = x.get_device()
+    if x.shape[1] < 1:
+        raise ValueError("x: at least one element a row needed")
+    same = (x.dtype, torch.float32)
+    if weight is not None:
+        _tensor(weight, "weight", 1, same, device, x.shape[1:])
+    in_residual = None if residual is None else _tensor(residual, "residual", 2, same, device, x.shape)
+    return device, in_x, in_residual
+
+
+def _norm_rows(x, in_x, weight, residual, in_residual, eps, device):
+    # in the order of the struct's fields
+    rows, width = x.shape
+    return lda.lda_norm_rows(
+        rows, width, _FLOATS[x.dtype], x.data_ptr(), in_x[0],
+        None if residual is None else residual.data_ptr(), 0 if residual is None else in_residual[0],
+        None if weight is None else weight.data_ptr(), _FLOATS[x.dtype if weight is None else weight.dtype],
+        _FLOATS[x.dtype if residual is None else residual.dtype], eps, 0, _raw_stream(device))
+
+
+def _norm(x, weight, residual, eps, with_stats):
+    """(y, sum or x itself, stats or None)"""
+    device, in_x, in_residual = _check_norm(x, weight, residual)
+    L = lda.load_library()
+    rows, width = x.shape
+    with _On(device):
+        r = _norm_rows(x, in_x, weight, residual, in_residual, eps, device)
+        y = torch.empty((rows, width), dtype=x.dtype, device=x.device)
+        h = x if residual is None else torch.empty((rows, width), dtype=residual.dtype, device=x.device)
+        stats = torch.empty((rows, 2), dtype=torch.float32, device=x.device) if with_stats else None
+        _check(L.lda_norm(r, y.data_ptr(), width, h.data_ptr(), width, stats.data_ptr() if with_stats else None))
+    return y, h, stats
+
+
+def _rows_of(g):
+    """An upstream gradient with adjacent elements."""
+    g = g.resolve_neg()
+    return g if g.stride(1) == 1 or g.size(1) <= 1 else g.contiguous()
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        y, h, stats = _norm(x, weight, residual, eps, True)
+        ctx.save_for_backward(weight, h, stats)
+        ctx.summed = residual is not None
+        ctx.eps, ctx.x_type = eps, x.dtype
+        ctx.set_materialize_grads(False)
+        return (y, h) if ctx.summed else y
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, y_grad, h_grad=None):
+        weight, h, stats = ctx.saved_tensors
+        if y_grad is None:  # the sum alone was used
+            to_x = None if h_grad is None or not ctx.needs_input_grad[0] else h_grad.to(ctx.x_type)
+            return to_x, None, h_grad, None
+        L = lda.load_library()
+        device = h.get_device()
+        rows, width = h.shape
+        to_x, to_weight, to_residual, _ = ctx.needs_input_grad
+        with _On(device):
+            y_grad = _rows_of(y_grad)
+            h_grad = None if h_grad is None else _rows_of(h_grad)
+            # x is looked at only where there is no residual, and is the sum there
+            r = lda.lda_norm_rows(
+                rows, width, _FLOATS[y_grad.dtype], h.data_ptr(), h.stride(0),
+                h.data_ptr() if ctx.summed else None, 0, None if weight is None else weight.data_ptr(),
+                _FLOATS[y_grad.dtype if weight is None else weight.dtype], _FLOATS[h.dtype], ctx.eps, 0,
+                _raw_stream(device))
+            one = h.dtype == y_grad.dtype  # gradients of x and of the residual are the same
+            x_grad = torch.empty((rows, width), dtype=y_grad.dtype, device=h.device) \
+                if to_x or one and to_residual else None
+            residual_grad = torch.empty((rows, width), dtype=h.dtype, device=h.device) \
+                if to_residual and not one else None
+            weight_grad = torch.empty(width, dtype=weight.dtype, device=h.device) if to_weight else None
+            g = lda.lda_norm_gradients(
+                y_grad.data_ptr(), y_grad.stride(0), None if h_grad is None else h_grad.data_ptr(),
+                0 if h_grad is None else h_grad.stride(0), h.data_ptr(), h.stride(0), stats.data_ptr(),
+                None if x_grad is None else x_grad.data_ptr(), width,
+                None if residual_grad is None else residual_grad.data_ptr(), width,
+                None if weight_grad is None else weight_grad.data_ptr())
+            w = _workspace(g, _check(L.lda_norm_grad_workspace(r)) if to_weight else 0, h.device)
+            _check(L.lda_norm_grad(r, g))
+            del w
+        return x_grad if to_x else None, weight_grad, (x_grad if one else residual_grad) if to_residual else None, None
+
+
+def rms_norm(x, weight=None, *, residual=None, eps=1e-6):
+    """y, or (y, sum) with a residual: y = weight * sum / sqrt(mean of sum^2 over the row + eps), sum = x + residual.
+
+    x [rows, width] float32, float16 or bfloat16; weight [width] and residual [rows, width] of x's type or
+    float32.  The sum has the residual's type and y is the norm of the sum as it is written, in x's type.
+    Differentiable in x, weight and residual; sums are 32-bit.  Rows of a tensor may lie any distance
+    apart; within a row elements are adjacent.  A backward pass captured into a graph must find no eager graph of
+    the same leaves alive.
+    """
+    eps = float(eps)
+    if _wants_gradient(x, weight, residual):
+        return _RmsNorm.apply(x, weight, residual, eps)
+    y, h, _ = _norm(x, weight, residual, eps, False)
+    return y if residual is None else (y, h)
+
+
+_LEVELS = {torch.int8: 0, torch.float8_e4m3fn: 1}
+
+
+def rms_norm_8bit(x, weight=None, *, residual=None, eps=1e-6, dtype=torch.int8):
+    """(q, scale), or (q, scale, sum) with a residual: rms_norm's y in 8 bits, q [rows, width] int8 or float8_e4m3fn, times
+    scale, float32 [rows].
+
+    The scale brings the largest |y| of a row to 127 or 448; q is y / scale, rounded to nearest, ties to even.  A
+    row of zeros has scale 0, a row with a NaN or an infinity scale NaN and q 0.  No gradient: tensors that require one are
+    refused outside torch.no_grad().
+    """
+    if dtype not in _LEVELS:
+        raise ValueError("dtype must be torch.int8 or torch.float8_e4m3fn, not %s" % dtype)
+    device, in_x, in_residual = _check_norm(x, weight, residual)
+    if _wants_gradient(x, weight, residual):
+        raise ValueError("rms_norm_8bit has no gradient (call .detach(), or rms_norm)")
+    L = lda.load_library()
+    rows, width = x.shape
+    with _On(device):
+        r = _norm_rows(x, in_x, weight, residual, in_residual, eps, device)
+        q = torch.empty((rows, width), dtype=dtype, device=x.device)
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+        h = None if residual is None else torch.empty((rows, width), dtype=residual.dtype, device=x.device)
+        _check(L.lda_norm_bytes(r, _LEVELS[dtype], q.data_ptr(), width, scale.data_ptr(),
+                                None if h is None else h.data_ptr(), width))
+    return (q, scale) if h is None else (q, scale, h)

@@ -1,0 +1,109 @@
+"""Refusals of the head's operators that need no GPU: the library's own checks of sizes, types, pointers and
+alignment, and the binding's checks of tensors."""
+import ctypes as C
+import os
+
+import pytest
+import torch
+
+from paper_1412_1576_amd import lda
+
+OUT = 1 << 21
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(lda.LIB_PATH):
+        from paper_1412_1576_amd import build
+        build.build_library()
+    return lda.load_library()
+
+
+def message(lib):
+    return lib.lda_last_error(None).decode()
+
+
+def norm(**kw):
+    r = lda.lda_norm_rows()
+    r.rows, r.width, r.x, r.x_stride, r.eps = 4, 100, 1 << 20, 100, 1e-6
+    r.residual, r.residual_stride, r.weight = 1 << 20, 100, 1 << 20
+    r.x_type = r.sum_type = r.weight_type = 2
+    for k, v in kw.items():
+        setattr(r, k, v)
+    return r
+
+
+def gradients(**kw):
+    g = lda.lda_norm_gradients()
+    g.y_grad = g.sum_grad = g.sum = g.stats = 1 << 20
+    g.y_grad_stride = g.sum_grad_stride = g.sum_stride = 100
+    g.x_grad = g.residual_grad = g.weight_grad = g.workspace = OUT
+    g.x_grad_stride = g.residual_grad_stride = 100
+    g.workspace_bytes = 1 << 20
+    for k, v in kw.items():
+        setattr(g, k, v)
+    return g
+
+
+@pytest.mark.parametrize("kw", [
+    dict(rows=-1), dict(width=0), dict(x_type=3), dict(weight_type=-1), dict(sum_type=4), dict(sum_type=1),
+    dict(weight_type=1), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")), dict(weight=(1 << 20) + 1),
+    dict(x=None), dict(x=(1 << 20) + 1), dict(residual=(1 << 20) + 1), dict(reserved_word=1)])
+def test_norm_refuses(lib, kw):
+    r = norm(**kw)
+    assert lib.lda_norm(r, OUT, 100, OUT, 100, OUT) == lda.LDA_ERR_ARG and "lda_norm:" in message(lib)
+    assert lib.lda_norm_bytes(r, 0, OUT, 100, OUT, OUT, 100) == lda.LDA_ERR_ARG and "lda_norm_bytes:" in message(lib)
+    if not set(kw) & {"x", "residual"}:  # the gradient looks at the sum instead
+        assert lib.lda_norm_grad(r, gradients()) == lda.LDA_ERR_ARG
+        assert lib.lda_norm_grad_workspace(r) == lda.LDA_ERR_ARG
+
+
+def test_norm_refuses_outputs(lib):
+    r = norm()
+    for args in ((None, 100, OUT, 100, OUT), (OUT + 1, 100, OUT, 100, OUT), (OUT, 99, OUT, 100, OUT),
+                 (OUT, 100, None, 100, OUT), (OUT, 100, OUT + 1, 100, OUT), (OUT, 100, OUT, 99, OUT),
+                 (OUT, 100, OUT, 100, OUT + 4)):
+        assert lib.lda_norm(r, *args) == lda.LDA_ERR_ARG, args
+    for args in ((2, OUT, 100, OUT, OUT, 100), (-1, OUT, 100, OUT, OUT, 100), (0, None, 100, OUT, OUT, 100),
+                 (0, OUT, 100, None, OUT, 100), (0, OUT, 100, OUT + 2, OUT, 100), (1, OUT, 99, OUT, OUT, 100),
+                 (1, OUT, 100, OUT, None, 100)):
+        assert lib.lda_norm_bytes(r, *args) == lda.LDA_ERR_ARG, args
+    assert lib.lda_norm(None, OUT, 100, OUT, 100, OUT) == lda.LDA_ERR_ARG
+    r.reserved[3] = 1
+    assert lib.lda_norm(r, OUT, 100, OUT, 100, OUT) == lda.LDA_ERR_ARG
+
+
+@pytest.mark.parametrize("kw", [
+    dict(y_grad=None), dict(sum=None), dict(stats=None), dict(y_grad=(1 << 20) + 1), dict(sum_grad=(1 << 20) + 1),
+    dict(stats=(1 << 20) + 4), dict(x_grad=OUT + 1), dict(residual_grad=OUT + 1), dict(weight_grad=OUT + 1),
+    dict(x_grad_stride=99), dict(residual_grad_stride=99), dict(workspace=None), dict(workspace_bytes=4 * 400 - 1),
+    dict(workspace=OUT + 8)])
+def test_norm_gradient_refuses(lib, kw):
+    assert lib.lda_norm_grad_workspace(norm()) == 4 * 400
+    assert lib.lda_norm_grad(norm(), gradients(**kw)) == lda.LDA_ERR_ARG and "lda_norm_grad:" in message(lib)
+
+
+def test_norm_of_no_rows(lib):
+    r = norm(rows=0, x=None)
+    assert lib.lda_norm(r, None, 0, None, 0, None) == lda.LDA_OK
+    assert lib.lda_norm_bytes(r, 0, None, 0, None, None, 0) == lda.LDA_OK
+    assert lib.lda_norm_grad_workspace(r) == 0
+    assert lib.lda_norm_grad(r, gradients(weight_grad=None)) == lda.LDA_OK
+    assert lib.lda_norm_grad(r, None) == lda.LDA_ERR_ARG
+    g = gradients(weight_grad=None)
+    g.reserved[0] = 1
+    assert lib.lda_norm_grad(r, g) == lda.LDA_ERR_ARG
+
+
+def test_struct_layouts():
+    assert C.sizeof(lda.lda_norm_rows) == 8 + 8 + 2 * 16 + 8 + 4 * 4 + 8 + 16
+    assert C.sizeof(lda.lda_norm_gradients) == 3 * 16 + 8 + 2 * 16 + 8 + 16 + 16
+
+
+def test_the_binding_refuses_host_tensors():
+    from paper_1412_1576_amd import operators
+    for call in (operators.rms_norm, operators.rms_norm_8bit):
+        with pytest.raises(ValueError, match="on the GPU"):
+            call(torch.zeros(2, 5))
+        with pytest.raises(ValueError, match="on the GPU"):
+            call(None)
