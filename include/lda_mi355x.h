@@ -470,6 +470,49 @@ int64_t lda_norm_grad_workspace(const lda_norm_rows* rows);
 /* Of the residual only that there is one is looked at. */
 int lda_norm_grad(const lda_norm_rows* rows, const lda_norm_gradients* gradients);
 
+/*
+ * Log probabilities of given tokens, entropy and top alternatives of rows of logits S [rows][classes], with T =
+ * temperature and the probabilities p = softmax(S / T), where p_v = 0 for S_v = -infinity:
+ *   log_prob = log p_t of the row's token t, 0 where t lies outside [0, classes);
+ *   entropy = - sum of p_v log p_v over the classes with p_v > 0;
+ *   ids, top: the `top` classes of the largest S_v > -infinity and their log p_v, the largest first, equal ones by class
+ *   (0 and -0 are equal); slots without a class have id -1 and -infinity;
+ *   gradient of sum of a log_prob + b entropy over the rows:
+ *   d / d S_v = (a ([v = t] - p_v) - b p_v (log p_v + entropy)) / T,  a taken as 0 where there is no token.
+ * With temperature 1, ids and top are a teacher for lda_distill_loss, with log_norm 0.
+ * A row without any S_v > -infinity has log_prob -infinity, entropy 0, empty slots and gradient 0.  One with a NaN or
+ * +infinity has NaN for log_prob (0 without a token), entropy, top and gradient, and ids -1.  A row with a = b = 0 has gradient
+ * 0 whatever S holds, and is not looked at.  Sums are 32-bit.
+ */
+typedef struct lda_log_prob_rows {
+    int64_t rows;            /* >= 0 */
+    int32_t classes;         /* >= 1 */
+    int32_t top;             /* 0 .. 256 (more: LDA_ERR_UNSUPPORTED) */
+    const void* logits;      /* [rows][classes], rows logits_stride apart */
+    int64_t logits_stride;
+    const void* tokens;      /* token of row i at tokens[i * tokens_stride] */
+    int64_t tokens_stride;
+    int32_t logits_type;     /* LDA_F32, LDA_F16, LDA_BF16 */
+    int32_t tokens_type;     /* LDA_I32, LDA_I64 */
+    float temperature;       /* 1/1024 .. 1024 */
+    int32_t reserved_word;   /* must be zero */
+    void* workspace;         /* at least lda_log_probs_workspace() bytes, aligned to 16 */
+    int64_t workspace_bytes;
+    void* hip_stream;
+    int32_t reserved[4];     /* must be zero */
+} lda_log_prob_rows;
+
+/* Bytes of workspace that lda_log_probs needs (may be 0), or a negative LDA_ERR_*. */
+int64_t lda_log_probs_workspace(const lda_log_prob_rows* rows);
+/* log_prob [rows]; entropy [rows] or NULL; ids and top [rows][top], not looked at with top = 0; stats, aligned to 16
+ * bytes: 4 floats a row for lda_log_probs_grad, or NULL. */
+int lda_log_probs(const lda_log_prob_rows* rows, float* log_prob, float* entropy, int32_t* ids, float* top, float* stats);
+/* a of row i at log_prob_grad[i * log_prob_grad_stride], NULL: 0; b alike.  grad [rows][classes] in the logits'
+ * type, rows grad_stride apart; what lies between rows is left as it was.  stats: of lda_log_probs on the same rows. */
+int lda_log_probs_grad(const lda_log_prob_rows* rows, const float* stats, const float* log_prob_grad,
+                       int64_t log_prob_grad_stride, const float* entropy_grad, int64_t entropy_grad_stride, void* grad,
+                       int64_t grad_stride);
+
 /* Wait for all work enqueued by this context. */
 int lda_sync(lda_ctx* ctx);
 /* Message of the last error of this context (ctx == NULL: of the last failed call on this thread,

@@ -10,7 +10,7 @@
 // Rows that fit a workgroup's registers are read from memory once, loss and gradient both
 // (distill_rows_kernel).  Longer rows, and long ones where there are too few to fill the GPU, are cut
 // into slices: distill_part_kernel, then distill_join_kernel, which reads them a second time for the gradient.
-#include "rows.hpp"
+#include "softmax_rows.hpp"
 
 namespace lda {
 
@@ -68,40 +68,6 @@ struct DistillArgs {
     int64_t grad_stride;
 };
 
-__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
-// exp((x - base) / T), exp2 in hardware.  The difference comes first: masks of the type's lowest value
-// times c would overflow, and a row of nothing else has to come out even.
-__device__ __forceinline__ float exp_above(float x, float base, float c)
-{
-    return __builtin_amdgcn_exp2f((x - base) * c);
-}
-
-__device__ __forceinline__ void join(float& m, float& s, float m2, float s2, float c)
-{
-    const float top = fmaxf(m, m2), base = base_of(top);
-    s = s * exp_above(m, base, c) + s2 * exp_above(m2, base, c);
-    m = top;
-}
-__device__ __forceinline__ void wave_join(float& m, float& s, float c)
-{
-    const float top = wave_max(m);
-    s = wave_sum(s * exp_above(m, base_of(top), c));
-    m = top;
-}
-template <int BLOCK>
-__device__ __forceinline__ void block_join(float& m, float& s, float c, float2* part)
-{
-    wave_join(m, s, c);
-    if (BLOCK == kWave) return;
-    __syncthreads();
-    if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = make_float2(m, s);
-    __syncthreads();
-    m = part[0].x;
-    s = part[0].y;
-#pragma unroll 1
-    for (int w = 1; w < BLOCK / kWave; ++w) join(m, s, part[w].x, part[w].y, c);
-}
-
 // What a sum of c (S - from) over n logits is with another base.  Sums of the logits themselves would lose
 // everything in a row of the type's lowest value, whose differences are 0.
 __device__ __forceinline__ double rebased(double scaled_sum, int32_t n, float from, float to, float c)
@@ -123,26 +89,6 @@ __device__ __forceinline__ bool get_any(const uint32_t* part)
 {
     return __ballot(part[threadIdx.x % (BLOCK / kWave)] != 0) != 0;
 }
-
-// A row as the whole 16-byte chunks of memory inside it, and the elements before and behind
-// those (fewer than two chunks), which a thread each takes.
-template <class T>
-struct SplitRow {
-    static constexpr int E = Row<T>::kChunk;
-    const T* p;
-    int32_t head, whole, extras;  // elements, chunks, elements
-
-    __device__ __forceinline__ SplitRow(const T* row, int32_t V) : p(row)
-    {
-        const int32_t lead = (int32_t)(((uintptr_t)row & 15u) / sizeof(T));
-        head = min((E - lead) % E, V);
-        whole = (V - head) / E;
-        extras = V - whole * E;
-    }
-    __device__ __forceinline__ int32_t chunk(int32_t i) const { return head + i * E; }
-    __device__ __forceinline__ int32_t extra(int32_t i) const { return i < head ? i : i + whole * E; }
-    __device__ __forceinline__ uint4 load(int32_t i) const { return *reinterpret_cast<const uint4*>(p + chunk(i)); }
-};
 
 // c (S - base) over classes without a slot whose logit lies above -infinity, and their number: what the floor's part
 // of the loss needs.  Every class is added while the row is read, and those that have a slot are taken out when
@@ -406,13 +352,6 @@ struct Gradient {
     __device__ __forceinline__ float dense(float x) const { return exp_above(x, base, c) * scale - low; }
     __device__ __forceinline__ float slot(float x, float p) const { return exp_above(x, base, c) * scale - p * wt; }
 };
-
-template <class T>
-__device__ __forceinline__ void store_chunk(T* g, const float (&x)[Row<T>::kChunk])
-{
-    const uint4 r = Row<T>::pack(x);
-    __builtin_memcpy(g, &r, 16);  // from any element on: the hardware takes unaligned addresses
-}
 
 // A thread's share of a row's loss: sum of p (log p - log q) over the slots; and where there is a floor, what
 // lies beside them

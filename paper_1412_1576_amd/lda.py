@@ -29,7 +29,8 @@ EXPORTS = [
     "lda_get_beta_table",
     "lda_distill_workspace", "lda_distill_loss", "lda_distill_grad", "lda_distill_step",
     "lda_verify_workspace", "lda_verify_drafts", "lda_topics_workspace", "lda_top_topics",
-    "lda_doc_topics", "lda_norm", "lda_norm_bytes", "lda_norm_grad_workspace", "lda_norm_grad", "lda_sync", "lda_last_error", "lda_destroy",
+    "lda_doc_topics", "lda_norm", "lda_norm_bytes", "lda_norm_grad_workspace", "lda_norm_grad",
+    "lda_log_probs_workspace", "lda_log_probs", "lda_log_probs_grad", "lda_sync", "lda_last_error", "lda_destroy",
 ]
 
 
@@ -118,6 +119,18 @@ class lda_norm_gradients(C.Structure):
     ]
 
 
+class lda_log_prob_rows(C.Structure):
+    _fields_ = [
+        ("rows", C.c_int64), ("classes", C.c_int32), ("top", C.c_int32),
+        ("logits", C.c_void_p), ("logits_stride", C.c_int64),
+        ("tokens", C.c_void_p), ("tokens_stride", C.c_int64),
+        ("logits_type", C.c_int32), ("tokens_type", C.c_int32),
+        ("temperature", C.c_float), ("reserved_word", C.c_int32),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64), ("hip_stream", C.c_void_p),
+        ("reserved", C.c_int32 * 4),
+    ]
+
+
 class LdaError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__("lda error %d: %s" % (code, msg))
@@ -183,6 +196,10 @@ def load_library():
         "lda_norm_bytes": (C.c_int, [C.POINTER(lda_norm_rows), C.c_int32, vp, C.c_int64, vp, vp, C.c_int64]),
         "lda_norm_grad_workspace": (C.c_int64, [C.POINTER(lda_norm_rows)]),
         "lda_norm_grad": (C.c_int, [C.POINTER(lda_norm_rows), C.POINTER(lda_norm_gradients)]),
+        "lda_log_probs_workspace": (C.c_int64, [C.POINTER(lda_log_prob_rows)]),
+        "lda_log_probs": (C.c_int, [C.POINTER(lda_log_prob_rows), vp, vp, vp, vp, vp]),
+        "lda_log_probs_grad": (C.c_int, [C.POINTER(lda_log_prob_rows), vp, vp, C.c_int64, vp, C.c_int64, vp,
+                                         C.c_int64]),
         "lda_sync": (C.c_int, [vp]),
         "lda_last_error": (C.c_char_p, [vp]),
         "lda_destroy": (None, [vp]),

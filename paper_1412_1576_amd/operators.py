@@ -6,6 +6,7 @@
   verify_drafts                drafted tokens accepted or redrawn from given random numbers
   rms_norm                     root-mean-square norm with the residual's addition, with autograd
   rms_norm_8bit                the same to 8 bits with a scale a row
+  token_log_probs              log probabilities of tokens, entropy, top alternatives, with autograd
 
 Work goes to torch's current stream of the tensors' device (inputs made on another stream have to
 be ready on it); outputs and workspaces come from torch's allocator; no call waits for the GPU, and
@@ -438,3 +439,86 @@ def rms_norm_8bit(x, weight=None, *, residual=None, eps=1e-6, dtype=torch.int8):
         _check(L.lda_norm_bytes(r, _LEVELS[dtype], q.data_ptr(), width, scale.data_ptr(),
                                 None if h is None else h.data_ptr(), width))
     return (q, scale) if h is None else (q, scale, h)
+
+
+def _log_prob_rows(logits, tokens, temperature, top):
+    # in the order of the struct's fields
+    rows, classes = logits.shape
+    return lda.lda_log_prob_rows(
+        rows, classes, top, logits.data_ptr(), logits.stride(0), tokens.data_ptr(), tokens.stride(0),
+        _FLOATS[logits.dtype], _INDEXES[tokens.dtype], temperature, 0, None, 0, _raw_stream(logits.get_device()))
+
+
+def _log_probs(logits, tokens, temperature, top, with_stats):
+    """(log_prob, entropy, ids, log probabilities, stats), the last three None where not wanted"""
+    L = lda.load_library()
+    device = logits.device
+    with _On(logits.get_device()):
+        r = _log_prob_rows(logits, tokens, temperature, top)
+        need = _check(L.lda_log_probs_workspace(r))
+        n = r.rows
+        log_prob = torch.empty(n, dtype=torch.float32, device=device)
+        entropy = torch.empty(n, dtype=torch.float32, device=device)
+        ids = values = stats = None
+        if top > 0:
+            ids = torch.empty((n, top), dtype=torch.int32, device=device)
+            values = torch.empty((n, top), dtype=torch.float32, device=device)
+        if with_stats:
+            stats = torch.empty((n, 4), dtype=torch.float32, device=device)
+        w = _workspace(r, need, device)
+        _check(L.lda_log_probs(r, log_prob.data_ptr(), entropy.data_ptr(), ids.data_ptr() if top > 0 else None,
+                               values.data_ptr() if top > 0 else None, stats.data_ptr() if with_stats else None))
+        del w
+    return log_prob, entropy, ids, values, stats
+
+
+class _LogProbs(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, tokens, temperature, top):
+        log_prob, entropy, ids, values, stats = _log_probs(logits, tokens, temperature, top, True)
+        ctx.save_for_backward(logits, tokens, stats)
+        ctx.temperature = temperature
+        ctx.set_materialize_grads(False)
+        if top <= 0:
+            return log_prob, entropy
+        ctx.mark_non_differentiable(ids, values)
+        return log_prob, entropy, ids, values
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, log_prob_grad, entropy_grad, *none):
+        if log_prob_grad is None and entropy_grad is None:
+            return None, None, None, None
+        logits, tokens, stats = ctx.saved_tensors
+        L = lda.load_library()
+        with _On(logits.get_device()):
+            grad = _gradient_like(logits)
+            r = _log_prob_rows(logits, tokens, ctx.temperature, 0)
+            a, b = (None if g is None else g.resolve_neg() for g in (log_prob_grad, entropy_grad))
+            _check(L.lda_log_probs_grad(
+                r, stats.data_ptr(), None if a is None else a.data_ptr(), 0 if a is None else a.stride(0),
+                None if b is None else b.data_ptr(), 0 if b is None else b.stride(0), grad.data_ptr(), grad.stride(0)))
+        return grad, None, None, None
+
+
+def token_log_probs(logits, tokens, *, temperature=1.0, top=0):
+    """(log_prob, entropy), float32 [rows]; with top also (ids int32, log probabilities float32), [rows, top].
+
+    logits [rows, classes] float32, float16 or bfloat16; tokens [rows] int32 or int64: log_prob is that of the row's token
+    under softmax(logits / temperature), 0 where the token is outside [0, classes) (padding).  top: so many of the
+    likeliest classes and their log probabilities, the likeliest first, equal ones by class; slots without a class of
+    probability have id -1 and -infinity.  At temperature 1 they are a teacher for distill_loss, with log_norm zeros.
+    Differentiable in logits through log_prob and entropy (not through the alternatives); rows whose gradients of both
+    are 0 are left out, whatever their logits hold.  A row without any logit above -infinity has log_prob -infinity, entropy 0 and
+    gradient 0.  Rows of a tensor may lie any distance apart; within a row elements are adjacent.  A
+    backward pass captured into a graph must find no eager graph of the same leaves alive.
+    """
+    _tensor(logits, "logits", 2, _FLOATS)
+    if logits.shape[1] < 1:
+        raise ValueError("logits: at least one class needed")
+    _tensor(tokens, "tokens", 1, _INDEXES, logits.get_device(), logits.shape[:1], spread=True)
+    temperature, top = float(temperature), _int32(top, "top")
+    if _wants_gradient(logits):
+        return _LogProbs.apply(logits, tokens, temperature, top)
+    out = _log_probs(logits, tokens, temperature, top, False)
+    return out[:4] if top > 0 else out[:2]

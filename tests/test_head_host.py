@@ -107,3 +107,59 @@ def test_the_binding_refuses_host_tensors():
             call(torch.zeros(2, 5))
         with pytest.raises(ValueError, match="on the GPU"):
             call(None)
+
+
+def log_probs(**kw):
+    r = lda.lda_log_prob_rows()
+    r.rows, r.classes, r.top, r.logits, r.logits_stride = 4, 1000, 8, 1 << 20, 1000
+    r.tokens, r.tokens_stride, r.temperature = 1 << 20, 1, 1.0
+    for k, v in kw.items():
+        setattr(r, k, v)
+    r.workspace, r.workspace_bytes = 1 << 20, 1 << 30
+    return r
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("rows", -1, lda.LDA_ERR_ARG), ("classes", 0, lda.LDA_ERR_ARG), ("top", -1, lda.LDA_ERR_ARG),
+    ("top", 257, lda.LDA_ERR_UNSUPPORTED), ("logits_type", 3, lda.LDA_ERR_ARG), ("tokens_type", 2, lda.LDA_ERR_ARG),
+    ("temperature", 0.0, lda.LDA_ERR_ARG), ("temperature", float("nan"), lda.LDA_ERR_ARG),
+    ("temperature", float("inf"), lda.LDA_ERR_ARG), ("temperature", 2.0 ** -11, lda.LDA_ERR_ARG),
+    ("logits", None, lda.LDA_ERR_ARG), ("tokens", None, lda.LDA_ERR_ARG), ("logits", (1 << 20) + 2, lda.LDA_ERR_ARG),
+    ("tokens", (1 << 20) + 2, lda.LDA_ERR_ARG), ("reserved_word", 1, lda.LDA_ERR_ARG)])
+def test_log_probs_refuse(lib, field, value, code):
+    r = log_probs(**{field: value})
+    for call, args in (("lda_log_probs_workspace", ()), ("lda_log_probs", (OUT, OUT, OUT, OUT, OUT)),
+                       ("lda_log_probs_grad", (OUT, OUT, 1, OUT, 1, OUT, 1000))):
+        assert getattr(lib, call)(r, *args) == code, call
+        assert call in message(lib)
+
+
+def test_log_probs_refuse_outputs_and_workspaces(lib):
+    r = log_probs()
+    for args in ((None, OUT, OUT, OUT, OUT), (OUT, OUT, None, OUT, OUT), (OUT, OUT, OUT, None, OUT),
+                 (OUT + 2, OUT, OUT, OUT, OUT), (OUT, OUT + 1, OUT, OUT, OUT), (OUT, OUT, OUT, OUT, OUT + 8)):
+        assert lib.lda_log_probs(r, *args) == lda.LDA_ERR_ARG, args
+    for args in ((None, OUT, 1, OUT, 1, OUT, 1000), (OUT, OUT, 1, OUT, 1, None, 1000), (OUT + 8, OUT, 1, OUT, 1, OUT, 1000),
+                 (OUT, OUT + 2, 1, OUT, 1, OUT, 1000), (OUT, OUT, 1, OUT + 2, 1, OUT, 1000), (OUT, OUT, 1, OUT, 1, OUT + 2, 1000),
+                 (OUT, OUT, 1, OUT, 1, OUT, 999)):
+        assert lib.lda_log_probs_grad(r, *args) == lda.LDA_ERR_ARG, args
+    big = log_probs(rows=1, classes=1_000_000, logits_stride=1_000_000)
+    need = lib.lda_log_probs_workspace(big)
+    assert need > 0
+    for pointer, nbytes in ((None, need), (1 << 21, need - 1), ((1 << 21) + 8, need)):
+        big.workspace, big.workspace_bytes = pointer, nbytes
+        assert lib.lda_log_probs(big, OUT, OUT, OUT, OUT, OUT) == lda.LDA_ERR_ARG and "workspace" in message(lib)
+    assert lib.lda_log_probs_workspace(None) == lda.LDA_ERR_ARG
+    r.reserved[1] = 1
+    assert lib.lda_log_probs(r, OUT, OUT, OUT, OUT, OUT) == lda.LDA_ERR_ARG
+    none = log_probs(rows=0, logits=None, tokens=None)
+    assert lib.lda_log_probs_workspace(none) == 0
+    assert lib.lda_log_probs(none, None, None, None, None, None) == lda.LDA_OK
+    assert lib.lda_log_probs_grad(none, None, None, 0, None, 0, None, 0) == lda.LDA_OK
+    assert C.sizeof(lda.lda_log_prob_rows) == 8 + 8 + 2 * 16 + 8 + 8 + 24 + 16
+
+
+def test_log_probs_binding_refuses_host_tensors():
+    from paper_1412_1576_amd import operators
+    with pytest.raises(ValueError, match="on the GPU"):
+        operators.token_log_probs(torch.zeros(2, 5), torch.zeros(2, dtype=torch.int64))
