@@ -471,6 +471,36 @@ int64_t lda_norm_grad_workspace(const lda_norm_rows* rows);
 int lda_norm_grad(const lda_norm_rows* rows, const lda_norm_gradients* gradients);
 
 /*
+ * Product of rows of 8-bit integers a [rows][width] with the classes' weights b [classes][width], a scale for each
+ * row of both:
+ *   out_ij = (float(sum over k of a_ik b_jk) a_scale_i) b_scale_j, rounded to out's type.
+ * The sum is exact.  Every integer may take all 256 values.
+ */
+typedef struct lda_product_rows {
+    int64_t rows;            /* 0 .. 2^31 */
+    int32_t classes;         /* >= 1 */
+    int32_t width;           /* 0 .. 131071: the sum has to fit 32 bits (more: LDA_ERR_UNSUPPORTED) */
+    const void* a;           /* [rows][width], rows a_stride apart */
+    int64_t a_stride;
+    const float* a_scale;    /* [rows] */
+    const void* b;           /* [classes][width], rows b_stride apart */
+    int64_t b_stride;
+    const float* b_scale;    /* [classes] */
+    int32_t out_type;        /* LDA_F32, LDA_F16, LDA_BF16 */
+    int32_t reserved_word;   /* must be zero */
+    void* workspace;         /* at least lda_product_workspace() bytes, aligned to 16 */
+    int64_t workspace_bytes;
+    void* hip_stream;
+    int32_t reserved[4];     /* must be zero */
+} lda_product_rows;
+
+/* Bytes of workspace that the call needs (may be 0), or a negative LDA_ERR_*. */
+int64_t lda_product_workspace(const lda_product_rows* rows);
+/* out [rows][classes], rows out_stride apart; what lies between rows is left as it was.  Rows of a and b whose
+ * pointers, strides and width are multiples of 16 are read faster. */
+int lda_product(const lda_product_rows* rows, void* out, int64_t out_stride);
+
+/*
  * Log probabilities of given tokens, entropy and top alternatives of rows of logits S [rows][classes], with T =
  * temperature and the probabilities p = softmax(S / T), where p_v = 0 for S_v = -infinity:
  *   log_prob = log p_t of the row's token t, 0 where t lies outside [0, classes);

@@ -30,7 +30,7 @@ EXPORTS = [
     "lda_distill_workspace", "lda_distill_loss", "lda_distill_grad", "lda_distill_step",
     "lda_verify_workspace", "lda_verify_drafts", "lda_topics_workspace", "lda_top_topics",
     "lda_doc_topics", "lda_norm", "lda_norm_bytes", "lda_norm_grad_workspace", "lda_norm_grad",
-    "lda_log_probs_workspace", "lda_log_probs", "lda_log_probs_grad", "lda_sync", "lda_last_error", "lda_destroy",
+    "lda_product_workspace", "lda_product", "lda_log_probs_workspace", "lda_log_probs", "lda_log_probs_grad", "lda_sync", "lda_last_error", "lda_destroy",
 ]
 
 
@@ -119,6 +119,17 @@ class lda_norm_gradients(C.Structure):
     ]
 
 
+class lda_product_rows(C.Structure):
+    _fields_ = [
+        ("rows", C.c_int64), ("classes", C.c_int32), ("width", C.c_int32),
+        ("a", C.c_void_p), ("a_stride", C.c_int64), ("a_scale", C.c_void_p),
+        ("b", C.c_void_p), ("b_stride", C.c_int64), ("b_scale", C.c_void_p),
+        ("out_type", C.c_int32), ("reserved_word", C.c_int32),
+        ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64), ("hip_stream", C.c_void_p),
+        ("reserved", C.c_int32 * 4),
+    ]
+
+
 class lda_log_prob_rows(C.Structure):
     _fields_ = [
         ("rows", C.c_int64), ("classes", C.c_int32), ("top", C.c_int32),
@@ -196,6 +207,8 @@ def load_library():
         "lda_norm_bytes": (C.c_int, [C.POINTER(lda_norm_rows), C.c_int32, vp, C.c_int64, vp, vp, C.c_int64]),
         "lda_norm_grad_workspace": (C.c_int64, [C.POINTER(lda_norm_rows)]),
         "lda_norm_grad": (C.c_int, [C.POINTER(lda_norm_rows), C.POINTER(lda_norm_gradients)]),
+        "lda_product_workspace": (C.c_int64, [C.POINTER(lda_product_rows)]),
+        "lda_product": (C.c_int, [C.POINTER(lda_product_rows), vp, C.c_int64]),
         "lda_log_probs_workspace": (C.c_int64, [C.POINTER(lda_log_prob_rows)]),
         "lda_log_probs": (C.c_int, [C.POINTER(lda_log_prob_rows), vp, vp, vp, vp, vp]),
         "lda_log_probs_grad": (C.c_int, [C.POINTER(lda_log_prob_rows), vp, vp, C.c_int64, vp, C.c_int64, vp,

@@ -6,6 +6,7 @@
   verify_drafts                drafted tokens accepted or redrawn from given random numbers
   rms_norm                     root-mean-square norm with the residual's addition, with autograd
   rms_norm_8bit                the same to 8 bits with a scale a row
+  int8_matmul                  rows times the classes' weights, 8-bit integers with a scale for each row of both
   token_log_probs              log probabilities of tokens, entropy, top alternatives, with autograd
 
 Work goes to torch's current stream of the tensors' device (inputs made on another stream have to
@@ -439,6 +440,44 @@ def rms_norm_8bit(x, weight=None, *, residual=None, eps=1e-6, dtype=torch.int8):
         _check(L.lda_norm_bytes(r, _LEVELS[dtype], q.data_ptr(), width, scale.data_ptr(),
                                 None if h is None else h.data_ptr(), width))
     return (q, scale) if h is None else (q, scale, h)
+
+
+def int8_matmul(a, a_scale, b, b_scale, *, dtype=torch.bfloat16):
+    """[rows, classes] of dtype (float32, float16 or bfloat16): (a @ b.T) * a_scale[:, None] * b_scale.
+
+    a [rows, width] and b [classes, width] int8, as rms_norm_8bit gives a and as weights are kept; a_scale float32
+    [rows], b_scale float32 [classes].  The sums are exact (width up to 131071), scaled in 32 bits and rounded once.
+    Rows of a and b may lie any distance apart (faster where width and distances are multiples of 16).  No
+    gradient: scales that require one are refused outside torch.no_grad().
+    """
+    if dtype not in _FLOATS:
+        raise ValueError("dtype must be one of %s, not %s" % (", ".join(map(str, _FLOATS)), dtype))
+    in_a = _tensor(a, "a", 2, (torch.int8,))
+    device = a.get_device()
+    in_b = _tensor(b, "b", 2, (torch.int8,), device)
+    rows, width = a.shape
+    classes = b.shape[0]
+    if b.shape[1] != width:
+        raise ValueError("b has %d numbers a row, a %d" % (b.shape[1], width))
+    if classes < 1:
+        raise ValueError("b: at least one class needed")
+    classes = _int32(classes, "classes")
+    _tensor(a_scale, "a_scale", 1, (torch.float32,), device, (rows,))
+    _tensor(b_scale, "b_scale", 1, (torch.float32,), device, (classes,))
+    if _wants_gradient(a_scale, b_scale):
+        raise ValueError("int8_matmul has no gradient (call .detach() on the scales)")
+    L = lda.load_library()
+    with _On(device):
+        # in the order of the struct's fields
+        r = lda.lda_product_rows(
+            rows, classes, width, a.data_ptr(), in_a[0], a_scale.data_ptr(), b.data_ptr(), in_b[0],
+            b_scale.data_ptr(), _FLOATS[dtype], 0, None, 0, _raw_stream(device))
+        need = _check(L.lda_product_workspace(r))
+        out = torch.empty((rows, classes), dtype=dtype, device=a.device)
+        w = _workspace(r, need, a.device)
+        _check(L.lda_product(r, out.data_ptr(), classes))
+        del w
+    return out
 
 
 def _log_prob_rows(logits, tokens, temperature, top):

@@ -163,3 +163,51 @@ def test_log_probs_binding_refuses_host_tensors():
     from paper_1412_1576_amd import operators
     with pytest.raises(ValueError, match="on the GPU"):
         operators.token_log_probs(torch.zeros(2, 5), torch.zeros(2, dtype=torch.int64))
+
+
+def product(**kw):
+    r = lda.lda_product_rows()
+    r.rows, r.classes, r.width, r.out_type = 4, 1000, 64, 2
+    r.a = r.b = r.a_scale = r.b_scale = 1 << 20
+    r.a_stride = r.b_stride = 64
+    for k, v in kw.items():
+        setattr(r, k, v)
+    return r
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("rows", -1, lda.LDA_ERR_ARG), ("classes", 0, lda.LDA_ERR_ARG), ("width", -1, lda.LDA_ERR_ARG),
+    ("width", 131_072, lda.LDA_ERR_UNSUPPORTED), ("rows", (1 << 31) + 1, lda.LDA_ERR_UNSUPPORTED),
+    ("out_type", 3, lda.LDA_ERR_ARG), ("a", None, lda.LDA_ERR_ARG), ("b", None, lda.LDA_ERR_ARG),
+    ("a_scale", None, lda.LDA_ERR_ARG), ("b_scale", None, lda.LDA_ERR_ARG), ("a_scale", (1 << 20) + 2, lda.LDA_ERR_ARG),
+    ("b_scale", (1 << 20) + 1, lda.LDA_ERR_ARG), ("reserved_word", 1, lda.LDA_ERR_ARG)])
+def test_product_refuses(lib, field, value, code):
+    r = product(**{field: value})
+    assert lib.lda_product_workspace(r) == code and "lda_product_workspace" in message(lib)
+    assert lib.lda_product(r, OUT, 1000) == code and "lda_product:" in message(lib)
+
+
+def test_product_refuses_outputs_and_workspaces(lib):
+    for args in ((None, 1000), (OUT + 1, 1000), (OUT, 999)):
+        assert lib.lda_product(product(), *args) == lda.LDA_ERR_ARG
+    assert lib.lda_product(None, OUT, 1000) == lda.LDA_ERR_ARG
+    assert lib.lda_product_workspace(None) == lda.LDA_ERR_ARG
+    r = product()
+    r.reserved[0] = 1
+    assert lib.lda_product(r, OUT, 1000) == lda.LDA_ERR_ARG
+    r = product(rows=100, classes=100, width=16_384)
+    need = lib.lda_product_workspace(r)
+    assert need > 0
+    for pointer, nbytes in ((None, need), (1 << 21, need - 1), ((1 << 21) + 8, need)):
+        r.workspace, r.workspace_bytes = pointer, nbytes
+        assert lib.lda_product(r, OUT, 1000) == lda.LDA_ERR_ARG and "workspace" in message(lib)
+    none = product(rows=0, a=None, b=None, a_scale=None)
+    assert lib.lda_product_workspace(none) == 0 and lib.lda_product(none, None, 0) == lda.LDA_OK
+    assert C.sizeof(lda.lda_product_rows) == 8 + 8 + 16 + 8 + 16 + 8 + 8 + 24 + 16
+
+
+def test_product_binding_refuses_host_tensors():
+    from paper_1412_1576_amd import operators
+    x = torch.zeros(2, 8, dtype=torch.int8)
+    with pytest.raises(ValueError, match="on the GPU"):
+        operators.int8_matmul(x, torch.ones(2), x, torch.ones(2))
