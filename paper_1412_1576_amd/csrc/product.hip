@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "rows.hpp"
+#include "xcd.hpp"
 
 namespace lda {
 
@@ -18,6 +19,8 @@ typedef int32_t i32x16 __attribute__((ext_vector_type(16)));
 constexpr int32_t kMostWidth = 131071;  // times 128^2 below 2^31
 constexpr int kStep = 64;               // bytes of a row that a step of the few-rows kernel takes
 constexpr int kTileK = 128;             // bytes of a row in a tile
+constexpr int kCus = 256, kLdsOfCu = 160 * 1024;
+constexpr int kRawBuffer = 0x00020000;  // a buffer resource's last word: no swizzle, 32-bit data
 
 struct ProductArgs {
     int64_t M;
@@ -35,14 +38,11 @@ struct ProductArgs {
     int32_t tiles_m, tiles_n;
 };
 
-// 16 bytes of a row from k on, 0 behind `end`
-template <bool ALIGNED>
+// 16 bytes of a row from k on, 0 behind `end`, from any address
 __device__ __forceinline__ i32x4 load16(const int8_t* row, int32_t k, int32_t end)
 {
     i32x4 v = {0, 0, 0, 0};
-    if (ALIGNED) {
-        if (k < end) v = *reinterpret_cast<const i32x4*>(row + k);  // end is a multiple of 16
-    } else if (k + 16 <= end) {
+    if (k + 16 <= end) {
         __builtin_memcpy(&v, row + k, 16);
     } else if (k < end) {
         const int32_t n = end - k;
@@ -53,23 +53,13 @@ __device__ __forceinline__ i32x4 load16(const int8_t* row, int32_t k, int32_t en
     return v;
 }
 
-__device__ __forceinline__ float scaled(int32_t sum, float sa, float sb)
+__device__ __forceinline__ float scaled(float v, float scale)
 {
-    float v = ((float)sum * sa) * sb;
-    asm("" : "+v"(v));  // else the last product and a rounding to fp16 become one instruction, with one rounding less
+    v *= scale;
+    asm("" : "+v"(v));  // else this and a rounding to fp16 become one instruction, with one rounding less
     return v;
 }
-
-template <class T>
-__device__ __forceinline__ void store_few(T* p, const float (&v)[4])  // 4 adjacent elements, aligned to one
-{
-    if constexpr (std::is_same<T, float>::value) {
-        __builtin_memcpy(p, v, 16);
-    } else {
-        const uint2 w = make_uint2(Row<T>::two(v[0], v[1]), Row<T>::two(v[2], v[3]));
-        __builtin_memcpy(p, &w, 8);
-    }
-}
+__device__ __forceinline__ float scaled(int32_t sum, float sa, float sb) { return scaled((float)sum * sa, sb); }
 
 // Up to 16 MT rows times 16 CT classes a workgroup; its waves take the row's steps in turn and join in LDS.
 template <class T, int MT, int CT, bool ALIGNED>
@@ -92,24 +82,31 @@ __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs p)
 #pragma unroll
         for (int m = 0; m < MT; ++m) sum[c][m] = i32x4{0, 0, 0, 0};
     constexpr int kUnroll = MT * CT >= 8 ? 2 : 4;
-    for (int32_t k = from + wave * kStep + g; k - g < end; k += kUnroll * kWaves * kStep) {
-        i32x4 x[kUnroll][MT], w[kUnroll][CT];
+    const auto take = [&](auto steps, auto whole, int32_t k) {
+        i32x4 x[steps()][MT], w[steps()][CT];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
+        for (int u = 0; u < steps(); ++u) {
             const int32_t at = k + u * kWaves * kStep;
 #pragma unroll
-            for (int c = 0; c < CT; ++c) w[u][c] = load16<ALIGNED>(b[c], at, end);
+            for (int c = 0; c < CT; ++c)
+                w[u][c] = whole() ? *reinterpret_cast<const i32x4*>(b[c] + at) : load16(b[c], at, end);
 #pragma unroll
-            for (int m = 0; m < MT; ++m) x[u][m] = load16<ALIGNED>(a[m], at, end);
+            for (int m = 0; m < MT; ++m)
+                x[u][m] = whole() ? *reinterpret_cast<const i32x4*>(a[m] + at) : load16(a[m], at, end);
         }
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
+        for (int u = 0; u < steps(); ++u)
 #pragma unroll
             for (int c = 0; c < CT; ++c)
 #pragma unroll
                 for (int m = 0; m < MT; ++m)
                     sum[c][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][c], x[u][m], sum[c][m], 0, 0, 0);
-    }
+    };
+    int32_t k = from + wave * kStep + g;
+    if (ALIGNED)
+        for (; k - g + (kUnroll - 1) * kWaves * kStep + kStep <= end; k += kUnroll * kWaves * kStep)
+            take(std::integral_constant<int, kUnroll>{}, std::true_type{}, k);
+    for (; k - g < end; k += kWaves * kStep) take(std::integral_constant<int, 1>{}, std::false_type{}, k);
     // lane: 4 adjacent classes of a row
 #pragma unroll
     for (int c = 0; c < CT; ++c)
@@ -127,119 +124,270 @@ __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs p)
     }
 }
 
-// A tile of TM rows times TN classes a workgroup of WM x WN waves.  LDS has rows of kTileK bytes, their 16-byte pieces
-// in an order that changes from row to row, so that reads down a column of pieces meet all banks.
+// The order of a step of product_tile_kernel: reads from LDS behind the first products, then writes and loads, a pair
+// behind each product.  Left alone the compiler puts reads where they are used, and waits.
+template <int PRODUCTS, int READS, int PAIRS>
+__device__ __forceinline__ void interleave(bool pairs)
+{
+    constexpr int kReadsEach = READS * 2 > PRODUCTS ? 2 : 1, kFirst = (READS + kReadsEach - 1) / kReadsEach;
+    constexpr int kPairsEach = (PAIRS + PRODUCTS - kFirst - 1) / (PRODUCTS - kFirst);
+#pragma unroll
+    for (int i = 0; i < PRODUCTS; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix
+        if (i < kFirst) {
+            __builtin_amdgcn_sched_group_barrier(0x100, kReadsEach, 0);  // LDS read
+        } else if (pairs) {
+            __builtin_amdgcn_sched_group_barrier(0x200, kPairsEach, 0);  // LDS write
+            __builtin_amdgcn_sched_group_barrier(0x020, kPairsEach, 0);  // memory read
+        }
+    }
+}
+
+// A tile of the result and of the long axis: where both sides' rows begin and how many there are
+struct ProductTile {
+    int64_t m0;
+    int32_t n0, split, rows_a, rows_b, from, end;
+    const int8_t *a, *b;
+};
+// Workgroups go to the 8 XCDs in turn: each XCD has a stretch of the tiles, in groups of kTileGroup rows of tiles, so that
+// those under way on it at once share what its L2 holds of both sides.  Number `turn` of workgroup `block`; false
+// where it has no more.
+constexpr int32_t kTileGroup = 8;
+template <int TM, int TN>
+__device__ __forceinline__ bool find_tile(const ProductArgs& p, int32_t block, int32_t turn, ProductTile& t)
+{
+    const int32_t tiles = p.tiles_m * p.tiles_n * p.splits;
+    const int32_t xcd = block % kXcds, each = tiles / kXcds, more = tiles % kXcds;
+    const int32_t at = block / kXcds + turn * ((int32_t)gridDim.x / kXcds);
+    if (at >= each + (xcd < more)) return false;
+    int32_t tile = xcd * each + min(xcd, more) + at;
+    t.split = tile / (p.tiles_m * p.tiles_n);
+    tile %= p.tiles_m * p.tiles_n;
+    const int32_t group = tile / (kTileGroup * p.tiles_n), rest = tile % (kTileGroup * p.tiles_n);
+    const int32_t high = min(kTileGroup, p.tiles_m - group * kTileGroup);
+    t.m0 = (int64_t)(group * kTileGroup + rest % high) * TM;
+    t.n0 = rest / high * TN;
+    t.rows_a = (int32_t)min((int64_t)TM, p.M - t.m0);
+    t.rows_b = min(TN, p.N - t.n0);
+    t.from = t.split * p.split_k;
+    t.end = min(p.K, t.from + p.split_k);
+    t.a = p.a + t.m0 * p.a_stride;
+    t.b = p.b + (int64_t)t.n0 * p.b_stride;
+    return true;
+}
+
+// Tiles of TM rows times TN classes, one after the other, by a workgroup of WM x WN waves.  The pieces of both sides
+// are one stream over all of a workgroup's tiles: two pieces of the long axis are under way while one is multiplied, also
+// from one tile to the next, so that a tile's beginning waits for nothing and its stores drain behind the next one's
+// products.  LDS has rows of kTileK bytes, their 16-byte pieces in an order that changes every two rows, so that 16 rows'
+// reads of a column of pieces meet all banks (with an order that changed every row a third of LDS's cycles were
+// conflicts).
 template <class T, int TM, int TN, int WM, int WN, bool ALIGNED>
 __global__ __launch_bounds__(WM * WN * 64, 1) void product_tile_kernel(ProductArgs p)
 {
     constexpr int kThreads = WM * WN * 64, kMi = TM / WM / 32, kNi = TN / WN / 32, kSteps = kTileK / 32;
-    constexpr int kRowsAtOnce = kThreads / 8, kLoadsA = TM / kRowsAtOnce, kLoadsB = TN / kRowsAtOnce;
-    extern __shared__ __align__(16) int8_t lds[];  // [2][TM + TN][kTileK]
+    constexpr int kRowsAtOnce = kThreads / 8, kLoadsA = TM / kRowsAtOnce, kLoadsB = TN / kRowsAtOnce, kLoads = kLoadsA + kLoadsB;
+    static_assert(kRowsAtOnce % 16 == 0 && TM % kRowsAtOnce == 0 && TN % kRowsAtOnce == 0 && TM <= kThreads && TN <= kThreads, "shape");
+    extern __shared__ __align__(16) int8_t lds[];  // [2][TM + TN][kTileK], [TM + TN] scales
     constexpr int kBuffer = (TM + TN) * kTileK;
+    float* const scale_a = reinterpret_cast<float*>(lds + 2 * kBuffer);
+    float* const scale_b = scale_a + TM;
     const int32_t tid = (int32_t)threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    const int32_t tile = (int32_t)blockIdx.x;
-    const int32_t tm = tile % p.tiles_m, tn = tile / p.tiles_m % p.tiles_n, split = tile / p.tiles_m / p.tiles_n;
-    const int64_t m0 = (int64_t)tm * TM;
-    const int32_t n0 = tn * TN;
-    const int32_t from = split * p.split_k, end = min(p.K, from + p.split_k);
-    // what a thread loads: piece tid % 8 of rows tid / 8, + kRowsAtOnce, ...
+    // What a thread loads: 16 bytes at `piece` of rows tid / 8, + kRowsAtOnce, ...
     const int32_t piece = tid % 8 * 16, row0 = tid / 8;
-    const int8_t *a[kLoadsA], *b[kLoadsB];
-#pragma unroll
-    for (int i = 0; i < kLoadsA; ++i) a[i] = p.a + min(m0 + row0 + i * kRowsAtOnce, p.M - 1) * p.a_stride;
-#pragma unroll
-    for (int i = 0; i < kLoadsB; ++i) b[i] = p.b + (int64_t)min(n0 + row0 + i * kRowsAtOnce, p.N - 1) * p.b_stride;
-    i32x4 held[kLoadsA + kLoadsB];
-    const auto load = [&](int32_t k) {
-#pragma unroll
-        for (int i = 0; i < kLoadsA; ++i) held[i] = load16<ALIGNED>(a[i], k + piece, end);
-#pragma unroll
-        for (int i = 0; i < kLoadsB; ++i) held[kLoadsA + i] = load16<ALIGNED>(b[i], k + piece, end);
+    const uint32_t at_a = (uint32_t)row0 * (uint32_t)p.a_stride + (uint32_t)piece, step_a = kRowsAtOnce * (uint32_t)p.a_stride;
+    const uint32_t at_b = (uint32_t)row0 * (uint32_t)p.b_stride + (uint32_t)piece, step_b = kRowsAtOnce * (uint32_t)p.b_stride;
+    // The stream.  ALIGNED: through buffers that end where a tile's last row ends; what lies beyond reads as 0.
+    ProductTile next{};
+    int32_t turn = 0, k_next = 0;
+    __amdgpu_buffer_rsrc_t buffer_a, buffer_b;
+    const auto open = [&]() {
+        const bool some = find_tile<TM, TN>(p, (int32_t)blockIdx.x, turn, next);
+        k_next = next.from;
+        if (!some) {  // nothing is read any more
+            next.rows_a = next.rows_b = 0;
+            next.end = 1 << 30;
+            k_next = 0;
+        }
+        ++turn;
+        if (ALIGNED) {
+            buffer_a = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(next.a), 0, some ? (next.rows_a - 1) * (int32_t)p.a_stride + p.K : 0, kRawBuffer);
+            buffer_b = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(next.b), 0, some ? (next.rows_b - 1) * (int32_t)p.b_stride + p.K : 0, kRawBuffer);
+        }
+        return some;
     };
-    const int32_t put_at = row0 * kTileK + (piece ^ (row0 % 8 * 16));  // kRowsAtOnce is a multiple of 8
-    const auto put = [&](int buffer) {
-        int8_t* const to = lds + buffer * kBuffer + put_at;
-#pragma unroll
-        for (int i = 0; i < kLoadsA + kLoadsB; ++i) *reinterpret_cast<i32x4*>(to + i * kRowsAtOnce * kTileK) = held[i];
+    const auto advance = [&]() {
+        k_next += kTileK;
+        if (k_next >= next.end) open();
+    };
+    i32x4 held[kLoads];
+    const auto load = [&](int i) {  // those of a first
+        const bool of_a = i < kLoadsA;
+        const int j = of_a ? i : i - kLoadsA;
+        if (ALIGNED) {
+            // behind the row's end: a place beyond the buffer, for one side
+            const uint32_t beyond = k_next + piece < next.end ? 0u : 1u << 31;
+            held[i] = __builtin_bit_cast(i32x4, of_a ? __builtin_amdgcn_raw_buffer_load_b128(buffer_a, (at_a + ((uint32_t)k_next + j * step_a)) | beyond, 0, 0)
+                                                     : __builtin_amdgcn_raw_buffer_load_b128(buffer_b, at_b + ((uint32_t)k_next + j * step_b), 0, 0));
+        } else {
+            held[i] = i32x4{0, 0, 0, 0};
+            if (next.rows_a > 0)
+                held[i] = of_a ? load16(next.a + min(row0 + j * kRowsAtOnce, next.rows_a - 1) * p.a_stride, k_next + piece, next.end)
+                               : load16(next.b + min(row0 + j * kRowsAtOnce, next.rows_b - 1) * p.b_stride, k_next + piece, next.end);
+        }
+    };
+    const int32_t put_at = row0 * kTileK + (piece ^ (row0 / 2 % 8 * 16));
+    const auto put = [&](int i, int buffer) {
+        *reinterpret_cast<i32x4*>(lds + buffer * kBuffer + put_at + i * kRowsAtOnce * kTileK) = held[i];
     };
     const int32_t wm = wave % WM * (TM / WM), wn = wave / WM * (TN / WN);
-    const int32_t r = lane % 32, half = lane / 32 * 16, turn = r % 8 * 16;
+    const int32_t r = lane % 32, half = lane / 32 * 16, order = r / 2 % 8 * 16;
     const int8_t* const read_a = lds + (wm + r) * kTileK;
     const int8_t* const read_b = lds + (TM + wn + r) * kTileK;
     i32x4 fa[2][kMi], fb[2][kNi];
     const auto read = [&](int buffer, int step, int set) {
-        const int32_t at = buffer * kBuffer + ((step * 32 + half) ^ turn);
+        const int32_t at = buffer * kBuffer + ((step * 32 + half) ^ order);
 #pragma unroll
         for (int i = 0; i < kNi; ++i) fb[set][i] = *reinterpret_cast<const i32x4*>(read_b + at + i * 32 * kTileK);
 #pragma unroll
         for (int i = 0; i < kMi; ++i) fa[set][i] = *reinterpret_cast<const i32x4*>(read_a + at + i * 32 * kTileK);
     };
-    i32x16 sum[kNi][kMi];
+    if (!open()) return;
+    ProductTile tile = next;
 #pragma unroll
-    for (int n = 0; n < kNi; ++n)
+    for (int i = 0; i < kLoads; ++i) load(i);
+    advance();
 #pragma unroll
-        for (int m = 0; m < kMi; ++m)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sum[n][m][i] = 0;
-    load(from);
-    put(0);
-    load(from + kTileK);
+    for (int i = 0; i < kLoads; ++i) {
+        put(i, 0);
+        load(i);
+    }
+    // (where a tile is one piece long the stream is a tile ahead already)
     __syncthreads();
     read(0, 0, 0);
     int buffer = 0;
-    for (int32_t k = from; k < end; k += kTileK) {
+    for (int32_t mine = 1;; ++mine) {
+        // held until they are wanted, behind the products
+        const float own_a = tid < tile.rows_a ? p.a_scale[tile.m0 + tid] : 0.0f;
+        const float own_b = tid < tile.rows_b ? p.b_scale[tile.n0 + tid] : 0.0f;
+        i32x16 sum[kNi][kMi];
 #pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-            if (s < kSteps - 1) {
-                read(buffer, s + 1, (s + 1) % 2);
-            } else {
-                __syncthreads();  // the next tile is there, and nobody reads this one any more
-                read(buffer ^ 1, 0, 0);
-            }
+        for (int n = 0; n < kNi; ++n)
 #pragma unroll
-            for (int n = 0; n < kNi; ++n)
+            for (int m = 0; m < kMi; ++m)
 #pragma unroll
-                for (int m = 0; m < kMi; ++m)
-                    sum[n][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[s % 2][n], fa[s % 2][m], sum[n][m], 0, 0, 0);
-            if (s == 1) {
-                put(buffer ^ 1);
-                load(k + 2 * kTileK);
-            }
-        }
-        buffer ^= 1;
-    }
-    // lane: a row, 4 adjacent classes at a time
-    T* const out = static_cast<T*>(p.out);
+                for (int i = 0; i < 16; ++i) sum[n][m][i] = 0;
+        int32_t k = tile.from;
+        do {
+            advance();
 #pragma unroll
-    for (int m = 0; m < kMi; ++m) {
-        const int64_t row = m0 + wm + 32 * m + lane % 32;
-        if (row >= p.M) continue;
-        const float sa = p.a_scale[row];
+            for (int s = 0; s < kSteps; ++s) {
+                if (s == kSteps - 1) __syncthreads();  // the next piece is there, and nobody reads this one any more
+                if (s < kSteps - 1) read(buffer, s + 1, (s + 1) % 2);
+                else read(buffer ^ 1, 0, 0);
+                // the next piece into LDS, half of it at a time, and the one after it into the registers that this frees
+                if (s == 1 || s == 2) {
 #pragma unroll
-        for (int n = 0; n < kNi; ++n) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int32_t c = n0 + wn + 32 * n + 8 * q + lane / 32 * 4;
-                if (p.splits > 1) {
-                    int32_t* const to = p.partial + ((int64_t)split * p.M + row) * p.N;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (c + i < p.N) to[c + i] = sum[n][m][4 * q + i];
-                    continue;
+                    for (int i = (s - 1) * kLoads / 2; i < s * kLoads / 2; ++i) {
+                        put(i, buffer ^ 1);
+                        load(i);
+                    }
                 }
-                T* const to = out + row * p.out_stride;
-                float v[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = c + i < p.N ? scaled(sum[n][m][4 * q + i], sa, p.b_scale[c + i]) : 0.0f;
-                if (c + 4 <= p.N) {
-                    store_few(to + c, v);
-                } else {
+                for (int n = 0; n < kNi; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (c + i < p.N) to[c + i] = Row<T>::from(v[i]);
+                    for (int m = 0; m < kMi; ++m)
+                        sum[n][m] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fb[s % 2][n], fa[s % 2][m], sum[n][m], 0, 0, 0);
+                interleave<kMi * kNi, kMi + kNi, (kLoads + 1) / 2>(s == 1 || s == 2);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            buffer ^= 1;
+            k += kTileK;
+        } while (k < tile.end);
+        // (the sums stay in their registers until they are written: the compiler fetched them in every turn of the loop, or all at
+        // once behind it, and put others into memory)
+#pragma unroll
+        for (int n = 0; n < kNi; ++n)
+#pragma unroll
+            for (int m = 0; m < kMi; ++m) asm volatile("" : "+a"(sum[n][m]));
+        // A lane has 4 adjacent classes of a row at a time.  A wave's 32 rows pass through LDS, by the piece that nobody reads
+        // any more, as 32-bit words, so that what goes to memory are rows' 16-byte pieces side by side and a lane needs
+        // the same classes' scales all along: stores straight from the registers took longer than the products of 4096
+        // numbers, scales fetched beside each 4 sums a third of that.
+        if (tid < TM) scale_a[tid] = own_a;
+        if (tid < TN) scale_b[tid] = own_b;
+        __syncthreads();
+        const auto write = [&](auto* out, int64_t stride, auto before, auto behind) {
+            using O = std::remove_pointer_t<decltype(out)>;
+            constexpr int kEach = 16 / (int)sizeof(O), kBlocks = kNi % 2 == 0 && WM * WN * 32 * 68 * 4 <= kBuffer ? 2 : 1;  // of 32 classes
+            constexpr int kWidth = kBlocks * 32, kRow = kWidth + 4, kPieces = kWidth / kEach, kRowsEach = kWave / kPieces;
+            static_assert(WM * WN * 32 * kRow * 4 <= kBuffer, "fits");
+            uint32_t* const stage = reinterpret_cast<uint32_t*>(lds + (buffer ^ 1) * kBuffer) + wave * 32 * kRow;
+            const int32_t c = lane % kPieces * kEach, row1 = lane / kPieces;
+            float sa[kMi];
+#pragma unroll
+            for (int m = 0; m < kMi; ++m) sa[m] = scale_a[wm + 32 * m + r];
+#pragma unroll
+            for (int n0 = 0; n0 < kNi; n0 += kBlocks) {
+                float sb[kEach];
+#pragma unroll
+                for (int i = 0; i < kEach; ++i) sb[i] = scale_b[wn + 32 * n0 + c + i];
+                const int32_t left = tile.rows_b - wn - 32 * n0 - c;
+#pragma unroll
+                for (int m = 0; m < kMi; ++m) {
+#pragma unroll
+                    for (int n = 0; n < kBlocks; ++n) {
+                        i32x16 block = sum[n0 + n][m];
+                        asm volatile("" : "+a"(block));
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            uint4 w;
+                            w.x = before(block[4 * q], sa[m]);
+                            w.y = before(block[4 * q + 1], sa[m]);
+                            w.z = before(block[4 * q + 2], sa[m]);
+                            w.w = before(block[4 * q + 3], sa[m]);
+                            *reinterpret_cast<uint4*>(stage + r * kRow + 32 * n + 8 * q + lane / 32 * 4) = w;
+                        }
+                    }
+                    wave_lds_order();
+                    O* to = out + (tile.m0 + wm + 32 * m + row1) * stride + tile.n0 + wn + 32 * n0 + c;
+#pragma unroll
+                    for (int j = 0; j < 32 / kRowsEach; ++j, to += kRowsEach * stride) {
+                        const int32_t row = row1 + j * kRowsEach;
+                        uint32_t w[kEach];
+#pragma unroll
+                        for (int i = 0; i < kEach; i += 4)
+                            *reinterpret_cast<uint4*>(w + i) = *reinterpret_cast<const uint4*>(stage + row * kRow + c + i);
+                        const uint4 v = behind(w, sb);
+                        if (wm + 32 * m + row >= tile.rows_a || left <= 0) continue;
+                        if (left >= kEach) {
+                            __builtin_memcpy(to, &v, 16);  // the hardware takes unaligned addresses
+                        } else {
+                            O each[kEach];
+                            __builtin_memcpy(each, &v, 16);
+#pragma unroll
+                            for (int i = 0; i < kEach; ++i)
+                                if (i < left) to[i] = each[i];
+                        }
+                    }
+                    wave_lds_order();
                 }
             }
+        };
+        if (p.splits > 1) {
+            write(p.partial + (int64_t)tile.split * p.M * p.N, (int64_t)p.N, [](int32_t s, float) { return (uint32_t)s; },
+                  [](const uint32_t (&w)[4], const float (&)[4]) { return make_uint4(w[0], w[1], w[2], w[3]); });
+        } else {
+            write(static_cast<T*>(p.out), p.out_stride, [](int32_t s, float sa) { return __float_as_uint((float)s * sa); },
+                  [](const uint32_t (&w)[Row<T>::kChunk], const float (&sb)[Row<T>::kChunk]) {
+                      float v[Row<T>::kChunk];
+#pragma unroll
+                      for (int i = 0; i < Row<T>::kChunk; ++i) v[i] = scaled(__uint_as_float(w[i]), sb[i]);
+                      return Row<T>::pack(v);
+                  });
         }
+        if (!find_tile<TM, TN>(p, (int32_t)blockIdx.x, mine, tile)) return;
+        __syncthreads();  // the stream goes on into what this has passed through
     }
 }
 
@@ -335,13 +483,15 @@ static hipError_t launch_product(ProductArgs a, const ProductPlan& plan, hipStre
     const auto tile = [&](auto tm, auto tn, auto wm, auto wn) {
         a.tiles_m = (int32_t)((a.M + tm() - 1) / tm());
         a.tiles_n = (a.N + tn() - 1) / tn();
-        constexpr size_t lds = 2 * (tm() + tn()) * kTileK;
+        constexpr size_t lds = (tm() + tn()) * (2 * kTileK + sizeof(float));
         const auto kernel = product_tile_kernel<T, tm(), tn(), wm(), wn(), ALIGNED>;
         if (lds > 65536) {
             const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
             if (e != hipSuccess) return e;
         }
-        const unsigned n = (unsigned)((int64_t)a.tiles_m * a.tiles_n * a.splits);
+        // as many workgroups as there is room for at once, a multiple of the XCDs
+        const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n * a.splits, room = kCus * (int64_t)(kLdsOfCu / lds);
+        const unsigned n = (unsigned)(((tiles < room ? tiles : room) + kXcds - 1) / kXcds * kXcds);
         kernel<<<n, wm() * wn() * 64, lds, stream>>>(a);
         return hipSuccess;
     };
@@ -415,7 +565,9 @@ try {
     a.out_stride = out_stride;
     a.partial = static_cast<int32_t*>(d->workspace);
     const hipStream_t stream = static_cast<hipStream_t>(d->hip_stream);
-    const bool aligned = a.K % 16 == 0 && aligned_to(a.a, 16) && aligned_to(a.b, 16) && a.a_stride % 16 == 0 && a.b_stride % 16 == 0;
+    // (places inside a tile are 32-bit)
+    const bool aligned = a.K % 16 == 0 && aligned_to(a.a, 16) && aligned_to(a.b, 16) && a.a_stride % 16 == 0 &&
+                         a.b_stride % 16 == 0 && a.a_stride >= 0 && a.b_stride >= 0 && a.a_stride < 1 << 22 && a.b_stride < 1 << 22;
     const auto typed = [&](auto t) -> hipError_t {
         using T = decltype(t);
         if (a.K == 0) {
