@@ -140,23 +140,64 @@ __device__ __forceinline__ float logit_of(u64 place)
 struct ListLds {
     int32_t histogram[256];
     int32_t count, chosen;
+    uint32_t high[16], low[16];
+    int32_t number[16];
     u64 best[kMostTop];
 };
 
+__device__ __forceinline__ uint32_t wave_most(uint32_t v)
+{
+    return (uint32_t)lane_value((int32_t)wave_scan(v, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; }), kWave - 1);
+}
+
 // The k-th largest of the workgroup's numbers, which each(f) gives to f; 1 where there are at most k.  By 8 bits
-// at a time from the top on, until those with the same upper bits are all wanted: exactly k numbers are at least what it
-// returns, which need not be one of them.
+// at a time from the first on that is not the same in all, until those with the same upper bits are all wanted: exactly k
+// numbers are at least what it returns, which need not be one of them.  (Bits that are the same in all would put every number
+// into one bin, one after the other.)
 template <int BLOCK, class Each>
 __device__ __forceinline__ u64 kth_largest(Each each, int32_t k, ListLds& l)
 {
+    constexpr int kWaves = BLOCK / kWave;
     const int32_t tid = (int32_t)threadIdx.x, lane = tid % kWave;
-    u64 prefix = 0;
-    for (int32_t shift = 56; shift >= 0; shift -= 8) {
-        for (int32_t i = tid; i < 256; i += BLOCK) l.histogram[i] = 0;
+    uint32_t high = 0, low = 0;  // of the upper halves; the least as its complement
+    int32_t number = 0;
+    each([&](u64 key) {
+        if (key == 0) return;
+        high = max(high, (uint32_t)(key >> 32));
+        low = max(low, ~(uint32_t)(key >> 32));
+        ++number;
+    });
+    high = wave_most(high);
+    low = wave_most(low);
+    number = wave_sum(number);
+    if (lane == 0) {
+        l.high[tid / kWave] = high;
+        l.low[tid / kWave] = low;
+        l.number[tid / kWave] = number;
+    }
+    for (int32_t i = tid; i < 256; i += BLOCK) l.histogram[i] = 0;
+    __syncthreads();
+    high = l.high[0];
+    low = l.low[0];
+    number = l.number[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) {
+        high = max(high, l.high[w]);
+        low = max(low, l.low[w]);
+        number += l.number[w];
+    }
+    if (number <= k) {
         __syncthreads();
+        return 1;
+    }
+    const uint32_t differ = high ^ ~low;
+    int32_t bits = differ == 0 ? 32 : 64 - __builtin_clz(differ);  // the lowest ones, that differ
+    u64 prefix = bits == 64 ? 0 : ((u64)high << 32) >> bits;
+    for (;;) {
+        const int32_t shift = max(bits - 8, 0);
         each([&](u64 key) {
-            if (key != 0 && (shift == 56 || key >> (shift + 8) == prefix))
-                atomicAdd(&l.histogram[(uint32_t)(key >> shift) & 255u], 1);
+            if (key != 0 && (bits == 64 || key >> bits == prefix))
+                atomicAdd(&l.histogram[(uint32_t)(key >> shift) & ((1u << (bits - shift)) - 1u)], 1);
         });
         __syncthreads();
         // every wave for itself: a lane has four bins, the highest first
@@ -164,9 +205,6 @@ __device__ __forceinline__ u64 kth_largest(Each each, int32_t k, ListLds& l)
 #pragma unroll
         for (int q = 0; q < 4; ++q) mine += n[q] = l.histogram[255 - (4 * lane + q)];
         const int32_t upto = wave_prefix(mine);
-        const int32_t all = lane_value(upto, kWave - 1);
-        __syncthreads();
-        if (shift == 56 && all <= k) return 1;
         int32_t digit = 0, above = upto - mine, in = 0;
         bool found = false;
 #pragma unroll
@@ -178,14 +216,16 @@ __device__ __forceinline__ u64 kth_largest(Each each, int32_t k, ListLds& l)
                 else above += n[q];
             }
         }
-        const uint64_t has = __ballot(found);
-        const int32_t at = __builtin_ctzll(has);
+        const int32_t at = __builtin_ctzll(__ballot(found));
         digit = lane_value(digit, at);
         k -= lane_value(above, at);
-        prefix = prefix << 8 | (uint32_t)digit;
-        if (lane_value(in, at) == k || shift == 0) return prefix << shift;
+        prefix = prefix << (bits - shift) | (uint32_t)digit;
+        bits = shift;
+        __syncthreads();
+        if (lane_value(in, at) == k || bits == 0) return prefix << bits;
+        for (int32_t i = tid; i < 256; i += BLOCK) l.histogram[i] = 0;
+        __syncthreads();
     }
-    return prefix;
 }
 
 // The list's entries of at least `bound`, at most kMostTop, to l.best; their number in every thread
@@ -264,7 +304,10 @@ __device__ __forceinline__ bool given_token(const LogProbArgs& a, int64_t row, f
     return true;
 }
 
-// A slice of a row a workgroup
+// A slice of a row a workgroup.  The first batch gives a bound from its chunks' largest; the others are read without
+// a barrier, each thread puts down what exceeds the bound, which rises each time as much again has been read: of a row in
+// no order some k more come each time.  Where more came than there is room for (a row that rises) they are gone through
+// again, the bound raised from batch to batch.
 template <class T, bool TOP>
 __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
 {
@@ -281,21 +324,17 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
     float token_x = 0.0f;
     const bool given = a.slices == 1 && given_token<T>(a, row, token_x);
     Sums sum = Sums::none();
-    u64 bound = place_of(-INFINITY, 0);
-    float bound_x = logit_of(bound + 1);  // what exceeds the bound is at least this, and above -infinity
-    if (TOP) {
-        if (tid == 0) l.count = 0;
-        __syncthreads();
-    }
     if (has_extra) sum.add(extra, a.c);
-    for (int32_t at = first; at < last || at == first; at += kBatch) {
-        uint4 raw[kScanLoads];
-        float tops[kScanLoads];
+    uint4 raw[kScanLoads];
+    float tops[kScanLoads];
+    const auto load = [&](int32_t at) {
 #pragma unroll
         for (int j = 0; j < kScanLoads; ++j) {
             const int32_t i = at + j * kScanBlock + tid;
             if (i < last) raw[j] = r.load(i);
         }
+    };
+    const auto add = [&](int32_t at) {
 #pragma unroll
         for (int j = 0; j < kScanLoads; ++j) {
             tops[j] = -INFINITY;
@@ -305,81 +344,121 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
                 tops[j] = sum.add(x, a.c);
             }
         }
-        if constexpr (TOP) {
-            const bool extras = at == first && has_extra;
-            // each element of at least `least`, in chunks that have some
-            const auto put = [&](u64 least) {
-                const float least_x = logit_of(least);
-                const auto one = [&](float x, int32_t id) {
-                    const u64 key = place_of(x, id);
-                    if (!(x >= least_x) || key < least) return;
-                    const int32_t n = atomicAdd(&l.count, 1);
-                    if (n < a.room) list[n] = key;
-                };
+    };
+    // each element of the batch that is at least `least`
+    const auto put_one = [&](float x, int32_t id, u64 least, float least_x) {
+        const u64 key = place_of(x, id);
+        if (!(x >= least_x) || key < least) return;
+        const int32_t n = atomicAdd(&l.count, 1);
+        if (n < a.room) list[n] = key;
+    };
+    const auto put = [&](int32_t at, u64 least, float least_x) {
 #pragma unroll
-                for (int j = 0; j < kScanLoads; ++j) {
-                    if (!(tops[j] >= least_x)) continue;
-                    float x[E];
-                    Row<T>::unpack(raw[j], x);
-                    const int32_t id = r.chunk(at + j * kScanBlock + tid);
+        for (int j = 0; j < kScanLoads; ++j) {
+            if (!(tops[j] >= least_x)) continue;
+            float x[E];
+            Row<T>::unpack(raw[j], x);
+            const int32_t id = r.chunk(at + j * kScanBlock + tid);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) one(x[e], id + e);
-                }
-                if (extras) one(extra[0], r.extra(tid));
-            };
-            // A bound from the batch alone: the k-th of its chunks' largest.  At least k elements, and at most
-            // k chunks' elements, reach it.
-            const auto raise = [&]() {
-                u64 keys[kScanLoads + 1];
+            for (int e = 0; e < E; ++e) put_one(x[e], id + e, least, least_x);
+        }
+    };
+    u64 bound = place_of(-INFINITY, 0);
+    float bound_x = logit_of(bound + 1);  // what exceeds the bound is at least this, and above -infinity
+    // What the batch's elements have to be at least, from the batch alone: the k-th of its chunks' largest, of those that
+    // exceed the bound.  At least k elements reach it, or all; at most k chunks have some that do.
+    const auto least_of = [&](int32_t at) {
+        u64 keys[kScanLoads];
 #pragma unroll
-                for (int j = 0; j < kScanLoads; ++j) {
-                    keys[j] = 0;
-                    if (!(tops[j] >= bound_x)) continue;
-                    float x[E];
-                    Row<T>::unpack(raw[j], x);
-                    const int32_t id = r.chunk(at + j * kScanBlock + tid);
+        for (int j = 0; j < kScanLoads; ++j) {
+            keys[j] = 0;
+            if (!(tops[j] >= bound_x)) continue;
+            float x[E];
+            Row<T>::unpack(raw[j], x);
+            const int32_t id = r.chunk(at + j * kScanBlock + tid);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        const u64 key = place_of(x[e], id + e);
-                        if (x[e] >= bound_x && key > bound && key > keys[j]) keys[j] = key;
-                    }
-                }
-                keys[kScanLoads] = 0;
-                if (extras && extra[0] >= bound_x) {
-                    const u64 key = place_of(extra[0], r.extra(tid));
-                    if (key > bound) keys[kScanLoads] = key;
-                }
-                const u64 kth = kth_largest<kScanBlock>([&](auto f) {
-#pragma unroll
-                    for (int j = 0; j <= kScanLoads; ++j) f(keys[j]);
-                }, a.k, l);
-                return kth > bound ? kth : bound + 1;
-            };
-            const int32_t before = l.count;
-            __syncthreads();
-            if (at == first && (last - first) * E > a.room) {  // else all of the batch would be put down
-                put(raise());
-            } else {
-                put(bound + 1);
-                __syncthreads();
-                if (l.count > a.room) {
-                    __syncthreads();
-                    if (tid == 0) l.count = before;
-                    const u64 least = raise();
-                    put(least);
-                }
-            }
-            __syncthreads();
-            const int32_t n = l.count;
-            if (n > a.room - E * a.k) {
-                __syncthreads();
-                bound = raised(bound, cut<kScanBlock>(list, n, a.k, l));
-                bound_x = logit_of(bound + 1);
+            for (int e = 0; e < E; ++e) {
+                const u64 key = place_of(x[e], id + e);
+                if (x[e] >= bound_x && key > bound && key > keys[j]) keys[j] = key;
             }
         }
-    }
+        const u64 kth = kth_largest<kScanBlock>([&](auto f) {
+#pragma unroll
+            for (int j = 0; j < kScanLoads; ++j) f(keys[j]);
+        }, a.k, l);
+        return kth > bound ? kth : bound + 1;
+    };
     int32_t n = 0;
-    if (TOP) {
+    if constexpr (!TOP) {
+        for (int32_t at = first; at < last; at += kBatch) {
+            load(at);
+            add(at);
+        }
+    } else {
+        if (tid == 0) l.count = 0;
+        load(first);
+        add(first);
+        if ((last - first + 2) * E > a.room) {  // (with the elements beside the chunks)
+            const u64 least = least_of(first);
+            bound = raised(bound, least);
+            bound_x = logit_of(bound + 1);
+        } else {
+            __syncthreads();
+        }
+        put(first, bound + 1, bound_x);
+        if (has_extra) put_one(extra[0], r.extra(tid), bound + 1, bound_x);
+        if (last - first > kBatch) {
+            __syncthreads();
+            int32_t kept = l.count, safe = first + kBatch, at = safe;  // the list at `safe`
+            __syncthreads();
+            for (int32_t until = kBatch;; until *= 2) {  // as many again as there were
+                const int32_t end = until < last - at ? at + until : last;
+                for (; at < end; at += kBatch) {
+                    load(at);
+                    add(at);
+                    put(at, bound + 1, bound_x);
+                }
+                __syncthreads();
+                n = l.count;
+                __syncthreads();
+                if (at >= last || n > a.room) break;
+                if (n >= 2 * a.k) {
+                    bound = raised(bound, cut<kScanBlock>(list, n, a.k, l));
+                    bound_x = logit_of(bound + 1);
+                    n = l.count;
+                }
+                kept = n;
+                safe = at;
+            }
+            if (n > a.room) {
+                if (tid == 0) l.count = kept;
+                for (int32_t b = safe; b < last; b += kBatch) {
+                    __syncthreads();
+                    n = l.count;
+                    if (n > a.room - E * a.k) {
+                        __syncthreads();
+                        bound = raised(bound, cut<kScanBlock>(list, n, a.k, l));
+                        bound_x = logit_of(bound + 1);
+                    }
+                    load(b);
+                    if (b >= at) {
+                        add(b);
+                    } else {  // the sums have these
+#pragma unroll
+                        for (int j = 0; j < kScanLoads; ++j) {
+                            tops[j] = -INFINITY;
+                            if (b + j * kScanBlock + tid >= last) continue;
+                            float x[E];
+                            Row<T>::unpack(raw[j], x);
+#pragma unroll
+                            for (int e = 0; e < E; ++e) tops[j] = fmaxf(tops[j], x[e]);
+                        }
+                    }
+                    const u64 least = least_of(b);
+                    put(b, least, logit_of(least));
+                }
+            }
+        }
         __syncthreads();
         n = l.count;
         __syncthreads();
