@@ -6,6 +6,8 @@
 // put on a list in LDS, and the bound rises when the list is cut to its k largest.  Elements are compared as one
 // number each, the logit's place in the order of numbers above the class's complement, so that no two are equal and
 // ties need no care.  Rows are cut into slices where there are few; the slices' sums and lists join.
+#include <type_traits>
+
 #include "softmax_rows.hpp"
 
 namespace lda {
@@ -325,62 +327,70 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
     const bool given = a.slices == 1 && given_token<T>(a, row, token_x);
     Sums sum = Sums::none();
     if (has_extra) sum.add(extra, a.c);
-    uint4 raw[kScanLoads];
-    float tops[kScanLoads];
-    const auto load = [&](int32_t at) {
-#pragma unroll
-        for (int j = 0; j < kScanLoads; ++j) {
-            const int32_t i = at + j * kScanBlock + tid;
-            if (i < last) raw[j] = r.load(i);
-        }
-    };
-    const auto add = [&](int32_t at) {
-#pragma unroll
-        for (int j = 0; j < kScanLoads; ++j) {
-            tops[j] = -INFINITY;
-            if (at + j * kScanBlock + tid < last) {
-                float x[E];
-                Row<T>::unpack(raw[j], x);
-                tops[j] = sum.add(x, a.c);
-            }
-        }
-    };
-    // each element of the batch that is at least `least`
+    u64 bound = place_of(-INFINITY, 0);
+    float bound_x = logit_of(bound + 1);  // what exceeds the bound is at least this, and above -infinity
+    float tops[kScanLoads];               // the largest of a batch's chunks
     const auto put_one = [&](float x, int32_t id, u64 least, float least_x) {
         const u64 key = place_of(x, id);
         if (!(x >= least_x) || key < least) return;
         const int32_t n = atomicAdd(&l.count, 1);
         if (n < a.room) list[n] = key;
     };
-    const auto put = [&](int32_t at, u64 least, float least_x) {
+    // Takes a batch: into the sums, if `sums`, and onto the list, if `puts`, each element that exceeds the bound
+    const auto take = [&](int32_t at, auto sums, auto puts) {
+        uint4 raw[kScanLoads];
 #pragma unroll
         for (int j = 0; j < kScanLoads; ++j) {
-            if (!(tops[j] >= least_x)) continue;
+            const int32_t i = at + j * kScanBlock + tid;
+            if (i < last) raw[j] = r.load(i);
+        }
+#pragma unroll
+        for (int j = 0; j < kScanLoads; ++j) {
+            const int32_t i = at + j * kScanBlock + tid;
+            tops[j] = -INFINITY;
+            if (i >= last) continue;
             float x[E];
             Row<T>::unpack(raw[j], x);
-            const int32_t id = r.chunk(at + j * kScanBlock + tid);
+            if (sums()) {
+                tops[j] = sum.add(x, a.c);
+            } else {
 #pragma unroll
-            for (int e = 0; e < E; ++e) put_one(x[e], id + e, least, least_x);
+                for (int e = 0; e < E; ++e) tops[j] = fmaxf(tops[j], x[e]);
+            }
+            if (puts() && tops[j] >= bound_x) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) put_one(x[e], r.chunk(i) + e, bound + 1, bound_x);
+            }
         }
     };
-    u64 bound = place_of(-INFINITY, 0);
-    float bound_x = logit_of(bound + 1);  // what exceeds the bound is at least this, and above -infinity
-    // What the batch's elements have to be at least, from the batch alone: the k-th of its chunks' largest, of those that
-    // exceed the bound.  At least k elements reach it, or all; at most k chunks have some that do.
+    // Puts down what a batch that has been taken has of at least `least`, read again: rare, and the chunks' registers
+    // are worth more to others
+    const auto put = [&](int32_t at, u64 least) {
+        const float least_x = logit_of(least);
+        uint32_t some = 0;
+#pragma unroll
+        for (int j = 0; j < kScanLoads; ++j) some |= tops[j] >= least_x ? 1u << j : 0u;
+        while (some != 0) {
+            const int32_t i = at + __builtin_ctz(some) * kScanBlock + tid;
+            some &= some - 1;
+            float x[E];
+            Row<T>::unpack(r.load(i), x);
+#pragma unroll
+            for (int e = 0; e < E; ++e) put_one(x[e], r.chunk(i) + e, least, least_x);
+        }
+    };
+    // What a batch's elements have to be at least, from the batch alone: the k-th of its chunks' largest, of those that
+    // exceed the bound.  A chunk's largest counts as the last element of its chunk, which it is at least.  At least k elements
+    // reach the k-th, or all do that exceed the bound; and chunks that have some are k at most, and two that end beyond the bound
+    // or the k-th and have equal ones before.
     const auto least_of = [&](int32_t at) {
         u64 keys[kScanLoads];
 #pragma unroll
         for (int j = 0; j < kScanLoads; ++j) {
             keys[j] = 0;
             if (!(tops[j] >= bound_x)) continue;
-            float x[E];
-            Row<T>::unpack(raw[j], x);
-            const int32_t id = r.chunk(at + j * kScanBlock + tid);
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const u64 key = place_of(x[e], id + e);
-                if (x[e] >= bound_x && key > bound && key > keys[j]) keys[j] = key;
-            }
+            const u64 key = place_of(tops[j], r.chunk(at + j * kScanBlock + tid) + E - 1);
+            if (key > bound) keys[j] = key;
         }
         const u64 kth = kth_largest<kScanBlock>([&](auto f) {
 #pragma unroll
@@ -389,23 +399,20 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
         return kth > bound ? kth : bound + 1;
     };
     int32_t n = 0;
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
     if constexpr (!TOP) {
-        for (int32_t at = first; at < last; at += kBatch) {
-            load(at);
-            add(at);
-        }
+        for (int32_t at = first; at < last; at += kBatch) take(at, yes, no);
     } else {
         if (tid == 0) l.count = 0;
-        load(first);
-        add(first);
+        take(first, yes, no);
         if ((last - first + 2) * E > a.room) {  // (with the elements beside the chunks)
-            const u64 least = least_of(first);
-            bound = raised(bound, least);
+            bound = raised(bound, least_of(first));
             bound_x = logit_of(bound + 1);
         } else {
             __syncthreads();
         }
-        put(first, bound + 1, bound_x);
+        put(first, bound + 1);
         if (has_extra) put_one(extra[0], r.extra(tid), bound + 1, bound_x);
         if (last - first > kBatch) {
             __syncthreads();
@@ -413,11 +420,7 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
             __syncthreads();
             for (int32_t until = kBatch;; until *= 2) {  // as many again as there were
                 const int32_t end = until < last - at ? at + until : last;
-                for (; at < end; at += kBatch) {
-                    load(at);
-                    add(at);
-                    put(at, bound + 1, bound_x);
-                }
+                for (; at < end; at += kBatch) take(at, yes, yes);
                 __syncthreads();
                 n = l.count;
                 __syncthreads();
@@ -435,27 +438,14 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
                 for (int32_t b = safe; b < last; b += kBatch) {
                     __syncthreads();
                     n = l.count;
-                    if (n > a.room - E * a.k) {
+                    if (n > a.room - E * (a.k + 2)) {
                         __syncthreads();
                         bound = raised(bound, cut<kScanBlock>(list, n, a.k, l));
                         bound_x = logit_of(bound + 1);
                     }
-                    load(b);
-                    if (b >= at) {
-                        add(b);
-                    } else {  // the sums have these
-#pragma unroll
-                        for (int j = 0; j < kScanLoads; ++j) {
-                            tops[j] = -INFINITY;
-                            if (b + j * kScanBlock + tid >= last) continue;
-                            float x[E];
-                            Row<T>::unpack(raw[j], x);
-#pragma unroll
-                            for (int e = 0; e < E; ++e) tops[j] = fmaxf(tops[j], x[e]);
-                        }
-                    }
-                    const u64 least = least_of(b);
-                    put(b, least, logit_of(least));
+                    if (b >= at) take(b, yes, no);
+                    else take(b, no, no);  // the sums have these
+                    put(b, least_of(b));
                 }
             }
         }
