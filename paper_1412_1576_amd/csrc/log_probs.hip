@@ -27,6 +27,9 @@ constexpr float kFloorY = -1.0e4f;  // powers of 2: none is left of e^y, and y e
 
 typedef unsigned long long u64;
 
+// Where k are wanted so many do as well: a bound among them is found by the first bits that differ, nearly always
+__host__ __device__ constexpr int32_t enough(int32_t k) { return k + (k / 4 > 8 ? k / 4 : 8); }
+
 struct LogProbArgs {
     int64_t rows, row0;
     int32_t V, k;
@@ -38,7 +41,7 @@ struct LogProbArgs {
     float T, c;  // c = log2(e) / T
     int32_t slices, slice_chunks, room;  // room: of a list in LDS
     struct LogProbPart* parts;  // [rows][slices]
-    u64* lists;                 // [rows][slices][k]
+    u64* lists;                 // [rows][slices][enough(k)]
     float* log_prob;
     float* entropy;
     int32_t* ids;
@@ -144,7 +147,7 @@ struct ListLds {
     int32_t count, chosen;
     uint32_t high[16], low[16];
     int32_t number[16];
-    u64 best[kMostTop];
+    u64 best[enough(kMostTop)];
 };
 
 __device__ __forceinline__ uint32_t wave_most(uint32_t v)
@@ -152,12 +155,11 @@ __device__ __forceinline__ uint32_t wave_most(uint32_t v)
     return (uint32_t)lane_value((int32_t)wave_scan(v, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; }), kWave - 1);
 }
 
-// The k-th largest of the workgroup's numbers, which each(f) gives to f; 1 where there are at most k.  By 8 bits
-// at a time from the first on that is not the same in all, until those with the same upper bits are all wanted: exactly k
-// numbers are at least what it returns, which need not be one of them.  (Bits that are the same in all would put every number
-// into one bin, one after the other.)
+// A bound that at least k and at most enough(k) of the workgroup's numbers reach, which each(f) gives to f; 1 where there
+// are fewer.  By 8 bits at a time from the first on that is not the same in all.  (Bits that are the same in all would
+// put every number into one bin, one after the other.)
 template <int BLOCK, class Each>
-__device__ __forceinline__ u64 kth_largest(Each each, int32_t k, ListLds& l)
+__device__ __forceinline__ u64 bound_of(Each each, int32_t k, ListLds& l)
 {
     constexpr int kWaves = BLOCK / kWave;
     const int32_t tid = (int32_t)threadIdx.x, lane = tid % kWave;
@@ -188,10 +190,12 @@ __device__ __forceinline__ u64 kth_largest(Each each, int32_t k, ListLds& l)
         low = max(low, l.low[w]);
         number += l.number[w];
     }
-    if (number <= k) {
+    const int32_t most = enough(k);
+    if (number <= most) {
         __syncthreads();
         return 1;
     }
+    int32_t taken = 0;  // above the prefix
     const uint32_t differ = high ^ ~low;
     int32_t bits = differ == 0 ? 32 : 64 - __builtin_clz(differ);  // the lowest ones, that differ
     u64 prefix = bits == 64 ? 0 : ((u64)high << 32) >> bits;
@@ -207,30 +211,31 @@ __device__ __forceinline__ u64 kth_largest(Each each, int32_t k, ListLds& l)
 #pragma unroll
         for (int q = 0; q < 4; ++q) mine += n[q] = l.histogram[255 - (4 * lane + q)];
         const int32_t upto = wave_prefix(mine);
-        int32_t digit = 0, above = upto - mine, in = 0;
+        int32_t digit = 0, above = taken + upto - mine;
         bool found = false;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             if (!found) {
                 digit = 255 - (4 * lane + q);
-                in = n[q];
-                if (above + n[q] >= k) found = true;
-                else above += n[q];
+                above += n[q];
+                found = above >= k;
+                if (found) mine = n[q];
             }
         }
         const int32_t at = __builtin_ctzll(__ballot(found));
         digit = lane_value(digit, at);
-        k -= lane_value(above, at);
+        above = lane_value(above, at);
+        taken = above - lane_value(mine, at);
         prefix = prefix << (bits - shift) | (uint32_t)digit;
         bits = shift;
         __syncthreads();
-        if (lane_value(in, at) == k || bits == 0) return prefix << bits;
+        if (above <= most || bits == 0) return prefix << bits;
         for (int32_t i = tid; i < 256; i += BLOCK) l.histogram[i] = 0;
         __syncthreads();
     }
 }
 
-// The list's entries of at least `bound`, at most kMostTop, to l.best; their number in every thread
+// The list's entries of at least `bound`, at most enough(k), to l.best; their number in every thread
 template <int BLOCK>
 __device__ __forceinline__ int32_t choose(const u64* list, int32_t n, u64 bound, ListLds& l)
 {
@@ -244,11 +249,11 @@ __device__ __forceinline__ int32_t choose(const u64* list, int32_t n, u64 bound,
     return l.chosen;
 }
 
-// Cuts the list to its k largest, which then are in l.best too; returns kth_largest()'s
+// Cuts the list to enough(k) of its largest, which then are in l.best too; returns bound_of()'s
 template <int BLOCK>
 __device__ __forceinline__ u64 cut(u64* list, int32_t n, int32_t k, ListLds& l)
 {
-    const u64 bound = kth_largest<BLOCK>([&](auto f) {
+    const u64 bound = bound_of<BLOCK>([&](auto f) {
         for (int32_t i = (int32_t)threadIdx.x; i < n; i += BLOCK) f(list[i]);
     }, k, l);
     const int32_t some = choose<BLOCK>(list, n, bound, l);
@@ -278,13 +283,15 @@ __device__ __forceinline__ void finish_row(const LogProbArgs& a, int64_t row, co
         if (a.stats) *reinterpret_cast<float4*>(a.stats + row * kLogProbStats) = make_float4(sum.m, sum.s, h, 0.0f);
     }
     if (!TOP) return;
-    for (int32_t i = (int32_t)threadIdx.x; i < a.k; i += BLOCK) {
+    for (int32_t i = (int32_t)threadIdx.x; i < max(a.k, n); i += BLOCK) {
         int32_t at = i, id = -1;
         float top = none ? NAN : -INFINITY;
         if (i < n) {
             const u64 key = l.best[i];
             at = 0;
+#pragma unroll 8
             for (int32_t j = 0; j < n; ++j) at += l.best[j] > key;
+            if (at >= a.k) continue;
             if (!none) {
                 id = id_of(key);
                 top = (float)(((double)logit_of(key) - m) * inv_t - log_s);
@@ -331,8 +338,9 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
     float bound_x = logit_of(bound + 1);  // what exceeds the bound is at least this, and above -infinity
     float tops[kScanLoads];               // the largest of a batch's chunks
     const auto put_one = [&](float x, int32_t id, u64 least, float least_x) {
+        if (!(x >= least_x)) return;
         const u64 key = place_of(x, id);
-        if (!(x >= least_x) || key < least) return;
+        if (key < least) return;
         const int32_t n = atomicAdd(&l.count, 1);
         if (n < a.room) list[n] = key;
     };
@@ -379,10 +387,10 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
             for (int e = 0; e < E; ++e) put_one(x[e], r.chunk(i) + e, least, least_x);
         }
     };
-    // What a batch's elements have to be at least, from the batch alone: the k-th of its chunks' largest, of those that
+    // What a batch's elements have to be at least, from the batch alone: a bound of its chunks' largest, of those that
     // exceed the bound.  A chunk's largest counts as the last element of its chunk, which it is at least.  At least k elements
-    // reach the k-th, or all do that exceed the bound; and chunks that have some are k at most, and two that end beyond the bound
-    // or the k-th and have equal ones before.
+    // reach it, or all do that exceed the bound; and the chunks that have some are enough(k) at most, and two that end beyond
+    // the bound or the new one and have equal ones before.
     const auto least_of = [&](int32_t at) {
         u64 keys[kScanLoads];
 #pragma unroll
@@ -392,11 +400,11 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
             const u64 key = place_of(tops[j], r.chunk(at + j * kScanBlock + tid) + E - 1);
             if (key > bound) keys[j] = key;
         }
-        const u64 kth = kth_largest<kScanBlock>([&](auto f) {
+        const u64 least = bound_of<kScanBlock>([&](auto f) {
 #pragma unroll
             for (int j = 0; j < kScanLoads; ++j) f(keys[j]);
         }, a.k, l);
-        return kth > bound ? kth : bound + 1;
+        return least > bound ? least : bound + 1;
     };
     int32_t n = 0;
     constexpr std::true_type yes{};
@@ -425,7 +433,7 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
                 n = l.count;
                 __syncthreads();
                 if (at >= last || n > a.room) break;
-                if (n >= 2 * a.k) {
+                if (n >= 2 * enough(a.k)) {
                     bound = raised(bound, cut<kScanBlock>(list, n, a.k, l));
                     bound_x = logit_of(bound + 1);
                     n = l.count;
@@ -438,7 +446,7 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
                 for (int32_t b = safe; b < last; b += kBatch) {
                     __syncthreads();
                     n = l.count;
-                    if (n > a.room - E * (a.k + 2)) {
+                    if (n > a.room - E * (enough(a.k) + 2)) {
                         __syncthreads();
                         bound = raised(bound, cut<kScanBlock>(list, n, a.k, l));
                         bound_x = logit_of(bound + 1);
@@ -452,7 +460,7 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
         __syncthreads();
         n = l.count;
         __syncthreads();
-        if (n > a.k) {
+        if (n > enough(a.k)) {
             cut<kScanBlock>(list, n, a.k, l);
             n = l.count;
         } else {
@@ -467,7 +475,7 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
     const int64_t at = row * a.slices + slice;
     if (tid == 0) a.parts[at] = LogProbPart{sum.m, sum.s, sum.u, n};
     if (TOP)
-        for (int32_t i = tid; i < n; i += kScanBlock) a.lists[at * a.k + i] = l.best[i];
+        for (int32_t i = tid; i < n; i += kScanBlock) a.lists[at * enough(a.k) + i] = l.best[i];
 }
 
 // A row's slices joined, a workgroup a row
@@ -491,15 +499,15 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_join_kernel(LogProbArgs 
         if (tid == 0) l.count = 0;
         __syncthreads();
         u64 bound = 0;
-        const u64* const lists = a.lists + row * a.slices * a.k;
-        const int32_t total = a.slices * a.k;
+        const int32_t each = enough(a.k), total = a.slices * each;
+        const u64* const lists = a.lists + row * total;
         for (int32_t at = 0; at < total; at += kScanBlock * kJoinEach) {
             u64 key[kJoinEach];
 #pragma unroll
             for (int j = 0; j < kJoinEach; ++j) {
                 const int32_t i = at + j * kScanBlock + tid;
                 key[j] = 0;
-                if (i < total && i % a.k < parts[i / a.k].n) key[j] = lists[i];
+                if (i < total && i % each < parts[i / each].n) key[j] = lists[i];
             }
 #pragma unroll
             for (int j = 0; j < kJoinEach; ++j)
@@ -513,7 +521,7 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_join_kernel(LogProbArgs 
                 __syncthreads();
             }
         }
-        if (n > a.k) {
+        if (n > enough(a.k)) {
             cut<kScanBlock>(list, n, a.k, l);
             n = l.count;
         } else {
@@ -606,8 +614,9 @@ static Slices slices_of(const lda_log_prob_rows* d)
     const int64_t wanted = d->rows >= 1024 ? 1 : 1024 / (d->rows < 1 ? 1 : d->rows);
     const int64_t most = (whole + kScanBlock - 1) / kScanBlock;
     int64_t count = wanted < most ? wanted : most;
+    if (count == 1) return {1, (int32_t)whole};
     int64_t chunks = (whole + count - 1) / count;
-    chunks = (chunks + kScanBlock - 1) / kScanBlock * kScanBlock;
+    chunks = chunks > kBatch ? (chunks + kBatch / 2) / kBatch * kBatch : (chunks + kScanBlock - 1) / kScanBlock * kScanBlock;
     count = (whole + chunks - 1) / chunks;
     return {(int32_t)count, (int32_t)chunks};
 }
@@ -616,7 +625,7 @@ static int64_t log_prob_bytes(const lda_log_prob_rows* d)
 {
     const int64_t count = slices_of(d).count;
     if (d->rows == 0 || count == 1) return 0;
-    return d->rows * count * ((int64_t)sizeof(LogProbPart) + d->top * (int64_t)sizeof(u64));
+    return d->rows * count * ((int64_t)sizeof(LogProbPart) + (d->top > 0 ? enough(d->top) : 0) * (int64_t)sizeof(u64));
 }
 
 }  // namespace lda
@@ -671,8 +680,8 @@ try {
     const hipStream_t stream = static_cast<hipStream_t>(d->hip_stream);
     const auto typed = [&](auto t) {
         using T = decltype(t);
-        // k largest, and what a batch may bring before they are cut: k chunks, or some hundreds
-        a.room = a.k + Row<T>::kChunk * a.k + 768;
+        // what a cut leaves, what a batch may bring behind it, and some hundreds between two cuts
+        a.room = enough(a.k) + Row<T>::kChunk * (enough(a.k) + 2) + 768;
         const size_t lds = a.k > 0 ? (size_t)a.room * sizeof(u64) : 0;
         for (a.row0 = 0; a.row0 < a.rows; a.row0 += 1 << 20) {
             const unsigned n = (unsigned)(a.rows - a.row0 < (1 << 20) ? a.rows - a.row0 : 1 << 20);
