@@ -61,46 +61,37 @@ __device__ __forceinline__ float scaled(float v, float scale)
 }
 __device__ __forceinline__ float scaled(int32_t sum, float sa, float sb) { return scaled((float)sum * sa, sb); }
 
-// Up to 16 MT rows times 16 CT classes a workgroup; its waves take the row's steps in turn and join in LDS.
-template <class T, int MT, int CT, bool ALIGNED>
+// Up to 16 rows times 16 CT classes a workgroup; its waves take the row's steps in turn and join in LDS.
+template <class T, int CT, bool ALIGNED>
 __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs p)
 {
-    constexpr int kWaves = 4, kClasses = 16 * CT, kRows = 16 * MT;
-    __shared__ int32_t part[kWaves][kRows][kClasses + 4];
+    constexpr int kWaves = 4, kClasses = 16 * CT, kUnroll = 4;
+    __shared__ int32_t part[kWaves][16][kClasses + 4];
     const int32_t tid = (int32_t)threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const int32_t n0 = (int32_t)blockIdx.x * kClasses, split = (int32_t)blockIdx.y;
     const int32_t from = split * p.split_k, end = min(p.K, from + p.split_k);
     const int32_t r = lane % 16, g = lane / 16 * 16;
-    const int8_t *a[MT], *b[CT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) a[i] = p.a + min((int64_t)(16 * i + r), p.M - 1) * p.a_stride;
+    const int8_t* const a = p.a + min((int64_t)r, p.M - 1) * p.a_stride;
+    const int8_t* b[CT];
 #pragma unroll
     for (int i = 0; i < CT; ++i) b[i] = p.b + (int64_t)min(n0 + 16 * i + r, p.N - 1) * p.b_stride;
-    i32x4 sum[CT][MT];
+    i32x4 sum[CT];
 #pragma unroll
-    for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int m = 0; m < MT; ++m) sum[c][m] = i32x4{0, 0, 0, 0};
-    constexpr int kUnroll = MT * CT >= 8 ? 2 : 4;
+    for (int c = 0; c < CT; ++c) sum[c] = i32x4{0, 0, 0, 0};
     const auto take = [&](auto steps, auto whole, int32_t k) {
-        i32x4 x[steps()][MT], w[steps()][CT];
+        i32x4 x[steps()], w[steps()][CT];
 #pragma unroll
         for (int u = 0; u < steps(); ++u) {
             const int32_t at = k + u * kWaves * kStep;
 #pragma unroll
             for (int c = 0; c < CT; ++c)
                 w[u][c] = whole() ? *reinterpret_cast<const i32x4*>(b[c] + at) : load16(b[c], at, end);
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-                x[u][m] = whole() ? *reinterpret_cast<const i32x4*>(a[m] + at) : load16(a[m], at, end);
+            x[u] = whole() ? *reinterpret_cast<const i32x4*>(a + at) : load16(a, at, end);
         }
 #pragma unroll
         for (int u = 0; u < steps(); ++u)
 #pragma unroll
-            for (int c = 0; c < CT; ++c)
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-                    sum[c][m] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][c], x[u][m], sum[c][m], 0, 0, 0);
+            for (int c = 0; c < CT; ++c) sum[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][c], x[u], sum[c], 0, 0, 0);
     };
     int32_t k = from + wave * kStep + g;
     if (ALIGNED)
@@ -109,13 +100,10 @@ __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs p)
     for (; k - g < end; k += kWaves * kStep) take(std::integral_constant<int, 1>{}, std::false_type{}, k);
     // lane: 4 adjacent classes of a row
 #pragma unroll
-    for (int c = 0; c < CT; ++c)
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-            *reinterpret_cast<i32x4*>(&part[wave][16 * m + lane % 16][16 * c + lane / 16 * 4]) = sum[c][m];
+    for (int c = 0; c < CT; ++c) *reinterpret_cast<i32x4*>(&part[wave][r][16 * c + g / 4]) = sum[c];
     __syncthreads();
     T* const out = static_cast<T*>(p.out);
-    for (int32_t i = tid; i < kRows * kClasses; i += 256) {
+    for (int32_t i = tid; i < 16 * kClasses; i += 256) {
         const int32_t m = i / kClasses, c = i % kClasses, n = n0 + c;
         if (m >= p.M || n >= p.N) continue;
         const int32_t s = part[0][m][c] + part[1][m][c] + part[2][m][c] + part[3][m][c];
@@ -129,8 +117,9 @@ __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs p)
 template <int PRODUCTS, int READS, int PAIRS>
 __device__ __forceinline__ void interleave(bool pairs)
 {
+    if (PRODUCTS < 4) return;  // few products: memory is what is waited for
     constexpr int kReadsEach = READS * 2 > PRODUCTS ? 2 : 1, kFirst = (READS + kReadsEach - 1) / kReadsEach;
-    constexpr int kPairsEach = (PAIRS + PRODUCTS - kFirst - 1) / (PRODUCTS - kFirst);
+    constexpr int kRest = PRODUCTS > kFirst ? PRODUCTS - kFirst : 1, kPairsEach = (PAIRS + kRest - 1) / kRest;
 #pragma unroll
     for (int i = 0; i < PRODUCTS; ++i) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix
@@ -425,7 +414,7 @@ static int check_product(const lda_product_rows* d, const char* call)
     return LDA_OK;
 }
 
-enum class ProductKind { kFew, kTile128, kTile256 };
+enum class ProductKind { kFew, kTile64, kTile128, kTile256 };
 struct ProductPlan {
     ProductKind kind;
     int classes, splits;  // of the few-rows kernel: 16-class tiles of a wave
@@ -435,12 +424,15 @@ static ProductPlan plan_product(const lda_product_rows* d)
 {
     ProductPlan p{};
     int64_t groups;
-    if (d->rows <= 64) {
+    const auto tiles = [&](int64_t m, int64_t n) { return ((d->rows + m - 1) / m) * ((d->classes + n - 1) / n); };
+    if (d->rows <= 16) {
         p.kind = ProductKind::kFew;
-        p.classes = d->classes >= 32768 && d->rows <= 48 ? 4 : d->classes >= 16384 ? 2 : 1;
-        groups = ((int64_t)d->classes + 16 * p.classes - 1) / (16 * p.classes);
+        p.classes = d->classes >= 32768 ? 4 : d->classes >= 16384 ? 2 : 1;
+        groups = tiles(16, 16 * p.classes);
+    } else if (d->rows <= 64) {
+        p.kind = ProductKind::kTile64;
+        groups = tiles(64, 128);
     } else {
-        const auto tiles = [&](int64_t m, int64_t n) { return ((d->rows + m - 1) / m) * ((d->classes + n - 1) / n); };
         p.kind = tiles(256, 256) >= 768 ? ProductKind::kTile256 : ProductKind::kTile128;
         groups = p.kind == ProductKind::kTile256 ? tiles(256, 256) : tiles(128, 128);
     }
@@ -476,9 +468,9 @@ static hipError_t launch_product(ProductArgs a, const ProductPlan& plan, hipStre
 {
     a.splits = plan.splits;
     a.split_k = plan.split_k;
-    const auto few = [&](auto mt, auto ct) {
+    const auto few = [&](auto ct) {
         const dim3 grid((unsigned)((a.N + 16 * ct() - 1) / (16 * ct())), (unsigned)a.splits);
-        product_few_kernel<T, mt(), ct(), ALIGNED><<<grid, 256, 0, stream>>>(a);
+        product_few_kernel<T, ct(), ALIGNED><<<grid, 256, 0, stream>>>(a);
     };
     const auto tile = [&](auto tm, auto tn, auto wm, auto wn) {
         a.tiles_m = (int32_t)((a.M + tm() - 1) / tm());
@@ -497,28 +489,16 @@ static hipError_t launch_product(ProductArgs a, const ProductPlan& plan, hipStre
     };
     using std::integral_constant;
     if (plan.kind == ProductKind::kFew) {
-        const int mt = (int)((a.M + 15) / 16);
-        const auto with = [&](auto ct) {
-            if (mt == 1) few(integral_constant<int, 1>{}, ct);
-            else if (mt == 2) few(integral_constant<int, 2>{}, ct);
-            else if (mt == 3) few(integral_constant<int, 3>{}, ct);
-            else few(integral_constant<int, 4>{}, ct);
-        };
-        if (plan.classes == 4) {
-            const auto ct = integral_constant<int, 4>{};
-            if (mt == 1) few(integral_constant<int, 1>{}, ct);
-            else if (mt == 2) few(integral_constant<int, 2>{}, ct);
-            else few(integral_constant<int, 3>{}, ct);
-        } else if (plan.classes == 2) {
-            with(integral_constant<int, 2>{});
-        } else {
-            with(integral_constant<int, 1>{});
-        }
+        if (plan.classes == 4) few(integral_constant<int, 4>{});
+        else if (plan.classes == 2) few(integral_constant<int, 2>{});
+        else few(integral_constant<int, 1>{});
     } else {
         const auto c256 = integral_constant<int, 256>{};
         const auto c128 = integral_constant<int, 128>{};
+        const auto c64 = integral_constant<int, 64>{};
         const auto c2 = integral_constant<int, 2>{};
-        const hipError_t e = plan.kind == ProductKind::kTile256 ? tile(c256, c256, c2, c2) : tile(c128, c128, c2, c2);
+        const hipError_t e = plan.kind == ProductKind::kTile256 ? tile(c256, c256, c2, c2)
+                             : plan.kind == ProductKind::kTile128 ? tile(c128, c128, c2, c2) : tile(c64, c128, c2, c2);
         if (e != hipSuccess) return e;
     }
     if (a.splits > 1) launch_join<T>(a, stream);
