@@ -425,7 +425,7 @@ static ProductPlan plan_product(const lda_product_rows* d)
     ProductPlan p{};
     int64_t groups;
     const auto tiles = [&](int64_t m, int64_t n) { return ((d->rows + m - 1) / m) * ((d->classes + n - 1) / n); };
-    if (d->rows <= 16) {
+    if (d->rows <= 8 || (d->rows <= 16 && d->classes < 65536)) {
         p.kind = ProductKind::kFew;
         p.classes = d->classes >= 32768 ? 4 : d->classes >= 16384 ? 2 : 1;
         groups = tiles(16, 16 * p.classes);
