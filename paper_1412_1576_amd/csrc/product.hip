@@ -38,12 +38,18 @@ struct ProductArgs {
     int32_t tiles_m, tiles_n;
 };
 
-// 16 bytes of a row from k on, 0 behind `end`, from any address
+__device__ __forceinline__ i32x4 load16(const int8_t* from)
+{
+    i32x4 v;
+    __builtin_memcpy(&v, from, 16);
+    return v;
+}
+// 16 bytes of a row from k on, 0 behind `end`
 __device__ __forceinline__ i32x4 load16(const int8_t* row, int32_t k, int32_t end)
 {
     i32x4 v = {0, 0, 0, 0};
     if (k + 16 <= end) {
-        __builtin_memcpy(&v, row + k, 16);
+        v = load16(row + k);
     } else if (k < end) {
         const int32_t n = end - k;
 #pragma unroll
@@ -61,8 +67,9 @@ __device__ __forceinline__ float scaled(float v, float scale)
 }
 __device__ __forceinline__ float scaled(int32_t sum, float sa, float sb) { return scaled((float)sum * sa, sb); }
 
-// Up to 16 rows times 16 CT classes a workgroup; its waves take the row's steps in turn and join in LDS.
-template <class T, int CT, bool ALIGNED>
+// Up to 16 rows times 16 CT classes a workgroup; its waves take the row's steps in turn and join in LDS.  Rows lie
+// anywhere: the hardware's loads take any address.
+template <class T, int CT>
 __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs p)
 {
     constexpr int kWaves = 4, kClasses = 16 * CT, kUnroll = 4;
@@ -85,8 +92,8 @@ __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs p)
             const int32_t at = k + u * kWaves * kStep;
 #pragma unroll
             for (int c = 0; c < CT; ++c)
-                w[u][c] = whole() ? *reinterpret_cast<const i32x4*>(b[c] + at) : load16(b[c], at, end);
-            x[u] = whole() ? *reinterpret_cast<const i32x4*>(a + at) : load16(a, at, end);
+                w[u][c] = whole() ? load16(b[c] + at) : load16(b[c], at, end);
+            x[u] = whole() ? load16(a + at) : load16(a, at, end);
         }
 #pragma unroll
         for (int u = 0; u < steps(); ++u)
@@ -94,9 +101,8 @@ __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs p)
             for (int c = 0; c < CT; ++c) sum[c] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u][c], x[u], sum[c], 0, 0, 0);
     };
     int32_t k = from + wave * kStep + g;
-    if (ALIGNED)
-        for (; k - g + (kUnroll - 1) * kWaves * kStep + kStep <= end; k += kUnroll * kWaves * kStep)
-            take(std::integral_constant<int, kUnroll>{}, std::true_type{}, k);
+    for (; k - g + (kUnroll - 1) * kWaves * kStep + kStep <= end; k += kUnroll * kWaves * kStep)
+        take(std::integral_constant<int, kUnroll>{}, std::true_type{}, k);
     for (; k - g < end; k += kWaves * kStep) take(std::integral_constant<int, 1>{}, std::false_type{}, k);
     // lane: 4 adjacent classes of a row
 #pragma unroll
@@ -219,10 +225,11 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void product_tile_kernel(ProductAr
             held[i] = __builtin_bit_cast(i32x4, of_a ? __builtin_amdgcn_raw_buffer_load_b128(buffer_a, (at_a + ((uint32_t)k_next + j * step_a)) | beyond, 0, 0)
                                                      : __builtin_amdgcn_raw_buffer_load_b128(buffer_b, at_b + ((uint32_t)k_next + j * step_b), 0, 0));
         } else {
-            held[i] = i32x4{0, 0, 0, 0};
-            if (next.rows_a > 0)
-                held[i] = of_a ? load16(next.a + min(row0 + j * kRowsAtOnce, next.rows_a - 1) * p.a_stride, k_next + piece, next.end)
-                               : load16(next.b + min(row0 + j * kRowsAtOnce, next.rows_b - 1) * p.b_stride, k_next + piece, next.end);
+            const int8_t* const row = of_a ? next.a + min(row0 + j * kRowsAtOnce, next.rows_a - 1) * p.a_stride
+                                           : next.b + min(row0 + j * kRowsAtOnce, next.rows_b - 1) * p.b_stride;
+            if (next.rows_a == 0) held[i] = i32x4{0, 0, 0, 0};
+            else if (k_next + kTileK <= next.end) held[i] = load16(row + k_next + piece);
+            else held[i] = load16(row, k_next + piece, next.end);
         }
     };
     const int32_t put_at = row0 * kTileK + (piece ^ (row0 / 2 % 8 * 16));
@@ -380,6 +387,14 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void product_tile_kernel(ProductAr
     }
 }
 
+// Rows that lie anywhere, side by side in pieces of 16 bytes, with zeros behind a row's end; a wave a row
+__global__ __launch_bounds__(256) void product_pack_kernel(const int8_t* from, int64_t stride, int64_t rows, int32_t width, i32x4* to)
+{
+    const int32_t pieces = (width + 15) / 16;
+    for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave; row < rows; row += (int64_t)gridDim.x * 4)
+        for (int32_t i = threadIdx.x % kWave; i < pieces; i += kWave) to[row * pieces + i] = load16(from + row * stride, i * 16, width);
+}
+
 // The splits' sums added up; none of a width of 0
 template <class T>
 __global__ __launch_bounds__(256) void product_join_kernel(ProductArgs p)
@@ -417,14 +432,25 @@ static int check_product(const lda_product_rows* d, const char* call)
 enum class ProductKind { kFew, kTile64, kTile128, kTile256 };
 struct ProductPlan {
     ProductKind kind;
-    int classes, splits;  // of the few-rows kernel: 16-class tiles of a wave
+    int classes, splits;    // of the few-rows kernel: 16-class tiles of a wave
     int32_t split_k;
+    bool aligned;           // for the tiles' buffers; otherwise rows are read where they lie
+    int64_t a_bytes, b_bytes;  // of rows that are packed first
 };
+// Loads of 16 bytes at multiples of 16, places inside a tile in 32 bits
+static bool in_pieces(const void* p, int64_t stride)
+{
+    return aligned_to(p, 16) && stride % 16 == 0 && stride >= 0 && stride < 1 << 22;
+}
 static ProductPlan plan_product(const lda_product_rows* d)
 {
     ProductPlan p{};
     int64_t groups;
     const auto tiles = [&](int64_t m, int64_t n) { return ((d->rows + m - 1) / m) * ((d->classes + n - 1) / n); };
+    const bool whole = d->width % 16 == 0, a_fine = whole && in_pieces(d->a, d->a_stride), b_fine = whole && in_pieces(d->b, d->b_stride);
+    p.aligned = a_fine && b_fine;
+    // 16 x 5120 x 101636: 134 us by the few-rows kernel, 106 by tiles; 16 x 4096 x 10000: 14.6 and 25; 8 x 4096 x
+    // 141043: 121 and 126
     if (d->rows <= 8 || (d->rows <= 16 && d->classes < 65536)) {
         p.kind = ProductKind::kFew;
         p.classes = d->classes >= 32768 ? 4 : d->classes >= 16384 ? 2 : 1;
@@ -435,6 +461,10 @@ static ProductPlan plan_product(const lda_product_rows* d)
     } else {
         p.kind = tiles(256, 256) >= 768 ? ProductKind::kTile256 : ProductKind::kTile128;
         groups = p.kind == ProductKind::kTile256 ? tiles(256, 256) : tiles(128, 128);
+        const int64_t packed = ((int64_t)d->width + 15) / 16 * 16;
+        if (!a_fine) p.a_bytes = d->rows * packed;
+        if (!b_fine) p.b_bytes = d->classes * packed;
+        p.aligned = true;
     }
     // a split has 1024 bytes of a row at least
     int64_t splits = groups >= 192 ? 1 : 256 / (groups < 1 ? 1 : groups);
@@ -442,10 +472,9 @@ static ProductPlan plan_product(const lda_product_rows* d)
     if (splits > most) splits = most;
     if (splits < 1) splits = 1;
     const int64_t pieces = ((int64_t)d->width + kTileK - 1) / kTileK;
-    const int64_t each = (pieces + splits - 1) / splits;
-    p.split_k = (int32_t)((each < 1 ? 1 : each) * kTileK);
-    p.splits = (int)((pieces + (each < 1 ? 1 : each) - 1) / (each < 1 ? 1 : each));
-    if (p.splits < 1) p.splits = 1;
+    const int64_t each = pieces < 1 ? 1 : (pieces + splits - 1) / splits;
+    p.split_k = (int32_t)(each * kTileK);
+    p.splits = pieces < 1 ? 1 : (int)((pieces + each - 1) / each);
     return p;
 }
 
@@ -453,7 +482,7 @@ static int64_t product_bytes(const lda_product_rows* d)
 {
     if (d->rows == 0 || d->width == 0) return 0;
     const ProductPlan p = plan_product(d);
-    return p.splits == 1 ? 0 : (int64_t)p.splits * d->rows * d->classes * (int64_t)sizeof(int32_t);
+    return p.a_bytes + p.b_bytes + (p.splits == 1 ? 0 : (int64_t)p.splits * d->rows * d->classes * (int64_t)sizeof(int32_t));
 }
 
 template <class T>
@@ -463,20 +492,28 @@ static void launch_join(const ProductArgs& a, hipStream_t stream)
     product_join_kernel<T><<<(unsigned)(n < 8192 ? n : 8192), 256, 0, stream>>>(a);
 }
 
-template <class T, bool ALIGNED>
+static const int8_t* pack(const int8_t* from, int64_t& stride, int64_t rows, int32_t width, int8_t* to, hipStream_t stream)
+{
+    const int64_t pieces = ((int64_t)width + 15) / 16, blocks = (rows + 3) / 4;
+    product_pack_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, stream>>>(from, stride, rows, width, reinterpret_cast<i32x4*>(to));
+    stride = pieces * 16;
+    return to;
+}
+
+template <class T>
 static hipError_t launch_product(ProductArgs a, const ProductPlan& plan, hipStream_t stream)
 {
     a.splits = plan.splits;
     a.split_k = plan.split_k;
     const auto few = [&](auto ct) {
         const dim3 grid((unsigned)((a.N + 16 * ct() - 1) / (16 * ct())), (unsigned)a.splits);
-        product_few_kernel<T, ct(), ALIGNED><<<grid, 256, 0, stream>>>(a);
+        product_few_kernel<T, ct()><<<grid, 256, 0, stream>>>(a);
     };
-    const auto tile = [&](auto tm, auto tn, auto wm, auto wn) {
+    const auto tile = [&](auto tm, auto tn, auto wm, auto wn, auto aligned) {
         a.tiles_m = (int32_t)((a.M + tm() - 1) / tm());
         a.tiles_n = (a.N + tn() - 1) / tn();
         constexpr size_t lds = (tm() + tn()) * (2 * kTileK + sizeof(float));
-        const auto kernel = product_tile_kernel<T, tm(), tn(), wm(), wn(), ALIGNED>;
+        const auto kernel = product_tile_kernel<T, tm(), tn(), wm(), wn(), aligned()>;
         if (lds > 65536) {
             const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
             if (e != hipSuccess) return e;
@@ -497,8 +534,11 @@ static hipError_t launch_product(ProductArgs a, const ProductPlan& plan, hipStre
         const auto c128 = integral_constant<int, 128>{};
         const auto c64 = integral_constant<int, 64>{};
         const auto c2 = integral_constant<int, 2>{};
-        const hipError_t e = plan.kind == ProductKind::kTile256 ? tile(c256, c256, c2, c2)
-                             : plan.kind == ProductKind::kTile128 ? tile(c128, c128, c2, c2) : tile(c64, c128, c2, c2);
+        constexpr std::true_type yes{};
+        const hipError_t e = plan.kind == ProductKind::kTile256   ? tile(c256, c256, c2, c2, yes)
+                             : plan.kind == ProductKind::kTile128 ? tile(c128, c128, c2, c2, yes)
+                             : plan.aligned                       ? tile(c64, c128, c2, c2, yes)
+                                                                  : tile(c64, c128, c2, c2, std::false_type{});
         if (e != hipSuccess) return e;
     }
     if (a.splits > 1) launch_join<T>(a, stream);
@@ -543,19 +583,26 @@ try {
     a.b_scale = d->b_scale;
     a.out = out;
     a.out_stride = out_stride;
-    a.partial = static_cast<int32_t*>(d->workspace);
     const hipStream_t stream = static_cast<hipStream_t>(d->hip_stream);
-    // (places inside a tile are 32-bit)
-    const bool aligned = a.K % 16 == 0 && aligned_to(a.a, 16) && aligned_to(a.b, 16) && a.a_stride % 16 == 0 &&
-                         a.b_stride % 16 == 0 && a.a_stride >= 0 && a.b_stride >= 0 && a.a_stride < 1 << 22 && a.b_stride < 1 << 22;
+    const ProductPlan plan = plan_product(d);
+    int8_t* room = static_cast<int8_t*>(d->workspace);
+    if (a.K > 0 && plan.a_bytes > 0) {
+        a.a = pack(a.a, a.a_stride, a.M, a.K, room, stream);
+        room += plan.a_bytes;
+    }
+    if (a.K > 0 && plan.b_bytes > 0) {
+        a.b = pack(a.b, a.b_stride, a.N, a.K, room, stream);
+        room += plan.b_bytes;
+    }
+    a.partial = reinterpret_cast<int32_t*>(room);
+    if (plan.a_bytes > 0 || plan.b_bytes > 0) a.K = (a.K + 15) / 16 * 16;  // with the zeros
     const auto typed = [&](auto t) -> hipError_t {
         using T = decltype(t);
         if (a.K == 0) {
             launch_join<T>(a, stream);
             return hipGetLastError();
         }
-        const ProductPlan plan = plan_product(d);
-        return aligned ? launch_product<T, true>(a, plan, stream) : launch_product<T, false>(a, plan, stream);
+        return launch_product<T>(a, plan, stream);
     };
     const hipError_t e = d->out_type == LDA_F32 ? typed(float{}) : d->out_type == LDA_F16 ? typed(__half{}) : typed(__hip_bfloat16{});
     LDA_HIP(static_cast<lda_ctx*>(nullptr), e);
