@@ -171,6 +171,17 @@ __device__ __forceinline__ bool find_tile(const ProductArgs& p, int32_t block, i
     return true;
 }
 
+// Where a wave's 32 rows pass through LDS on their way out: as many classes of a row as the wave has, since memory's lines
+// that are written in parts cost time (rows of 141 043 16-bit numbers begin anywhere; 4096 x 1024 of them took 948 us by 64
+// classes at a time).  The waves that find no room in the piece that nobody reads any more have some behind it.
+template <int TM, int TN, int WM, int WN>
+struct ProductStage {
+    static constexpr int kBlocks = TM >= 128 ? TN / WN / 32 : 1;  // of 32 classes
+    static constexpr int kRow = kBlocks * 32 + 4, kBytes = 32 * kRow * 4;
+    static constexpr int kFit = (TM + TN) * kTileK / kBytes, kInside = kFit < WM * WN ? kFit : WM * WN;
+    static constexpr size_t kLds = (TM + TN) * (2 * kTileK + sizeof(float)) + (WM * WN - kInside) * kBytes;
+};
+
 // Tiles of TM rows times TN classes, one after the other, by a workgroup of WM x WN waves.  The pieces of both sides
 // are one stream over all of a workgroup's tiles: two pieces of the long axis are under way while one is multiplied, also
 // from one tile to the next, so that a tile's beginning waits for nothing and its stores drain behind the next one's
@@ -183,7 +194,8 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void product_tile_kernel(ProductAr
     constexpr int kThreads = WM * WN * 64, kMi = TM / WM / 32, kNi = TN / WN / 32, kSteps = kTileK / 32;
     constexpr int kRowsAtOnce = kThreads / 8, kLoadsA = TM / kRowsAtOnce, kLoadsB = TN / kRowsAtOnce, kLoads = kLoadsA + kLoadsB;
     static_assert(kRowsAtOnce % 16 == 0 && TM % kRowsAtOnce == 0 && TN % kRowsAtOnce == 0 && TM <= kThreads && TN <= kThreads, "shape");
-    extern __shared__ __align__(16) int8_t lds[];  // [2][TM + TN][kTileK], [TM + TN] scales
+    using Stage = ProductStage<TM, TN, WM, WN>;
+    extern __shared__ __align__(16) int8_t lds[];  // [2][TM + TN][kTileK], [TM + TN] scales, stages
     constexpr int kBuffer = (TM + TN) * kTileK;
     float* const scale_a = reinterpret_cast<float*>(lds + 2 * kBuffer);
     float* const scale_b = scale_a + TM;
@@ -315,10 +327,11 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void product_tile_kernel(ProductAr
         __syncthreads();
         const auto write = [&](auto* out, int64_t stride, auto before, auto behind) {
             using O = std::remove_pointer_t<decltype(out)>;
-            constexpr int kEach = 16 / (int)sizeof(O), kBlocks = kNi % 2 == 0 && WM * WN * 32 * 68 * 4 <= kBuffer ? 2 : 1;  // of 32 classes
-            constexpr int kWidth = kBlocks * 32, kRow = kWidth + 4, kPieces = kWidth / kEach, kRowsEach = kWave / kPieces;
-            static_assert(WM * WN * 32 * kRow * 4 <= kBuffer, "fits");
-            uint32_t* const stage = reinterpret_cast<uint32_t*>(lds + (buffer ^ 1) * kBuffer) + wave * 32 * kRow;
+            constexpr int kEach = 16 / (int)sizeof(O), kBlocks = Stage::kBlocks, kRow = Stage::kRow;
+            constexpr int kPieces = kBlocks * 32 / kEach, kRowsEach = kWave / kPieces;
+            uint32_t* const stage = reinterpret_cast<uint32_t*>(
+                wave < Stage::kInside ? lds + (buffer ^ 1) * kBuffer + wave * Stage::kBytes
+                                      : reinterpret_cast<int8_t*>(scale_b + TN) + (wave - Stage::kInside) * Stage::kBytes);
             const int32_t c = lane % kPieces * kEach, row1 = lane / kPieces;
             float sa[kMi];
 #pragma unroll
@@ -462,9 +475,10 @@ static ProductPlan plan_product(const lda_product_rows* d)
         p.kind = tiles(256, 256) >= 768 ? ProductKind::kTile256 : ProductKind::kTile128;
         groups = p.kind == ProductKind::kTile256 ? tiles(256, 256) : tiles(128, 128);
         const int64_t packed = ((int64_t)d->width + 15) / 16 * 16;
-        if (!a_fine) p.a_bytes = d->rows * packed;
-        if (!b_fine) p.b_bytes = d->classes * packed;
-        p.aligned = true;
+        // 516 x 7937 x 21153: 277 us as they lie, 245 packed first; 87 x 10049 x 14837: 76 and 105
+        if (d->rows > 128 && !a_fine) p.a_bytes = d->rows * packed;
+        if (d->rows > 128 && !b_fine) p.b_bytes = d->classes * packed;
+        if (d->rows > 128) p.aligned = true;
     }
     // a split has 1024 bytes of a row at least
     int64_t splits = groups >= 192 ? 1 : 256 / (groups < 1 ? 1 : groups);
@@ -512,7 +526,7 @@ static hipError_t launch_product(ProductArgs a, const ProductPlan& plan, hipStre
     const auto tile = [&](auto tm, auto tn, auto wm, auto wn, auto aligned) {
         a.tiles_m = (int32_t)((a.M + tm() - 1) / tm());
         a.tiles_n = (a.N + tn() - 1) / tn();
-        constexpr size_t lds = (tm() + tn()) * (2 * kTileK + sizeof(float));
+        constexpr size_t lds = ProductStage<tm(), tn(), wm(), wn()>::kLds;
         const auto kernel = product_tile_kernel<T, tm(), tn(), wm(), wn(), aligned()>;
         if (lds > 65536) {
             const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
@@ -536,7 +550,7 @@ static hipError_t launch_product(ProductArgs a, const ProductPlan& plan, hipStre
         const auto c2 = integral_constant<int, 2>{};
         constexpr std::true_type yes{};
         const hipError_t e = plan.kind == ProductKind::kTile256   ? tile(c256, c256, c2, c2, yes)
-                             : plan.kind == ProductKind::kTile128 ? tile(c128, c128, c2, c2, yes)
+                             : plan.kind == ProductKind::kTile128 ? (plan.aligned ? tile(c128, c128, c2, c2, yes) : tile(c128, c128, c2, c2, std::false_type{}))
                              : plan.aligned                       ? tile(c64, c128, c2, c2, yes)
                                                                   : tile(c64, c128, c2, c2, std::false_type{});
         if (e != hipSuccess) return e;
