@@ -427,7 +427,7 @@ int lda_doc_topics(lda_ctx* ctx, int64_t rows, const int32_t* docs, int32_t slot
 #define LDA_E4M3 1
 typedef struct lda_norm_rows {
     int64_t rows;            /* >= 0 */
-    int32_t width;           /* >= 1 */
+    int32_t width;           /* 1 .. 2^30 (more: LDA_ERR_UNSUPPORTED) */
     int32_t x_type;          /* of x, y and their gradients: LDA_F32, LDA_F16, LDA_BF16 */
     const void* x;           /* [rows][width], rows x_stride apart */
     int64_t x_stride;
@@ -477,7 +477,7 @@ int lda_norm_grad(const lda_norm_rows* rows, const lda_norm_gradients* gradients
  * The sum is exact.  Every integer may take all 256 values.
  */
 typedef struct lda_product_rows {
-    int64_t rows;            /* 0 .. 2^31 */
+    int64_t rows;            /* 0 .. 2^31, rows * classes up to 2^40 (more: LDA_ERR_UNSUPPORTED) */
     int32_t classes;         /* >= 1 */
     int32_t width;           /* 0 .. 131071: the sum has to fit 32 bits (more: LDA_ERR_UNSUPPORTED) */
     const void* a;           /* [rows][width], rows a_stride apart */

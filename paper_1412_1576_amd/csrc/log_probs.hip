@@ -414,7 +414,7 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
     } else {
         if (tid == 0) l.count = 0;
         take(first, yes, no);
-        if ((last - first + 2) * E > a.room) {  // (with the elements beside the chunks)
+        if ((int64_t)(last - first + 2) * E > a.room) {  // (with the elements beside the chunks)
             bound = raised(bound, least_of(first));
             bound_x = logit_of(bound + 1);
         } else {

@@ -430,6 +430,7 @@ static int check_norm(const lda_norm_rows* d, const char* call)
         if (r != 0) return fail(nullptr, LDA_ERR_ARG, "%s: reserved fields must be zero", call);
     if (d->reserved_word != 0) return fail(nullptr, LDA_ERR_ARG, "%s: reserved fields must be zero", call);
     if (d->rows < 0 || d->width < 1) return fail(nullptr, LDA_ERR_ARG, "%s: rows >= 0 and width >= 1 needed", call);
+    if (d->width > 1 << 30) return fail(nullptr, LDA_ERR_UNSUPPORTED, "%s: at most 2^30 numbers a row", call);
     if (!known_type(d->x_type) || !known_type(d->sum_type) || !known_type(d->weight_type))
         return fail(nullptr, LDA_ERR_ARG, "%s: unknown type", call);
     if (d->sum_type != d->x_type && d->sum_type != LDA_F32)

@@ -433,7 +433,8 @@ static int check_product(const lda_product_rows* d, const char* call)
     if (!known_type(d->out_type)) return fail(nullptr, LDA_ERR_ARG, "%s: unknown type", call);
     if (d->width > kMostWidth)
         return fail(nullptr, LDA_ERR_UNSUPPORTED, "%s: at most %d numbers a row (sums are 32-bit)", call, kMostWidth);
-    if (d->rows > (int64_t)1 << 31) return fail(nullptr, LDA_ERR_UNSUPPORTED, "%s: at most 2^31 rows", call);
+    if (d->rows > (int64_t)1 << 31 || d->rows * d->classes > (int64_t)1 << 40)
+        return fail(nullptr, LDA_ERR_UNSUPPORTED, "%s: at most 2^31 rows and 2^40 results", call);
     if (d->rows == 0) return LDA_OK;
     if (!d->a_scale || !d->b_scale || (d->width > 0 && (!d->a || !d->b)))
         return fail(nullptr, LDA_ERR_ARG, "%s: NULL pointer", call);

@@ -58,6 +58,13 @@ def test_norm_refuses(lib, kw):
         assert lib.lda_norm_grad_workspace(r) == lda.LDA_ERR_ARG
 
 
+def test_rows_that_are_too_long(lib):
+    assert lib.lda_norm(norm(width=(1 << 30) + 1, rows=1), OUT, 1 << 31, OUT, 1 << 31, OUT) == lda.LDA_ERR_UNSUPPORTED
+    assert lib.lda_norm_grad_workspace(norm(width=(1 << 30) + 1)) == lda.LDA_ERR_UNSUPPORTED
+    assert lib.lda_product_workspace(product(rows=1 << 31, classes=513)) == lda.LDA_ERR_UNSUPPORTED
+    assert "2^40" in message(lib)
+
+
 def test_norm_refuses_outputs(lib):
     r = norm()
     for args in ((None, 100, OUT, 100, OUT), (OUT + 1, 100, OUT, 100, OUT), (OUT, 99, OUT, 100, OUT),
