@@ -6,6 +6,7 @@
 // registers, and that is what bounds it.  Many rows (product_tile_kernel): tiles of both sides go through LDS, two
 // buffers, the fragments of a step read while the one before multiplies.  With too few tiles for the GPU the long axis
 // is split over workgroups and a second kernel adds up.
+#include <atomic>
 #include <type_traits>
 
 #include "rows.hpp"
@@ -530,8 +531,15 @@ static hipError_t launch_product(ProductArgs a, const ProductPlan& plan, hipStre
         constexpr size_t lds = ProductStage<tm(), tn(), wm(), wn()>::kLds;
         const auto kernel = product_tile_kernel<T, tm(), tn(), wm(), wn(), aligned()>;
         if (lds > 65536) {
-            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            static std::atomic<uint64_t> allowed{0};  // a bit a device: once is enough
+            int device = 0;
+            hipError_t e = hipGetDevice(&device);
             if (e != hipSuccess) return e;
+            if (device > 63 || !(allowed.load(std::memory_order_relaxed) >> device & 1)) {
+                e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+                if (e != hipSuccess) return e;
+                if (device <= 63) allowed.fetch_or((uint64_t)1 << device, std::memory_order_relaxed);
+            }
         }
         // as many workgroups as there is room for at once, a multiple of the XCDs
         const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n * a.splits, room = kCus * (int64_t)(kLdsOfCu / lds);

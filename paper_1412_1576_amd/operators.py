@@ -30,9 +30,8 @@ def _stream_of(device):
     return torch.cuda.current_stream(device).cuda_stream
 
 
-# What current_stream() and current_device() wrap, where torch has it: some 1 us less of a call
+# What current_stream() wraps, where torch has it: some 1 us less of a call
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream_of)
-_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _tensor(x, name, dims, types, device=None, shape=None, spread=False):
@@ -79,7 +78,7 @@ class _On:
         self.device = device
 
     def __enter__(self):
-        self.before = _current_device()
+        self.before = torch.cuda.current_device()
         if self.before != self.device:
             torch.cuda.set_device(self.device)
 

@@ -26,7 +26,7 @@ def least(t):
 
 
 def sums(width):
-    """Roundings of a sum over a row: a thread adds 16 numbers, or a 1024th of a wider row; 6 steps in a wave, 16
+    """Roundings of a sum over a row: a thread adds 16 numbers at most, or a 1024th of a wider row; 6 steps in a wave, 16
     waves."""
     return max(16, width / 1024 + 8) + 24
 
@@ -124,8 +124,8 @@ def check(ops, x, w=None, r=None, eps=1e-6, gradient=True, seed=0):
         close(by_leaf["r"], d, db + (d.abs() + db) * half(h.dtype) * 1.001 + least(h.dtype), "gradient of the residual")
     if w is not None:
         gw = (gd * norm).sum(0)
-        # rows of a group one by one, groups in four sums
-        gb = (gd * norm).abs().sum(0) * (rn + (n / 512 + min(n, 512) / 4 + 8) * U)
+        # rows of a group one by one (512 groups at least, or a row each), up to 2048 groups in 16 sums, these; a product
+        gb = (gd * norm).abs().sum(0) * (rn + (n / 512 + min(n, 2048) / 16 + 19) * U)
         close(by_leaf["w"], gw, gb + (gw.abs() + gb) * half(w.dtype) * 1.001 + least(w.dtype), "gradient of the weight")
 
 
