@@ -401,12 +401,23 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void product_tile_kernel(ProductAr
     }
 }
 
-// Rows that lie anywhere, side by side in pieces of 16 bytes, with zeros behind a row's end; a wave a row
-__global__ __launch_bounds__(256) void product_pack_kernel(const int8_t* from, int64_t stride, int64_t rows, int32_t width, i32x4* to)
+// Rows that lie anywhere, side by side in pieces of 16 bytes, with zeros behind a row's end; a wave a row.  Both
+// sides in one launch.
+struct PackArgs {
+    const int8_t* from[2];
+    int64_t stride[2], rows[2];
+    i32x4* to[2];
+    int32_t width;
+};
+__global__ __launch_bounds__(256) void product_pack_kernel(PackArgs p)
 {
-    const int32_t pieces = (width + 15) / 16;
+    const int side = (int)blockIdx.y;
+    const int8_t* const from = side ? p.from[1] : p.from[0];
+    const int64_t stride = side ? p.stride[1] : p.stride[0], rows = side ? p.rows[1] : p.rows[0];
+    i32x4* const to = side ? p.to[1] : p.to[0];
+    const int32_t pieces = (p.width + 15) / 16;
     for (int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave; row < rows; row += (int64_t)gridDim.x * 4)
-        for (int32_t i = threadIdx.x % kWave; i < pieces; i += kWave) to[row * pieces + i] = load16(from + row * stride, i * 16, width);
+        for (int32_t i = threadIdx.x % kWave; i < pieces; i += kWave) to[row * pieces + i] = load16(from + row * stride, i * 16, p.width);
 }
 
 // The splits' sums added up; none of a width of 0
@@ -508,12 +519,35 @@ static void launch_join(const ProductArgs& a, hipStream_t stream)
     product_join_kernel<T><<<(unsigned)(n < 8192 ? n : 8192), 256, 0, stream>>>(a);
 }
 
-static const int8_t* pack(const int8_t* from, int64_t& stride, int64_t rows, int32_t width, int8_t* to, hipStream_t stream)
+// Packs the sides that the plan wants packed to the workspace's beginning; returns what lies behind
+static int8_t* pack(ProductArgs& a, const ProductPlan& plan, int8_t* room, hipStream_t stream)
 {
-    const int64_t pieces = ((int64_t)width + 15) / 16, blocks = (rows + 3) / 4;
-    product_pack_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, stream>>>(from, stride, rows, width, reinterpret_cast<i32x4*>(to));
-    stride = pieces * 16;
-    return to;
+    if (plan.a_bytes == 0 && plan.b_bytes == 0) return room;
+    PackArgs p{};
+    const int64_t packed = ((int64_t)a.K + 15) / 16 * 16;
+    p.width = a.K;
+    if (plan.a_bytes > 0) {
+        p.from[0] = a.a;
+        p.stride[0] = a.a_stride;
+        p.rows[0] = a.M;
+        p.to[0] = reinterpret_cast<i32x4*>(room);
+        a.a = room;
+        a.a_stride = packed;
+        room += plan.a_bytes;
+    }
+    if (plan.b_bytes > 0) {
+        p.from[1] = a.b;
+        p.stride[1] = a.b_stride;
+        p.rows[1] = a.N;
+        p.to[1] = reinterpret_cast<i32x4*>(room);
+        a.b = room;
+        a.b_stride = packed;
+        room += plan.b_bytes;
+    }
+    a.K = (int32_t)packed;  // with the zeros
+    const int64_t blocks = ((p.rows[0] > p.rows[1] ? p.rows[0] : p.rows[1]) + 3) / 4;
+    product_pack_kernel<<<dim3((unsigned)(blocks < 16384 ? blocks : 16384), 2), 256, 0, stream>>>(p);
+    return room;
 }
 
 template <class T>
@@ -608,17 +642,7 @@ try {
     a.out_stride = out_stride;
     const hipStream_t stream = static_cast<hipStream_t>(d->hip_stream);
     const ProductPlan plan = plan_product(d);
-    int8_t* room = static_cast<int8_t*>(d->workspace);
-    if (a.K > 0 && plan.a_bytes > 0) {
-        a.a = pack(a.a, a.a_stride, a.M, a.K, room, stream);
-        room += plan.a_bytes;
-    }
-    if (a.K > 0 && plan.b_bytes > 0) {
-        a.b = pack(a.b, a.b_stride, a.N, a.K, room, stream);
-        room += plan.b_bytes;
-    }
-    a.partial = reinterpret_cast<int32_t*>(room);
-    if (plan.a_bytes > 0 || plan.b_bytes > 0) a.K = (a.K + 15) / 16 * 16;  // with the zeros
+    a.partial = reinterpret_cast<int32_t*>(a.K > 0 ? pack(a, plan, static_cast<int8_t*>(d->workspace), stream) : nullptr);
     const auto typed = [&](auto t) -> hipError_t {
         using T = decltype(t);
         if (a.K == 0) {
