@@ -316,7 +316,9 @@ __device__ __forceinline__ bool given_token(const LogProbArgs& a, int64_t row, f
 // A slice of a row a workgroup.  The first batch gives a bound from its chunks' largest; the others are read without
 // a barrier, each thread puts down what exceeds the bound, which rises each time as much again has been read: of a row in
 // no order some k more come each time.  Where more came than there is room for (a row that rises) they are gone through
-// again, the bound raised from batch to batch.
+// again, the bound raised from batch to batch.  Without alternatives bound by memory, 48 x 10^6 float32 30 us, or as much by
+// its 10 vector instructions an element, 2048 x 141043 bf16 152 us (3.8 TB/s); 2048 x 101636 fp16 with the top 64
+// 110 us (82 without), 64 x 141043 bf16 with the top 20 in 18 slices each 13.7.
 template <class T, bool TOP>
 __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
 {
@@ -478,7 +480,7 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
         for (int32_t i = tid; i < n; i += kScanBlock) a.lists[at * enough(a.k) + i] = l.best[i];
 }
 
-// A row's slices joined, a workgroup a row
+// A row's slices joined, a workgroup a row: 4 to 6 us of latency
 template <class T, bool TOP>
 __global__ __launch_bounds__(kScanBlock) void log_probs_join_kernel(LogProbArgs a)
 {
@@ -533,7 +535,7 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_join_kernel(LogProbArgs 
 }
 
 // A slice of a row's gradient a workgroup.  With e = 2^y it is e (A + B y), and 1 / T times the token's own weight
-// more at the token.
+// more at the token.  Bound by memory: 2048 x 141043 bf16 214 us, 5.4 TB/s of read and written bytes.
 template <class T>
 __global__ __launch_bounds__(kScanBlock) void log_probs_grad_kernel(LogProbGradArgs a)
 {
@@ -604,7 +606,9 @@ static int check_log_probs(const lda_log_prob_rows* d, const char* call)
     return LDA_OK;
 }
 
-// Slices of a row: enough workgroups to fill the GPU, and a batch of a workgroup's chunks at least
+// Slices of a row: enough workgroups to fill the GPU (1024; 2048 rows of 101636 take 103 us whole, 128 in two slices), each a
+// chunk of every thread at least, or whole batches (64 rows of 141043 with the top 20: 21 us by slices of two batches, 19
+// of one)
 struct Slices {
     int32_t count, chunks;
 };

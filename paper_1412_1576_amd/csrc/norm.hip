@@ -156,33 +156,54 @@ struct Levels {
         k = none ? 0.0f : 1.0f / scale;
     }
 };
+// Where a level in 32 bits lies so near the middle of two numbers of Q that its roundings (some 4 of 2^-24) could
+// take it to the wrong side: that middle.  false elsewhere.
 template <class Q>
-__device__ __forceinline__ uint2 levels_of(const float (&y)[8], const Levels& l);
+__device__ __forceinline__ bool near_middle(float level, float& middle);
 template <>
-__device__ __forceinline__ uint2 levels_of<int8_t>(const float (&y)[8], const Levels& l)
+__device__ __forceinline__ bool near_middle<int8_t>(float level, float& middle)
 {
-    uint32_t w[2] = {0, 0};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int32_t q = (int32_t)rintf(fminf(fmaxf(y[e] * l.k, -127.0f), 127.0f));
-        w[e / 4] |= ((uint32_t)q & 0xFFu) << (e % 4 * 8);
-    }
-    return make_uint2(w[0], w[1]);
+    middle = floorf(level) + 0.5f;
+    return fabsf(level - middle) <= 0x1p-20f * fabsf(middle);
 }
 struct E4m3 {
     uint8_t bits;
 };
 template <>
-__device__ __forceinline__ uint2 levels_of<E4m3>(const float (&y)[8], const Levels& l)
+__device__ __forceinline__ bool near_middle<E4m3>(float level, float& middle)  // 3 bits behind the leading one, 2^-9 at least
+{
+    if (fabsf(level) < 0x1p-6f) {
+        middle = (floorf(level * 0x1p9f) + 0.5f) * 0x1p-9f;
+        return fabsf(level - middle) <= 0x1p-20f * fabsf(middle);
+    }
+    const uint32_t bits = __float_as_uint(level);
+    middle = __uint_as_float((bits & 0xFFF00000u) | 0x80000u);
+    return (bits & 0xFFFFFu) - (0x80000u - 16u) <= 32u;
+}
+template <class Q>
+__device__ __forceinline__ uint2 pack_levels(const float (&v)[8]);
+template <>
+__device__ __forceinline__ uint2 pack_levels<int8_t>(const float (&v)[8])
+{
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const int32_t q = (int32_t)rintf(fminf(fmaxf(v[e], -127.0f), 127.0f));
+        w[e / 4] |= ((uint32_t)q & 0xFFu) << (e % 4 * 8);
+    }
+    return make_uint2(w[0], w[1]);
+}
+template <>
+__device__ __forceinline__ uint2 pack_levels<E4m3>(const float (&v)[8])
 {
     int w[2] = {0, 0};
 #pragma unroll
     for (int e = 0; e < 8; e += 4) {
-        float v[4];
+        float c[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = fminf(fmaxf(y[e + i] * l.k, -448.0f), 448.0f);
-        w[e / 4] = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], w[e / 4], false);
-        w[e / 4] = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w[e / 4], true);
+        for (int i = 0; i < 4; ++i) c[i] = fminf(fmaxf(v[e + i], -448.0f), 448.0f);
+        w[e / 4] = __builtin_amdgcn_cvt_pk_fp8_f32(c[0], c[1], w[e / 4], false);
+        w[e / 4] = __builtin_amdgcn_cvt_pk_fp8_f32(c[2], c[3], w[e / 4], true);
     }
     return make_uint2((uint32_t)w[0], (uint32_t)w[1]);
 }
@@ -190,10 +211,8 @@ template <class Q>
 constexpr float most_of() { return std::is_same<Q, E4m3>::value ? 448.0f : 127.0f; }
 
 template <class Q>
-__device__ __forceinline__ void store_levels(Q* row, int32_t i, int32_t H, const float (&y)[8], const Levels& l)
+__device__ __forceinline__ void store_levels(Q* row, int32_t i, int32_t H, uint2 w)
 {
-    uint2 w = levels_of<Q>(y, l);
-    if (l.none) w = make_uint2(0, 0);
     if (i + 8 <= H) {
         __builtin_memcpy(row + i, &w, 8);
     } else {
@@ -239,13 +258,13 @@ __global__ __launch_bounds__(BLOCK) void norm_kernel(NormArgs a)
         if (kWide) {
             for (int32_t i = tid * kNormChunk; i < H; i += kStep) {
                 load(i, h[0]);
-                f(i, h[0]);
+                f(i, 0);
             }
         } else {
 #pragma unroll
             for (int j = 0; j < CHUNKS; ++j) {
                 const int32_t i = j * kStep + tid * kNormChunk;
-                if (i < H) f(i, h[j]);
+                if (i < H) f(i, j);
             }
         }
     };
@@ -257,63 +276,84 @@ __global__ __launch_bounds__(BLOCK) void norm_kernel(NormArgs a)
         }
     }
     float squares = 0.0f;
-    each([&](int32_t i, const float (&v)[8]) {
-        if (r) store_some(sum, i, H, v);
+    each([&](int32_t i, int j) {
+        if (r) store_some(sum, i, H, h[j]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) squares = __builtin_fmaf(v[e], v[e], squares);
+        for (int e = 0; e < 8; ++e) squares = __builtin_fmaf(h[j][e], h[j][e], squares);
     });
     squares = block_sum<BLOCK>(squares, part);
     float first = 1.0f;
     // rare: squares left 32 bits and eps does not hide it, or the row is 0
     if (!(squares + (float)H * a.eps >= kLeastSquares && squares <= kMostSquares)) {
         uint32_t top = 0;
-        each([&](int32_t, const float (&v)[8]) {
+        each([&](int32_t, int j) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[e]));
+            for (int e = 0; e < 8; ++e) top = max(top, magnitude(h[j][e]));
         });
         first = power_for(max(block_top<BLOCK>(top, part_top), __float_as_uint(sqrtf(a.eps))));
         squares = 0.0f;
-        each([&](int32_t, const float (&v)[8]) {
+        each([&](int32_t, int j) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) squares = __builtin_fmaf(v[e] * first, v[e] * first, squares);
+            for (int e = 0; e < 8; ++e) squares = __builtin_fmaf(h[j][e] * first, h[j][e] * first, squares);
         });
         squares = block_sum<BLOCK>(squares, part);
     }
     const NormFactor f = factor_of(squares, first, H, a.eps);
     if (a.stats && tid == 0) *reinterpret_cast<float2*>(a.stats + row * kNormStats) = make_float2(f.first, f.second);
-    const auto normed = [&](int32_t i, const float (&v)[8], float (&y)[8]) {
-        load_weight<T>(a.weight, a.weight_type, i, H, y);
+    float y[kHeld][8];
+    const auto normed = [&](int32_t i, int j) {
+        load_weight<T>(a.weight, a.weight_type, i, H, y[j]);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = f.of(v[e]) * y[e];
+        for (int e = 0; e < 8; ++e) y[j][e] = f.of(h[j][e]) * y[j][e];
     };
     if constexpr (!k8) {
-        each([&](int32_t i, const float (&v)[8]) {
-            float y[8];
-            normed(i, v, y);
-            store_some(out, i, H, y);
+        each([&](int32_t i, int j) {
+            normed(i, j);
+            store_some(out, i, H, y[j]);
         });
     } else {
+        // A level is h w over the largest |h w| of the row, times Q's largest: the root cancels.  It is taken in 32 bits,
+        // and again in 64, from h and w themselves, where it lies so near the middle of two numbers that roundings
+        // would decide: of rows in 16 bits many lie right there.
+        __shared__ unsigned long long largest;  // the bits of the largest |h w|, in 64
         uint32_t top = 0;
-        each([&](int32_t i, float (&v)[8]) {
-            float y[8];
-            normed(i, v, y);
+        each([&](int32_t i, int j) {
+            normed(i, j);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, i + e < H ? magnitude(y[e]) : 0u);
-            if (!kWide) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = y[e];
-            }
+            for (int e = 0; e < 8; ++e) top = max(top, i + e < H ? magnitude(y[j][e]) : 0u);
         });
-        const Levels l(block_top<BLOCK>(top, part_top), most_of<Q>());
+        if (tid == 0) largest = 0;
+        top = block_top<BLOCK>(top, part_top);
+        const Levels l(top, most_of<Q>());
         if (tid == 0) a.scale[row] = l.scale;
-        each([&](int32_t i, const float (&v)[8]) {
-            if (!kWide) {
-                store_levels(out, i, H, v, l);
-            } else {
-                float y[8];
-                normed(i, v, y);
-                store_levels(out, i, H, y, l);
+        if (BLOCK == kWave) wave_lds_order();
+        const auto exact = [&](int32_t i, float v) {
+            const double w = !a.weight ? 1.0 : (double)element_at(a.weight, a.weight_type, i);
+            return (double)v * w;
+        };
+        each([&](int32_t i, int j) {
+            if (kWide) normed(i, j);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (!l.none && i + e < H && magnitude(y[j][e]) + 4 >= top)
+                    atomicMax(&largest, __builtin_bit_cast(unsigned long long, fabs(exact(i + e, h[j][e]))));
+        });
+        if (BLOCK == kWave) wave_lds_order();
+        else __syncthreads();
+        const double most = __builtin_bit_cast(double, largest);
+        each([&](int32_t i, int j) {
+            if (kWide) normed(i, j);
+            float level[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                level[e] = y[j][e] * l.k;
+                float middle;
+                if (!near_middle<Q>(level[e], middle) || l.none || i + e >= H) continue;
+                const double to = exact(i + e, h[j][e]) * ((double)most_of<Q>() / most), off = to - (double)middle;
+                // the neighbour of the middle on the level's side, which rounds as the level does
+                level[e] = fabs(off) <= 0x1p-48 * fabs(to) ? middle : middle + (off > 0.0 ? 1.0f : -1.0f) * 0x1p-20f * fabsf(middle);
             }
+            store_levels(out, i, H, l.none ? make_uint2(0, 0) : pack_levels<Q>(level));
         });
     }
 }

@@ -69,7 +69,8 @@ __device__ __forceinline__ float scaled(float v, float scale)
 __device__ __forceinline__ float scaled(int32_t sum, float sa, float sb) { return scaled((float)sum * sa, sb); }
 
 // Up to 16 rows times 16 CT classes a workgroup; its waves take the row's steps in turn and join in LDS.  Rows lie
-// anywhere: the hardware's loads take any address.
+// anywhere: the hardware's loads take any address.  1 x 4096 x 141043: 108 us, 5.3 TB/s of weights; 1 x 1000 x 1024 is
+// the host's call.
 template <class T, int CT>
 __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs p)
 {
@@ -188,7 +189,8 @@ struct ProductStage {
 // from one tile to the next, so that a tile's beginning waits for nothing and its stores drain behind the next one's
 // products.  LDS has rows of kTileK bytes, their 16-byte pieces in an order that changes every two rows, so that 16 rows'
 // reads of a column of pieces meet all banks (with an order that changed every row a third of LDS's cycles were
-// conflicts).
+// conflicts).  4096 x 4096 x 141043 by 256 x 256: 2.15 ms, 2.2 Pop/s, the matrix units busy 63 % of the cycles at the 1.47 GHz
+// that the card's power leaves; 48 x 5120 x 101636 by 64 x 128: 113 us, 4.7 TB/s of weights.
 template <class T, int TM, int TN, int WM, int WN, bool ALIGNED>
 __global__ __launch_bounds__(WM * WN * 64, 1) void product_tile_kernel(ProductArgs p)
 {
@@ -485,6 +487,7 @@ static ProductPlan plan_product(const lda_product_rows* d)
         p.kind = ProductKind::kTile64;
         groups = tiles(64, 128);
     } else {
+        // 4096 x 4096 x 32768 (2048 tiles): 496 us by 256 x 256, 682 by 128 x 128; 2048 x 4096 x 10000 (320): 104 and 92
         p.kind = tiles(256, 256) >= 768 ? ProductKind::kTile256 : ProductKind::kTile128;
         groups = p.kind == ProductKind::kTile256 ? tiles(256, 256) : tiles(128, 128);
         const int64_t packed = ((int64_t)d->width + 15) / 16 * 16;

@@ -212,6 +212,41 @@ def test_ties_go_to_even(ops):
     assert q[0].float().tolist() == [float(i) for i in want[:1] + want[1:]]
 
 
+@pytest.mark.parametrize("value", [3.0, 0.7, 1e-4, 2.0 ** 70, 2.0 ** -70])
+def test_ties_in_rows_of_any_root(ops, value):
+    """All of a row's numbers are alike and the weights have the levels: the root leaves 32 bits, the ties remain."""
+    w = torch.arange(-127, 128, device="cuda").float() / 2.0
+    w = torch.cat([w, torch.tensor([127.0], device="cuda")])
+    for x in (torch.full((3, 256), value, device="cuda"), torch.full((3, 256), value, device="cuda").bfloat16()):
+        q, scale = ops.rms_norm_8bit(x, w, eps=1e-12)
+        assert torch.equal(q.float(), torch.round(w).expand(3, 256))
+    v = torch.cat([torch.arange(16, 33, device="cuda").float(), torch.tensor([448.0], device="cuda")])
+    q, scale = ops.rms_norm_8bit(torch.full((2, 18), value, device="cuda"), v, eps=0.0, dtype=torch.float8_e4m3fn)
+    want = [16, 16, 18, 20, 20, 20, 22, 24, 24, 24, 26, 28, 28, 28, 30, 32, 32, 448]
+    assert q[0].float().tolist() == [float(i) for i in want]
+
+
+@pytest.mark.parametrize("width", [100, 1000, 5000, 20_000])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_levels_are_those_of_64_bits(ops, width, dtype):
+    """A level is h w / max |h w| times the type's largest: 64 bits are off by some 2^-51 of it, so that numbers further from
+    the middle of two levels than 2^-40 go to one side."""
+    n = 400
+    x, r = make(n, width, TYPES[dtype], 1), make(n, width, TYPES[dtype], 2, kind=torch.float32)
+    for w in (None, make(1, width, TYPES[dtype], 3)[0]):
+        for kind, most in ((torch.int8, 127.0), (torch.float8_e4m3fn, 448.0)):
+            q, scale, h = ops.rms_norm_8bit(x, w, residual=r, dtype=kind)
+            p = h.double() if w is None else h.double() * w.double()
+            level = p / p.abs().amax(1, keepdim=True) * most
+            if kind == torch.int8:
+                step = torch.ones_like(level)
+            else:
+                step = torch.exp2(torch.floor(torch.log2(level.abs().clamp(min=2.0 ** -6))) - 3)
+            places = level / step
+            clear = (places - torch.floor(places) - 0.5).abs() > 2.0 ** -40
+            assert torch.equal(q.double()[clear], (torch.round(places) * step)[clear])
+
+
 def test_gradient_against_differences(ops):
     """(f(x + h d) - f(x - h d)) / 2h of f = sum(gy y) + sum(gh sum), rows of 60 with a mean square near 1, d of
     length 1.  n is smooth in x at the scale of the row's length, 7.7: a third derivative of gy y along d is at most
