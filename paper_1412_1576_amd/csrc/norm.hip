@@ -180,6 +180,22 @@ __device__ __forceinline__ bool near_middle<E4m3>(float level, float& middle)  /
     middle = __uint_as_float((bits & 0xFFF00000u) | 0x80000u);
     return (bits & 0xFFFFFu) - (0x80000u - 16u) <= 32u;
 }
+// Whether any of them may be, by fewer instructions
+template <class Q>
+__device__ __forceinline__ bool any_near_middle(const float (&v)[8])
+{
+    bool some = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if (std::is_same<Q, int8_t>::value) some = some || fabsf(fabsf(v[e] - rintf(v[e])) - 0.5f) <= 0x1p-12f;
+        else some = some || (__float_as_uint(v[e]) << 12) + (0x80000000u + (16u << 12)) <= 32u << 12;
+    }
+    if (std::is_same<Q, int8_t>::value) return some;
+    float least = fabsf(v[0]);
+#pragma unroll
+    for (int e = 1; e < 8; ++e) least = fminf(least, fabsf(v[e]));
+    return some || least < 0x1p-6f;
+}
 template <class Q>
 __device__ __forceinline__ uint2 pack_levels(const float (&v)[8]);
 template <>
@@ -300,16 +316,16 @@ __global__ __launch_bounds__(BLOCK) void norm_kernel(NormArgs a)
     }
     const NormFactor f = factor_of(squares, first, H, a.eps);
     if (a.stats && tid == 0) *reinterpret_cast<float2*>(a.stats + row * kNormStats) = make_float2(f.first, f.second);
-    float y[kHeld][8];
-    const auto normed = [&](int32_t i, int j) {
-        load_weight<T>(a.weight, a.weight_type, i, H, y[j]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[j][e] = f.of(h[j][e]) * y[j][e];
-    };
+    float w[kHeld][8];
+    const auto weigh = [&](int32_t i, int j) { load_weight<T>(a.weight, a.weight_type, i, H, w[j]); };
+    const auto normed = [&](int j, int e) { return f.of(h[j][e]) * w[j][e]; };
     if constexpr (!k8) {
         each([&](int32_t i, int j) {
-            normed(i, j);
-            store_some(out, i, H, y[j]);
+            weigh(i, j);
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = normed(j, e);
+            store_some(out, i, H, y);
         });
     } else {
         // A level is h w over the largest |h w| of the row, times Q's largest: the root cancels.  It is taken in 32 bits,
@@ -317,41 +333,55 @@ __global__ __launch_bounds__(BLOCK) void norm_kernel(NormArgs a)
         // would decide: of rows in 16 bits many lie right there.
         __shared__ unsigned long long largest;  // the bits of the largest |h w|, in 64
         uint32_t top = 0;
-        each([&](int32_t i, int j) {
-            normed(i, j);
+        const auto top_of = [&](int32_t i, int j) {
+            uint32_t t = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, i + e < H ? magnitude(y[j][e]) : 0u);
+            for (int e = 0; e < 8; ++e) t = max(t, i + e < H ? magnitude(normed(j, e)) : 0u);
+            return t;
+        };
+        uint32_t tops[kHeld];
+        each([&](int32_t i, int j) {
+            weigh(i, j);
+            tops[j] = top_of(i, j);
+            top = max(top, tops[j]);
         });
         if (tid == 0) largest = 0;
         top = block_top<BLOCK>(top, part_top);
         const Levels l(top, most_of<Q>());
         if (tid == 0) a.scale[row] = l.scale;
         if (BLOCK == kWave) wave_lds_order();
-        const auto exact = [&](int32_t i, float v) {
-            const double w = !a.weight ? 1.0 : (double)element_at(a.weight, a.weight_type, i);
-            return (double)v * w;
-        };
+        const auto exact = [&](int j, int e) { return (double)h[j][e] * (double)w[j][e]; };
         each([&](int32_t i, int j) {
-            if (kWide) normed(i, j);
+            if (kWide) {
+                weigh(i, j);
+                tops[j] = top_of(i, j);
+            }
+            if (l.none || tops[j] + 4 < top) return;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (!l.none && i + e < H && magnitude(y[j][e]) + 4 >= top)
-                    atomicMax(&largest, __builtin_bit_cast(unsigned long long, fabs(exact(i + e, h[j][e]))));
+                if (i + e < H && magnitude(normed(j, e)) + 4 >= top)
+                    atomicMax(&largest, __builtin_bit_cast(unsigned long long, fabs(exact(j, e))));
         });
         if (BLOCK == kWave) wave_lds_order();
         else __syncthreads();
         const double most = __builtin_bit_cast(double, largest);
         each([&](int32_t i, int j) {
-            if (kWide) normed(i, j);
+            if (kWide) weigh(i, j);
             float level[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                level[e] = y[j][e] * l.k;
-                float middle;
-                if (!near_middle<Q>(level[e], middle) || l.none || i + e >= H) continue;
-                const double to = exact(i + e, h[j][e]) * ((double)most_of<Q>() / most), off = to - (double)middle;
-                // the neighbour of the middle on the level's side, which rounds as the level does
-                level[e] = fabs(off) <= 0x1p-48 * fabs(to) ? middle : middle + (off > 0.0 ? 1.0f : -1.0f) * 0x1p-20f * fabsf(middle);
+            for (int e = 0; e < 8; ++e) level[e] = normed(j, e) * l.k;
+            if (!l.none && any_near_middle<Q>(level)) {
+                double inverse = __builtin_amdgcn_rcp(most);  // a quotient in 64 bits takes three times as long
+                inverse = __builtin_fma(__builtin_fma(-most, inverse, 1.0), inverse, inverse);
+                inverse = __builtin_fma(__builtin_fma(-most, inverse, 1.0), inverse, inverse);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float middle;
+                    if (!near_middle<Q>(level[e], middle) || i + e >= H) continue;
+                    const double to = exact(j, e) * (inverse * (double)most_of<Q>()), off = to - (double)middle;
+                    // the neighbour of the middle on the level's side, which rounds as the level does
+                    level[e] = fabs(off) <= 0x1p-48 * fabs(to) ? middle : middle + (off > 0.0 ? 1.0f : -1.0f) * 0x1p-20f * fabsf(middle);
+                }
             }
             store_levels(out, i, H, l.none ? make_uint2(0, 0) : pack_levels<Q>(level));
         });
