@@ -241,9 +241,9 @@ __device__ __forceinline__ void store_levels(Q* row, int32_t i, int32_t H, uint2
 }
 
 // T: of x and y; S: of the residual and the sum; Q: T, or 8 bits.  Bound by memory: 16384 x 8192 bf16 with a bf16
-// residual to e4m3 take 164 us, 5.7 TB/s of read and written bytes (a copy of 1 GiB: 5.15); 8192 x 4096 bf16 with a float32
-// residual 83 us.  One row of 4096: 2.5 us, the latency of its loads and of two reductions.  A row's elements stay
-// in registers, 16 at most, between the reductions.
+// residual to e4m3 take 185 us, 5.1 TB/s of read and written bytes (a copy of 1 GiB: 5.15), 165 with levels rounded from 32
+// bits alone; 8192 x 4096 bf16 with a float32 residual 83 us.  One row of 4096: 2.5 us, the latency of its loads and of a
+// reduction.  A row's elements and weights stay in registers, 16 of each at most, between the reductions.
 template <class T, class S, class Q, int BLOCK, int CHUNKS>
 __global__ __launch_bounds__(BLOCK) void norm_kernel(NormArgs a)
 {

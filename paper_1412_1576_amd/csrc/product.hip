@@ -496,9 +496,11 @@ static ProductPlan plan_product(const lda_product_rows* d)
         if (d->rows > 128 && !b_fine) p.b_bytes = d->classes * packed;
         if (d->rows > 128) p.aligned = true;
     }
-    // a split has 1024 bytes of a row at least
+    // A split's second kernel takes 3 to 4 us, so that a split has some bytes of a row at least.  1 x 16384 x 1000: 13.7 us
+    // whole, 16.4 in 2 splits; 1 x 131008 x 1000: 136, and 45 in 16; 300 x 2048 x 2000: 13 whole, 15.6 in 2; 300 x 8192 x 1000: 34
+    // and 19 in 4
     int64_t splits = groups >= 192 ? 1 : 256 / (groups < 1 ? 1 : groups);
-    const int64_t most = d->width / 1024;
+    const int64_t most = d->width / (p.kind == ProductKind::kFew ? 16384 : 2048);
     if (splits > most) splits = most;
     if (splits < 1) splits = 1;
     const int64_t pieces = ((int64_t)d->width + kTileK - 1) / kTileK;
