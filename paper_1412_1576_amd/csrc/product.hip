@@ -488,7 +488,8 @@ static ProductPlan plan_product(const lda_product_rows* d)
         groups = tiles(64, 128);
     } else {
         // 4096 x 4096 x 32768 (2048 tiles): 496 us by 256 x 256, 682 by 128 x 128; 2048 x 4096 x 10000 (320): 104 and 92
-        p.kind = tiles(256, 256) >= 768 ? ProductKind::kTile256 : ProductKind::kTile128;
+        // (up to 128 rows nothing is packed, and the larger tile has buffers alone)
+        p.kind = tiles(256, 256) >= 768 && (p.aligned || d->rows > 128) ? ProductKind::kTile256 : ProductKind::kTile128;
         groups = p.kind == ProductKind::kTile256 ? tiles(256, 256) : tiles(128, 128);
         const int64_t packed = ((int64_t)d->width + 15) / 16 * 16;
         // 516 x 7937 x 21153: 277 us as they lie, 245 packed first; 87 x 10049 x 14837: 76 and 105
@@ -597,6 +598,7 @@ static hipError_t launch_product(ProductArgs a, const ProductPlan& plan, hipStre
         const auto c64 = integral_constant<int, 64>{};
         const auto c2 = integral_constant<int, 2>{};
         constexpr std::true_type yes{};
+        if (plan.kind == ProductKind::kTile256 && !plan.aligned) return hipErrorInvalidValue;  // no plan has this
         const hipError_t e = plan.kind == ProductKind::kTile256   ? tile(c256, c256, c2, c2, yes)
                              : plan.kind == ProductKind::kTile128 ? (plan.aligned ? tile(c128, c128, c2, c2, yes) : tile(c128, c128, c2, c2, std::false_type{}))
                              : plan.aligned                       ? tile(c64, c128, c2, c2, yes)

@@ -80,6 +80,24 @@ def test_rows_that_start_anywhere(ops, k, pad, offset):
     check(ops, integers(1, k, 1).expand(90, k), integers(300, k, 2))
 
 
+@pytest.mark.parametrize("m", [65, 100, 128])
+@pytest.mark.parametrize("k,pad,offset", [(77, 0, 0), (1000, 0, 0), (1008, 1, 0), (1008, 0, 1), (1008, 16, 0)])
+def test_many_classes_of_rows_that_start_anywhere(ops, m, k, pad, offset):
+    """As many classes as make tiles of 256 x 256, which read whole 16-byte pieces, and too few rows to be packed."""
+    a, b = integers(m, k, 1), integers(200_003, k, 2, pad, offset)
+    check(ops, a, b)
+    if pad or offset:
+        check(ops, integers(m, k, 1, pad, offset), integers(200_003, k, 2))
+
+
+def test_rows_far_apart_and_many_classes(ops):
+    """Rows so far apart that a place inside a tile leaves 32 bits."""
+    store = torch.zeros(65, 1 << 24, dtype=torch.int8, device="cuda")
+    a = store[:, 16:80]
+    a.copy_(integers(65, 64, 1))
+    check(ops, a, integers(200_003, 64, 2))
+
+
 def test_the_largest_sums(ops):
     """Widths up to the largest with nothing but -128: the sum is 2^31 - 2^14."""
     for m in (1, 70):
