@@ -439,6 +439,7 @@ __global__ __launch_bounds__(kScanBlock) void log_probs_kernel(LogProbArgs a)
                     bound = raised(bound, cut<kScanBlock>(list, n, a.k, l));
                     bound_x = logit_of(bound + 1);
                     n = l.count;
+                    __syncthreads();  // every wave has read it before a fast one puts the next on the list
                 }
                 kept = n;
                 safe = at;

@@ -186,6 +186,27 @@ def test_orders_and_ties(ops, v, top, n):
     check(ops, x.flip(1).contiguous(), t, top=top, gradient=False)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [1, 8, 100, 256])
+def test_rows_that_flood_the_list_behind_a_cut(ops, top, dtype):
+    """Whole rows by a workgroup each.  The second batch brings enough for the list to be cut, the next two more than
+    there is room for, so that they are gone through again from what the cut had left."""
+    n, batch = 1100, 1024 * (4 if dtype == "f32" else 8)
+    v = 8 * batch + 77
+    g = torch.Generator(device="cuda").manual_seed(top)
+    x = torch.rand(n, v, generator=g, device="cuda")
+    k = 3 * (top + max(8, top // 4))
+    for i in range(0, n, 7):  # the same places in seven rows each
+        at = batch + torch.randperm(batch, generator=g, device="cuda")[:k]
+        x[i:i + 7, at] += 2.0
+        at = 2 * batch + torch.randperm(2 * batch, generator=g, device="cuda")[:4000]
+        x[i:i + 7, at] += 4.0
+        at = 4 * batch + torch.randperm(4 * batch, generator=g, device="cuda")[:top // 2]
+        x[i:i + 7, at] += 8.0
+    t = torch.randint(0, v, (n,), generator=g, device="cuda")
+    check(ops, x.to(TYPES[dtype]), t, top=top, gradient=False)
+
+
 @pytest.mark.parametrize("v", [40, 3000, 60_003])
 @pytest.mark.parametrize("times", [1, 120])
 def test_masked_and_odd_logits(ops, v, times):
