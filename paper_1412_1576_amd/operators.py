@@ -17,6 +17,7 @@ refusals of the library LdaError.
 from __future__ import annotations
 
 import torch
+from torch.autograd import forward_ad
 
 from . import lda
 from .lda import LDA_OK, LdaError
@@ -305,10 +306,13 @@ def doc_topics(sampler, slots, docs=None):
 
 
 def _wants_gradient(*tensors):
+    """Whether a derivative is asked for: of leaves, or along tangents of forward mode, which torch.no_grad() leaves on."""
     for t in tensors:
-        if t is not None and getattr(t, "requires_grad", False):
-            return torch.is_grad_enabled()
-    return False
+        if t is not None and getattr(t, "requires_grad", False) and torch.is_grad_enabled():
+            return True
+    if getattr(forward_ad, "_current_level", 0) < 0:  # no tensor has a tangent
+        return False
+    return any(isinstance(t, torch.Tensor) and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
 
 
 def _check_norm(x, weight, residual):
@@ -411,9 +415,9 @@ def rms_norm(x, weight=None, *, residual=None, eps=1e-6):
 
     x [rows, width] float32, float16 or bfloat16; weight [width] and residual [rows, width] of x's type or
     float32.  The sum has the residual's type and y is the norm of the sum as it is written, in x's type.
-    Differentiable in x, weight and residual; sums are 32-bit.  Rows of a tensor may lie any distance
-    apart; within a row elements are adjacent.  A backward pass captured into a graph must find no eager graph of
-    the same leaves alive.
+    Differentiable in x, weight and residual (backward: tangents of forward mode raise NotImplementedError); sums are
+    32-bit.  Rows of a tensor may lie any distance apart; within a row elements are adjacent.  A backward pass captured
+    into a graph must find no eager graph of the same leaves alive.
     """
     eps = float(eps)
     if _wants_gradient(x, weight, residual):
@@ -431,7 +435,7 @@ def rms_norm_8bit(x, weight=None, *, residual=None, eps=1e-6, dtype=torch.int8):
 
     The scale brings the largest |y| of a row to 127 or 448; q is y / scale, rounded to nearest, ties to even.  A
     row of zeros has scale 0, a row with a NaN or an infinity scale NaN and q 0.  No gradient: tensors that require one are
-    refused outside torch.no_grad().
+    refused outside torch.no_grad(), tensors with a tangent of forward mode everywhere.
     """
     if dtype not in _LEVELS:
         raise ValueError("dtype must be torch.int8 or torch.float8_e4m3fn, not %s" % dtype)
@@ -456,7 +460,7 @@ def int8_matmul(a, a_scale, b, b_scale, *, dtype=torch.bfloat16):
     a [rows, width] and b [classes, width] int8, as rms_norm_8bit gives a and as weights are kept; a_scale float32
     [rows], b_scale float32 [classes].  The sums are exact (width up to 131071), scaled in 32 bits and rounded once.
     Rows of a and b may lie any distance apart (faster where width and distances are multiples of 16).  No
-    gradient: scales that require one are refused outside torch.no_grad().
+    gradient: scales that require one are refused outside torch.no_grad(), scales with a tangent of forward mode everywhere.
     """
     if dtype not in _FLOATS:
         raise ValueError("dtype must be one of %s, not %s" % (", ".join(map(str, _FLOATS)), dtype))
@@ -555,7 +559,8 @@ def token_log_probs(logits, tokens, *, temperature=1.0, top=0):
     under softmax(logits / temperature), 0 where the token is outside [0, classes) (padding).  top: so many of the
     likeliest classes and their log probabilities, the likeliest first, equal ones by class; slots without a class of
     probability have id -1 and -infinity.  At temperature 1 they are a teacher for distill_loss, with log_norm zeros.
-    Differentiable in logits through log_prob and entropy (not through the alternatives); rows whose gradients of both
+    Differentiable in logits through log_prob and entropy (not through the alternatives; backward: a tangent of forward
+    mode raises NotImplementedError); rows whose gradients of both
     are 0 are left out, whatever their logits hold.  A row without any logit above -infinity has log_prob -infinity, entropy 0 and
     gradient 0.  Rows of a tensor may lie any distance apart; within a row elements are adjacent.  A
     backward pass captured into a graph must find no eager graph of the same leaves alive.

@@ -327,6 +327,16 @@ def test_the_binding_refuses(ops):
     assert none.grad.shape == (0, 100)
 
 
+def test_tangents_are_refused(ops):
+    from torch.autograd import forward_ad
+    x, t = make(4, 100, torch.float32, seed=10)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(x, torch.ones_like(x))
+        for on in (True, False):
+            with torch.set_grad_enabled(on), pytest.raises(NotImplementedError):
+                ops.token_log_probs(dual, t, top=3)
+
+
 @pytest.mark.parametrize("stride", [1003, 1004, 1500])
 @pytest.mark.parametrize("start", [0, 1, 7])
 def test_gradient_rows_that_start_elsewhere(ops, stride, start):

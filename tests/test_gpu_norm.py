@@ -348,6 +348,23 @@ def test_the_binding_refuses(ops):
     assert none.grad.shape == (0, 100) and (wl.grad == 0).all()
 
 
+def test_tangents_are_refused(ops):
+    """Forward mode: a result without a tangent would stand for a derivative of zero."""
+    from torch.autograd import forward_ad
+    x, w, r = make(4, 100, torch.float32, 1), make(1, 100, torch.float32, 2)[0], make(4, 100, torch.float32, 3)
+    with forward_ad.dual_level():
+        for k in range(3):
+            args = [x, w, r]
+            args[k] = forward_ad.make_dual(args[k], torch.ones_like(args[k]))
+            for on in (True, False):
+                with torch.set_grad_enabled(on):
+                    with pytest.raises(NotImplementedError):
+                        ops.rms_norm(args[0], args[1], residual=args[2])
+                    with pytest.raises(ValueError, match="gradient"):
+                        ops.rms_norm_8bit(args[0], args[1], residual=args[2])
+        assert torch.equal(ops.rms_norm(args[0], args[1], residual=args[2].detach())[0], ops.rms_norm(x, w, residual=r)[0])
+
+
 def test_what_lies_between_rows_stays(ops):
     from paper_1412_1576_amd import lda
     x, stride = make(3, 1003, torch.bfloat16, 1), 1030

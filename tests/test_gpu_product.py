@@ -141,6 +141,15 @@ def test_the_binding_refuses(ops):
         ops.int8_matmul(wide, sa[:1], wide, sb[:1])
 
 
+def test_tangents_are_refused(ops):
+    from torch.autograd import forward_ad
+    a, b, sa, sb = integers(4, 64, 1), integers(8, 64, 2), scales(4, 3), scales(8, 4)
+    with forward_ad.dual_level():
+        for scale in ((forward_ad.make_dual(sa, sa), sb), (sa, forward_ad.make_dual(sb, sb))):
+            with pytest.raises(ValueError, match="gradient"), torch.no_grad():
+                ops.int8_matmul(a, scale[0], b, scale[1])
+
+
 @pytest.mark.parametrize("m,n", [(3, 100), (100, 300), (600, 70_000)])
 def test_what_lies_between_rows_stays(ops, m, n):
     from paper_1412_1576_amd import lda

@@ -218,3 +218,20 @@ def test_product_binding_refuses_host_tensors():
     x = torch.zeros(2, 8, dtype=torch.int8)
     with pytest.raises(ValueError, match="on the GPU"):
         operators.int8_matmul(x, torch.ones(2), x, torch.ones(2))
+
+
+def test_a_derivative_is_wanted():
+    """By leaves where gradients are on, by tangents of forward mode everywhere."""
+    from torch.autograd import forward_ad
+
+    from paper_1412_1576_amd import operators
+    x = torch.ones(2, 5)
+    leaf = x.clone().requires_grad_(True)
+    assert not operators._wants_gradient(x, None) and operators._wants_gradient(None, x, leaf)
+    with torch.no_grad():
+        assert not operators._wants_gradient(leaf)
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(x, x)
+        assert operators._wants_gradient(None, x, dual) and not operators._wants_gradient(x, None, "x")
+        with torch.no_grad():
+            assert operators._wants_gradient(dual) and not operators._wants_gradient(leaf, dual.detach())
