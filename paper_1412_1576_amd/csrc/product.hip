@@ -37,6 +37,7 @@ struct ProductArgs {
     int32_t splits, split_k;  // bytes of a row in each, a multiple of kTileK
     int32_t* partial;         // [splits][M][N]
     int32_t tiles_m, tiles_n;
+    int32_t block0;           // of the few-rows kernel, whose blocks are launched in stretches
 };
 
 __device__ __forceinline__ i32x4 load16(const int8_t* from)
@@ -77,13 +78,13 @@ __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs p)
     constexpr int kWaves = 4, kClasses = 16 * CT, kUnroll = 4;
     __shared__ int32_t part[kWaves][16][kClasses + 4];
     const int32_t tid = (int32_t)threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-    const int32_t n0 = (int32_t)blockIdx.x * kClasses, split = (int32_t)blockIdx.y;
+    const int32_t n0 = (p.block0 + (int32_t)blockIdx.x) * kClasses, left = p.N - n0, split = (int32_t)blockIdx.y;
     const int32_t from = split * p.split_k, end = min(p.K, from + p.split_k);
     const int32_t r = lane % 16, g = lane / 16 * 16;
     const int8_t* const a = p.a + min((int64_t)r, p.M - 1) * p.a_stride;
     const int8_t* b[CT];
 #pragma unroll
-    for (int i = 0; i < CT; ++i) b[i] = p.b + (int64_t)min(n0 + 16 * i + r, p.N - 1) * p.b_stride;
+    for (int i = 0; i < CT; ++i) b[i] = p.b + (int64_t)(n0 + min(16 * i + r, left - 1)) * p.b_stride;
     i32x4 sum[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c) sum[c] = i32x4{0, 0, 0, 0};
@@ -112,8 +113,9 @@ __global__ __launch_bounds__(256) void product_few_kernel(ProductArgs p)
     __syncthreads();
     T* const out = static_cast<T*>(p.out);
     for (int32_t i = tid; i < 16 * kClasses; i += 256) {
-        const int32_t m = i / kClasses, c = i % kClasses, n = n0 + c;
-        if (m >= p.M || n >= p.N) continue;
+        const int32_t m = i / kClasses, c = i % kClasses;
+        if (m >= p.M || c >= left) continue;
+        const int32_t n = n0 + c;
         const int32_t s = part[0][m][c] + part[1][m][c] + part[2][m][c] + part[3][m][c];
         if (p.splits > 1) p.partial[((int64_t)split * p.M + m) * p.N + n] = s;
         else out[m * p.out_stride + n] = Row<T>::from(scaled(s, p.a_scale[m], p.b_scale[n]));
@@ -562,12 +564,17 @@ static hipError_t launch_product(ProductArgs a, const ProductPlan& plan, hipStre
     a.splits = plan.splits;
     a.split_k = plan.split_k;
     const auto few = [&](auto ct) {
-        const dim3 grid((unsigned)((a.N + 16 * ct() - 1) / (16 * ct())), (unsigned)a.splits);
-        product_few_kernel<T, ct()><<<grid, 256, 0, stream>>>(a);
+        // a launch has less than 2^32 threads
+        constexpr int32_t kMost = 1 << 22;
+        const int32_t blocks = (int32_t)(((int64_t)a.N + 16 * ct() - 1) / (16 * ct()));
+        for (a.block0 = 0; a.block0 < blocks; a.block0 += kMost) {
+            const dim3 grid((unsigned)(blocks - a.block0 < kMost ? blocks - a.block0 : kMost), (unsigned)a.splits);
+            product_few_kernel<T, ct()><<<grid, 256, 0, stream>>>(a);
+        }
     };
     const auto tile = [&](auto tm, auto tn, auto wm, auto wn, auto aligned) {
         a.tiles_m = (int32_t)((a.M + tm() - 1) / tm());
-        a.tiles_n = (a.N + tn() - 1) / tn();
+        a.tiles_n = (int32_t)(((int64_t)a.N + tn() - 1) / tn());
         constexpr size_t lds = ProductStage<tm(), tn(), wm(), wn()>::kLds;
         const auto kernel = product_tile_kernel<T, tm(), tn(), wm(), wn(), aligned()>;
         if (lds > 65536) {

@@ -220,6 +220,22 @@ def test_far_into_memory(ops):
     assert torch.equal(got[-300:], want)
 
 
+def test_as_many_classes_as_there_may_be(ops):
+    """2^31 - 1 classes: the first, those about the launches' and the middle's borders, and the last."""
+    n = 2 ** 31 - 1
+    torch.cuda.empty_cache()
+    b, sb = integers(n, 1, 1), scales(n, 2)
+    for m in (1, 9):    # by the few-rows kernel, by tiles
+        a, sa = integers(m, 1, 3), scales(m, 4)
+        got = ops.int8_matmul(a, sa, b, sb)
+        for at in (0, 2 ** 22 * 64 - 1000, 2 ** 30 - 1000, n - 2000):
+            some = slice(at, at + 2000)
+            assert torch.equal(got[:, some], definition(a, sa, b[some], sb[some], torch.bfloat16))
+        del got
+    del b, sb
+    torch.cuda.empty_cache()
+
+
 def test_a_head(ops):
     """Norm to 8 bits, product, log probabilities: hidden rows to what is read off their logits, against the same from
     the numbers that the 8 bits stand for."""
