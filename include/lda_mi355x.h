@@ -421,7 +421,7 @@ int lda_doc_topics(lda_ctx* ctx, int64_t rows, const int32_t* docs, int32_t slot
  * whose max |y| is below 2^-100 has scale 0 and out 0, one with a NaN or an infinity in y has scale NaN and out 0.
  * Gradient, from y' of y and h' of the sum (NULL: 0), with u = y' w:
  *   x' = r' = h' + (u - n mean over the row of u n) / sqrt(mean of h^2 + eps);  w' = sum over the rows of y' n
- * Sums are 32-bit; squares that leave 32 bits are scaled.
+ * Sums are 32-bit, over rows of more than 16384 numbers 64-bit but for 8 numbers each; squares that leave 32 bits are scaled.
  */
 #define LDA_INT8 0
 #define LDA_E4M3 1

@@ -120,6 +120,12 @@ __device__ __forceinline__ uint32_t block_top(uint32_t v, uint32_t* part)  // la
     return v;
 }
 
+// What a thread's sum over a row is held in.  A thread has 16 numbers of a row in registers, and any number of a wider one:
+// 32 bits would be rounded the same way at each addition where the numbers are alike (1.1 in 2^26 places: 6e-4 of
+// the squares).  Each chunk is summed in 32.
+template <bool WIDE>
+using RowSum = std::conditional_t<WIDE, double, float>;
+
 // n = (h * first) * second.  first is 1 but where squares leave 32 bits.
 struct NormFactor {
     float first, second;
@@ -249,7 +255,7 @@ __global__ __launch_bounds__(BLOCK) void norm_kernel(NormArgs a)
 {
     constexpr bool k8 = !std::is_same<Q, T>::value, kWide = CHUNKS == 0;
     constexpr int kHeld = kWide ? 1 : CHUNKS, kStep = BLOCK * kNormChunk;
-    __shared__ float part[BLOCK / kWave];
+    __shared__ RowSum<kWide> part[BLOCK / kWave];
     __shared__ uint32_t part_top[BLOCK / kWave];
     const int32_t tid = (int32_t)threadIdx.x, H = a.H;
     const int64_t row = a.row0 + blockIdx.x;
@@ -291,13 +297,20 @@ __global__ __launch_bounds__(BLOCK) void norm_kernel(NormArgs a)
             if (i < H) load(i, h[j]);
         }
     }
-    float squares = 0.0f;
-    each([&](int32_t i, int j) {
-        if (r) store_some(sum, i, H, h[j]);
+    const auto sum_of_squares = [&](float first, auto also) {
+        RowSum<kWide> s = 0;
+        each([&](int32_t i, int j) {
+            also(i, j);
+            float t = kWide ? 0.0f : (float)s;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) squares = __builtin_fmaf(h[j][e], h[j][e], squares);
+            for (int e = 0; e < 8; ++e) t = __builtin_fmaf(h[j][e] * first, h[j][e] * first, t);
+            s = kWide ? s + t : t;
+        });
+        return (float)block_sum<BLOCK>(s, part);
+    };
+    float squares = sum_of_squares(1.0f, [&](int32_t i, int j) {
+        if (r) store_some(sum, i, H, h[j]);
     });
-    squares = block_sum<BLOCK>(squares, part);
     float first = 1.0f;
     // rare: squares left 32 bits and eps does not hide it, or the row is 0
     if (!(squares + (float)H * a.eps >= kLeastSquares && squares <= kMostSquares)) {
@@ -307,12 +320,7 @@ __global__ __launch_bounds__(BLOCK) void norm_kernel(NormArgs a)
             for (int e = 0; e < 8; ++e) top = max(top, magnitude(h[j][e]));
         });
         first = power_for(max(block_top<BLOCK>(top, part_top), __float_as_uint(sqrtf(a.eps))));
-        squares = 0.0f;
-        each([&](int32_t, int j) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) squares = __builtin_fmaf(h[j][e] * first, h[j][e] * first, squares);
-        });
-        squares = block_sum<BLOCK>(squares, part);
+        squares = sum_of_squares(first, [](int32_t, int) {});
     }
     const NormFactor f = factor_of(squares, first, H, a.eps);
     if (a.stats && tid == 0) *reinterpret_cast<float2*>(a.stats + row * kNormStats) = make_float2(f.first, f.second);
@@ -396,7 +404,7 @@ __global__ __launch_bounds__(BLOCK) void norm_grad_kernel(NormGradArgs a)
 {
     constexpr bool kWide = CHUNKS == 0;
     constexpr int kHeld = kWide ? 1 : CHUNKS, kStep = BLOCK * kNormChunk;
-    __shared__ float part[BLOCK / kWave];
+    __shared__ RowSum<kWide> part[BLOCK / kWave];
     const int32_t tid = (int32_t)threadIdx.x, H = a.H;
     float n[kHeld][8], g[kHeld][8], w[kHeld][8], sums[kHeld][8];
 #pragma unroll
@@ -434,16 +442,18 @@ __global__ __launch_bounds__(BLOCK) void norm_grad_kernel(NormGradArgs a)
             if (kWide) load_weight<T>(a.weight, a.weight_type, i, H, w[j]);
         };
         if (!kWide) each(load);
-        float along = 0.0f;
+        RowSum<kWide> sum = 0;
         each([&](int32_t i, int j) {
             if (kWide) load(i, j);
+            float t = kWide ? 0.0f : (float)sum;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float gn = g[j][e] * n[j][e];
                 if (kWide) sums[0][e] = gn;
                 else if (i + e < H) sums[j][e] += gn;
-                along = __builtin_fmaf(gn, i + e < H ? w[j][e] : 0.0f, along);
+                t = __builtin_fmaf(gn, i + e < H ? w[j][e] : 0.0f, t);
             }
+            sum = kWide ? sum + t : t;
             if (kWide && partial) {
                 float before[8];
                 if (!fresh) load_some(partial, i, H, before);
@@ -454,7 +464,7 @@ __global__ __launch_bounds__(BLOCK) void norm_grad_kernel(NormGradArgs a)
         });
         fresh = false;
         if (!gx && !gr) continue;
-        along = block_sum<BLOCK>(along, part) / (float)H;
+        const float along = (float)block_sum<BLOCK>(sum, part) / (float)H;
         each([&](int32_t i, int j) {
             if (kWide) load(i, j);
             float b[8];

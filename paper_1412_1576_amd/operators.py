@@ -416,7 +416,7 @@ def rms_norm(x, weight=None, *, residual=None, eps=1e-6):
     x [rows, width] float32, float16 or bfloat16; weight [width] and residual [rows, width] of x's type or
     float32.  The sum has the residual's type and y is the norm of the sum as it is written, in x's type.
     Differentiable in x, weight and residual (backward: tangents of forward mode raise NotImplementedError); sums are
-    32-bit.  Rows of a tensor may lie any distance apart; within a row elements are adjacent.  A backward pass captured
+    32-bit at least.  Rows of a tensor may lie any distance apart; within a row elements are adjacent.  A backward pass captured
     into a graph must find no eager graph of the same leaves alive.
     """
     eps = float(eps)

@@ -247,6 +247,25 @@ def test_levels_are_those_of_64_bits(ops, width, dtype):
             assert torch.equal(q.double()[clear], (torch.round(places) * step)[clear])
 
 
+def test_very_wide_rows_of_like_numbers(ops):
+    """Each addition of a long sum in 32 bits would be rounded the same way.  A chunk's 8 numbers are added in 32 bits, the
+    chunks in 64: 8 roundings of the squares, halved by the root, and seven more; the gradient's mean has 8 and six of its
+    terms, then 8 roundings of numbers below 3."""
+    width = 1 << 26
+    x = torch.full((2, width), 1.1, device="cuda")
+    x[1, ::3] = 0.3
+    n, _, inv = forward(x, None, 1e-6)
+    leaf = x.clone().requires_grad_(True)
+    y = ops.rms_norm(leaf)
+    close(y.detach(), n, n * (8 / 2 + 7 + 1) * U, "y")
+    gy = torch.full_like(x, 0.7)
+    got, = torch.autograd.grad(y, leaf, gy)
+    want = (gy.double() - n * (gy.double() * n).mean(1, keepdim=True)) * inv
+    close(got, want, 3 * (8 + 6 + 2 * 11 + 8) * U, "gradient")
+    q, scale = ops.rms_norm_8bit(x)
+    close(scale, n.amax(1) / 127, n.amax(1) / 127 * (8 / 2 + 7 + 3) * U, "scale")
+
+
 def test_gradient_against_differences(ops):
     """(f(x + h d) - f(x - h d)) / 2h of f = sum(gy y) + sum(gh sum), rows of 60 with a mean square near 1, d of
     length 1.  n is smooth in x at the scale of the row's length, 7.7: a third derivative of gy y along d is at most
