@@ -49,7 +49,7 @@ struct NormGradArgs {
     int64_t residual_grad_stride;
     float* partial;  // [groups][H], or NULL: no gradient of the weight
     void* weight_grad;
-    int32_t groups;
+    int32_t groups, column0;  // column0: of a launch of norm_weight_grad_kernel
 };
 
 // The 8 elements from p on; p is aligned to its type, which is all that the hardware's loads ask for.
@@ -493,7 +493,7 @@ template <class W>
 __global__ __launch_bounds__(kWeightBlock * kWeightLanes) void norm_weight_grad_kernel(NormGradArgs a)
 {
     __shared__ float part[kWeightLanes][kWeightBlock];
-    const int32_t column = (int32_t)(blockIdx.x * kWeightBlock + threadIdx.x % kWeightBlock), q = threadIdx.x / kWeightBlock;
+    const int32_t column = a.column0 + (int32_t)(blockIdx.x * kWeightBlock + threadIdx.x % kWeightBlock), q = threadIdx.x / kWeightBlock;
     float s = 0.0f;
     if (column < a.H) {
 #pragma unroll 8
@@ -711,9 +711,13 @@ try {
                 norm_grad_kernel<T, S, block(), chunks()><<<a.groups, block(), 0, stream>>>(a);
             });
         if (!with_weight) return;
-        const unsigned n = (unsigned)((a.H + kWeightBlock - 1) / kWeightBlock);
-        if (d->weight_type == LDA_F32) norm_weight_grad_kernel<float><<<n, kWeightBlock * kWeightLanes, 0, stream>>>(a);
-        else norm_weight_grad_kernel<T><<<n, kWeightBlock * kWeightLanes, 0, stream>>>(a);
+        constexpr int32_t kMost = 1 << 20;  // a launch has less than 2^32 threads
+        for (; a.column0 < a.H; a.column0 += kMost * kWeightBlock) {
+            const int32_t left = (a.H - a.column0 + kWeightBlock - 1) / kWeightBlock;
+            const unsigned n = (unsigned)(left < kMost ? left : kMost);
+            if (d->weight_type == LDA_F32) norm_weight_grad_kernel<float><<<n, kWeightBlock * kWeightLanes, 0, stream>>>(a);
+            else norm_weight_grad_kernel<T><<<n, kWeightBlock * kWeightLanes, 0, stream>>>(a);
+        }
     });
     LDA_HIP(static_cast<lda_ctx*>(nullptr), hipGetLastError());
     return LDA_OK;

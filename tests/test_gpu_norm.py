@@ -466,6 +466,39 @@ def test_rows_far_into_memory(ops):
     assert torch.equal(g[-600:], gp)
 
 
+def test_the_widest_row(ops):
+    """2^30 numbers, the most that a row may have: its norm, 8 bits and gradients, the weight's by more threads than a launch
+    has.  The row is 1 but for a few larger numbers, here and there."""
+    width = 1 << 30
+    torch.cuda.empty_cache()
+    x = torch.ones(1, width, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 1, (1 << 26) - 1, 1 << 26, (1 << 28) + 5, width // 2, width - 1], device="cuda")
+    x[0, at] = torch.tensor([3.0, -2.0, 1.5, 100.0, 7.0, -0.5, 9.0], device="cuda").bfloat16()
+    w = torch.ones(width, dtype=torch.bfloat16, device="cuda")
+    w[at] = 2.0
+    square = (width - 7 + 9 + 4 + 2.25 + 10_000 + 49 + 0.25 + 81) / width
+    root = (square + 1e-6) ** 0.5
+    leaf, wl = x.requires_grad_(True), w.requires_grad_(True)
+    y = ops.rms_norm(leaf, wl)
+    some = torch.cat([at, at[:-1] + 2])
+    n = x.detach()[0, some].double() / root
+    want = n * w.detach()[some].double()
+    close(y.detach()[0, some], want, want.abs() * (12 * U + half(x.dtype) * 1.001), "y")
+    gx, gw = torch.autograd.grad(y, (leaf, wl), torch.ones_like(y))
+    close(gw[some], n, n.abs() * (13 * U + half(x.dtype) * 1.001), "gradient of the weight")
+    # mean of w n over the row, the others are 1 / root each
+    along = (width - 7 + 2 * (3.0 - 2.0 + 1.5 + 100.0 + 7.0 - 0.5 + 9.0)) / width / root
+    u = w.detach()[some].double()
+    d = (u - n * along) / root
+    close(gx[0, some], d, (u + n.abs()) * 30 * U + d.abs() * half(x.dtype) * 1.001, "gradient of x")
+    del y, gx, gw, leaf, wl
+    q, scale = ops.rms_norm_8bit(x.detach(), w.detach())
+    assert torch.equal(q[0, some].double(), torch.round(want / want.max() * 127))
+    close(scale, want.max()[None] / 127, want.max() / 127 * 14 * U, "scale")
+    del q, x, w
+    torch.cuda.empty_cache()
+
+
 def test_more_rows_than_a_launch_has(ops):
     n = (1 << 20) + 5
     x = torch.randn(n, 9, device="cuda")
