@@ -490,8 +490,9 @@ static ProductPlan plan_product(const lda_product_rows* d)
         groups = tiles(64, 128);
     } else {
         // 4096 x 4096 x 32768 (2048 tiles): 496 us by 256 x 256, 682 by 128 x 128; 2048 x 4096 x 10000 (320): 104 and 92
-        // (up to 128 rows nothing is packed, and the larger tile has buffers alone)
-        p.kind = tiles(256, 256) >= 768 && (p.aligned || d->rows > 128) ? ProductKind::kTile256 : ProductKind::kTile128;
+        // Up to 128 rows half of a larger tile would be empty (100 x 4096 x 200003: 194 us by 128 x 128, 259), and nothing is
+        // packed, while the larger tile has buffers alone.
+        p.kind = d->rows > 128 && tiles(256, 256) >= 768 ? ProductKind::kTile256 : ProductKind::kTile128;
         groups = p.kind == ProductKind::kTile256 ? tiles(256, 256) : tiles(128, 128);
         const int64_t packed = ((int64_t)d->width + 15) / 16 * 16;
         // 516 x 7937 x 21153: 277 us as they lie, 245 packed first; 87 x 10049 x 14837: 76 and 105
