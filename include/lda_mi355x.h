@@ -496,8 +496,8 @@ typedef struct lda_product_rows {
 
 /* Bytes of workspace that the call needs (may be 0), or a negative LDA_ERR_*. */
 int64_t lda_product_workspace(const lda_product_rows* rows);
-/* out [rows][classes], rows out_stride apart; what lies between rows is left as it was.  Of more than 64 rows a and b are
- * copied into the workspace first, unless pointers, strides and width are multiples of 16. */
+/* out [rows][classes], rows out_stride apart; what lies between rows is left as it was.  Of more than 128 rows a side
+ * is copied into the workspace first, unless its pointer, its stride (below 2^22) and the width are multiples of 16. */
 int lda_product(const lda_product_rows* rows, void* out, int64_t out_stride);
 
 /*
