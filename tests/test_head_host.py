@@ -213,6 +213,17 @@ def test_product_refuses_outputs_and_workspaces(lib):
     assert C.sizeof(lda.lda_product_rows) == 8 + 8 + 16 + 8 + 16 + 8 + 8 + 24 + 16
 
 
+def test_which_sides_of_a_product_are_packed(lib):
+    """Above 128 rows, where a side does not lie in pieces of 16 bytes less than 2^22 apart; both where the width is no
+    multiple of 16."""
+    def need(rows, width=1008, **kw):
+        return lib.lda_product_workspace(product(rows=rows, classes=200_000, width=width, **{"a_stride": 1008, "b_stride": 1008, **kw}))
+    assert need(128, width=1000) == need(128, b_stride=1009) == need(129) == 0
+    assert need(129, width=1000) == (129 + 200_000) * 1008
+    assert need(129, a=(1 << 20) + 1) == need(129, a_stride=1 << 22) == need(129, a_stride=1009) == 129 * 1008
+    assert need(129, b=(1 << 20) + 8) == need(129, b_stride=1024 + 8) == 200_000 * 1008
+
+
 def test_product_binding_refuses_host_tensors():
     from paper_1412_1576_amd import operators
     x = torch.zeros(2, 8, dtype=torch.int8)
