@@ -182,6 +182,19 @@ def test_sizes_of_numbers(ops):
         assert scale[0] == 0 and (q[0] == 0).all() and scale[1] > 0
 
 
+@pytest.mark.parametrize("n,width", [(2100, 300), (1100, 1500), (600, 4100), (520, 16_500)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_of_different_sizes(ops, n, width, dtype):
+    """Orders of magnitude between neighbours, more rows than a gradient has workgroups: another row's root or scale would
+    show."""
+    size = 10.0 ** torch.randint(-6, 7, (n, 1), generator=torch.Generator().manual_seed(n), dtype=torch.float32).cuda()
+    for kind in (None, torch.float32):
+        x, r = make(n, width, TYPES[dtype], 1) * size.to(TYPES[dtype]), None
+        if kind is not None:
+            r = make(n, width, kind, 2) * size
+        check(ops, x, make(1, width, TYPES[dtype], 3)[0], r, eps=0.0)
+
+
 @pytest.mark.parametrize("width", [130, 3000, 20_000])
 def test_numbers_that_are_none(ops, width):
     inf, nan = float("inf"), float("nan")
