@@ -247,8 +247,9 @@ __device__ __forceinline__ void store_levels(Q* row, int32_t i, int32_t H, uint2
 }
 
 // T: of x and y; S: of the residual and the sum; Q: T, or 8 bits.  Bound by memory: 16384 x 8192 bf16 with a bf16
-// residual to e4m3 take 185 us, 5.1 TB/s of read and written bytes (a copy of 1 GiB: 5.15), 165 with levels rounded from 32
-// bits alone; 8192 x 4096 bf16 with a float32 residual 83 us.  One row of 4096: 2.5 us, the latency of its loads and of a
+// residual to e4m3 take 183 us, one call after the other (194 under the profiler), to int8 179 to 188, 5.1 TB/s of read and
+// written bytes (a copy of 1 GiB: 5.15), 165 with levels rounded from 32 bits alone; 8192 x 4096 bf16 with a float32 residual
+// 83 us.  One row of 4096: 2.5 us, the latency of its loads and of a
 // reduction.  A row's elements and weights stay in registers, 16 of each at most, between the reductions.
 template <class T, class S, class Q, int BLOCK, int CHUNKS>
 __global__ __launch_bounds__(BLOCK) void norm_kernel(NormArgs a)
@@ -530,8 +531,8 @@ static int check_norm(const lda_norm_rows* d, const char* call)
 
 // Threads and chunks of a thread that hold a row, 0 chunks: a row too wide for registers; and how many workgroups share
 // the rows of a gradient (each has its partial sum of the weight's).  8192 x 1024 bf16: 10.6 us by 64 threads of two
-// chunks, 13.6 by 256 of one; x 4096: 38.8 by 512, 40.4 by 256 of two, 46 by 1024.  Gradients of 65536 x 512: 60 us by 2048
-// workgroups, 174 by 512; of 8192 x 8192: 104 by 512, 110 by 1024; of 8192 x 4096 with a float32 sum and the partial sums' own
+// chunks, 13.6 by 256 of one; x 4096: 38.8 by 512, 40.4 by 256 of two, 46 by 1024.  Gradients, of a bf16 residual too, of 65536 x 512: 60 us by 2048
+// workgroups, 174 by 512 (without a residual 43 by 2048); of 8192 x 8192: 104 by 512, 110 by 1024; of 8192 x 4096 with a float32 sum and the partial sums' own
 // pass: 105 by 512, 111 by 1024.
 struct NormShape {
     int block, chunks, groups;

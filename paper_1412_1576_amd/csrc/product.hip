@@ -318,7 +318,8 @@ __global__ __launch_bounds__(WM * WN * 64, 1) void product_tile_kernel(ProductAr
             k += kTileK;
         } while (k < tile.end);
         // (the sums stay in their registers until they are written: the compiler fetched them in every turn of the loop, or all at
-        // once behind it, and put others into memory)
+        // once behind it.  With all 512 registers of a lane taken, tiles of 256 x 256 still put 132 to 192 bytes into memory, before the
+        // loops, that are read between a tile's products and its way out, none in the loop of products)
 #pragma unroll
         for (int n = 0; n < kNi; ++n)
 #pragma unroll
@@ -479,8 +480,8 @@ static ProductPlan plan_product(const lda_product_rows* d)
     const auto tiles = [&](int64_t m, int64_t n) { return ((d->rows + m - 1) / m) * ((d->classes + n - 1) / n); };
     const bool whole = d->width % 16 == 0, a_fine = whole && in_pieces(d->a, d->a_stride), b_fine = whole && in_pieces(d->b, d->b_stride);
     p.aligned = a_fine && b_fine;
-    // 16 x 5120 x 101636: 134 us by the few-rows kernel, 106 by tiles; 16 x 4096 x 10000: 14.6 and 25; 8 x 4096 x
-    // 141043: 121 and 126
+    // 16 x 5120 x 101636: 137 us by the few-rows kernel, 106 by tiles; 16 x 4096 x 10000: 15.5 and 16 (in 3 splits, two
+    // launches); 8 x 4096 x 141043: 119 and 127
     if (d->rows <= 8 || (d->rows <= 16 && d->classes < 65536)) {
         p.kind = ProductKind::kFew;
         p.classes = d->classes >= 32768 ? 4 : d->classes >= 16384 ? 2 : 1;
@@ -489,20 +490,23 @@ static ProductPlan plan_product(const lda_product_rows* d)
         p.kind = ProductKind::kTile64;
         groups = tiles(64, 128);
     } else {
-        // 4096 x 4096 x 32768 (2048 tiles): 496 us by 256 x 256, 682 by 128 x 128; 2048 x 4096 x 10000 (320): 104 and 92
+        // 4096 x 4096 x 32768 (2048 tiles of 256 x 256): 544 us by these, 810 by 128 x 128; 2048 x 4096 x 10000 (320): 113 and 99.
+        // Between the two what counts is how full the last round of 256 CUs is (4096 x 4096 x 8192, two whole rounds: 137 and 166),
+        // which this rule does not ask.
         // Up to 128 rows half of a larger tile would be empty (100 x 4096 x 200003: 194 us by 128 x 128, 259), and nothing is
         // packed, while the larger tile has buffers alone.
         p.kind = d->rows > 128 && tiles(256, 256) >= 768 ? ProductKind::kTile256 : ProductKind::kTile128;
         groups = p.kind == ProductKind::kTile256 ? tiles(256, 256) : tiles(128, 128);
         const int64_t packed = ((int64_t)d->width + 15) / 16 * 16;
-        // 516 x 7937 x 21153: 277 us as they lie, 245 packed first; 87 x 10049 x 14837: 76 and 105
+        // 516 x 7937 x 21153: 277 us as they lie, 245 packed first (227 on another card, 56 of it the packing); 87 x 10049 x 14837:
+        // 76 and 105
         if (d->rows > 128 && !a_fine) p.a_bytes = d->rows * packed;
         if (d->rows > 128 && !b_fine) p.b_bytes = d->classes * packed;
         if (d->rows > 128) p.aligned = true;
     }
-    // A split's second kernel takes 3 to 4 us, so that a split has some bytes of a row at least.  1 x 16384 x 1000: 13.7 us
-    // whole, 16.4 in 2 splits; 1 x 131008 x 1000: 136, and 45 in 16; 300 x 2048 x 2000: 13 whole, 15.6 in 2; 300 x 8192 x 1000: 34
-    // and 19 in 4
+    // A split's second kernel takes 4 to 5 us and a launch, so that a split has some bytes of a row at least.  1 x 16384 x
+    // 1000: 11 us whole, 12 to 15 in 2 splits; 1 x 131008 x 1000: 81 whole, 29 in 4 (as many as 63 workgroups make), 27 in 16; 300 x
+    // 2048 x 2000: 12 whole, 16 in 2; 300 x 8192 x 1000: 33 and 20 in 4
     int64_t splits = groups >= 192 ? 1 : 256 / (groups < 1 ? 1 : groups);
     const int64_t most = d->width / (p.kind == ProductKind::kFew ? 16384 : 2048);
     if (splits > most) splits = most;

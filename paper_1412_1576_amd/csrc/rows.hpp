@@ -1,5 +1,5 @@
-// What the row operators (distill.hip, verify.hip, top_topics.hip) share: element types, reductions
-// over a wave and over a workgroup.
+// What the row operators (distill.hip, verify.hip, top_topics.hip, norm.hip, log_probs.hip, product.hip) share: element
+// types, reductions over a wave and over a workgroup.
 #pragma once
 
 #include <hip/hip_bf16.h>
